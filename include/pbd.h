@@ -85,6 +85,7 @@ typedef void* pbd_stream_t;            /* hipStream_t */
 #define PBD_STATUS_FORCED_N  4         /* forced accepted count outside [0, D] */
 #define PBD_STATUS_TIMEOUT   8         /* a bounded wait of the persistent batch-1 pass gave up:
                                           that pass's outputs are invalid */
+#define PBD_STATUS_PAGE     16         /* a page id outside [0, n_pages) among the pages a sequence uses */
 
 /*
  * Model and capacity description.  The backbone is a Qwen3-style decoder
@@ -324,6 +325,184 @@ int pbd_accept_commit(pbd_ctx* ctx, int32_t batch, const int32_t* draft, const i
  * reading is reported there, not mixed into the status bits).
  */
 int pbd_sync_status(pbd_ctx* ctx, pbd_stream_t stream, int32_t* status);
+
+/* ------------------------------------------------------------------------
+ * Operators over a paged KV cache, and log probabilities of tokens.
+ *
+ * These take no context: a program that decodes one token at a time uses them
+ * on a cache of its own layout, and pbd_decode_paged runs them inside a pass.
+ * Pointers are device pointers unless a comment says host; nothing is allocated;
+ * calls are asynchronous on `stream`, whose device must be current, and can be
+ * captured in a HIP graph.  A workspace belongs to one call at a time: calls
+ * that may overlap (other streams, graphs replayed side by side) take one each.
+ * Errors that the host can detect are returned before anything is enqueued,
+ * with pbd_last_error(NULL) for the message.  Errors that only the device can
+ * detect are OR-ed into the device word `status` (NULL: dropped; the caller
+ * clears it) and the sequence (or row) is skipped: all its outputs stay as
+ * they were.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * A paged KV cache.  A sequence's positions are slots 0, 1, ...; slot i lies in
+ * page table[b * table_width + i / page_size].  A page of one KV head is
+ * page_size / 16 blocks of 16 slots, each 16 * head_dim elements in the order of
+ * the context's own cache: with E = 16 bytes of elements,
+ *   K[slot][dim] at ((dim / E) * 16 + slot) * E + dim % E
+ *   V[slot][dim] at ((dim / 16 * 4 + slot / 4) * 16 + dim % 16) * 4 + slot % 4
+ * (slot within the block).  Page p of KV head h starts at element
+ * p * page_stride + h * head_stride of k and of v; both strides are multiples of
+ * 16 * head_dim, k and v are 16-byte aligned.  Pages may be shared by sequences
+ * that only read them.  Table entries past the pages a call uses are not read.
+ * score and slot_pos (both optional) hold, per sequence, KV head and slot, the
+ * attention weight accumulated so far and the position of the token in the
+ * slot; [batch][n_kv_heads][slot_stride].
+ */
+typedef struct pbd_pages {
+    int32_t dtype;              /* PBD_DTYPE_* of k and v */
+    int32_t n_q_heads;          /* a multiple of n_kv_heads; at most 16384 / head_dim */
+    int32_t n_kv_heads;
+    int32_t head_dim;           /* 64 or 128 */
+    int32_t page_size;          /* 16 times a power of two, at most 4096 */
+    int32_t n_pages;            /* page ids lie in [0, n_pages) */
+    int64_t page_stride;        /* elements */
+    int64_t head_stride;        /* elements */
+    int64_t layer_stride;       /* elements from a layer's cache to the next (pbd_decode_paged only) */
+    void* k;
+    void* v;
+    const int32_t* table;       /* [batch][table_width] */
+    int32_t table_width;        /* at least 1; a sequence has at most table_width * page_size <= 2^30 slots */
+    float* score;               /* NULL: no weights are accumulated */
+    int32_t* slot_pos;          /* NULL: no positions are kept */
+    int64_t slot_stride;        /* at least the slots any call uses */
+    int64_t state_layer_stride; /* elements of score and slot_pos from a layer to the next (pbd_decode_paged only) */
+    int32_t* status;            /* device word, or NULL */
+} pbd_pages;
+
+/*
+ * Append rows to the cache.  Sequence b has lens[b] slots in use and gets
+ * n_new[b] more (n_new NULL: max_new each; in [0, max_new]).  Its row i is row
+ * b * max_new + i of k, v and q: rows of n_kv_heads * head_dim (k, v) and
+ * n_q_heads * head_dim (q) floats, row_stride floats apart, so that all three
+ * may be columns of one projection's output.  Per head, k (and q) are RMS
+ * normalised over head_dim with the gains k_norm (q_norm; elements of
+ * pages->dtype; NULL: not normalised) and rotated (rotate-half RoPE) by row
+ * pos[b] + i of rope, [rope_len][head_dim / 2] pairs (cos, sin); v is taken as
+ * it is.  K and V go to slots lens[b] + i, rounded once to pages->dtype; those
+ * slots' score becomes 0 and their slot_pos the position, where the cache has
+ * them.  q (NULL: none) goes to q_out [batch][max_new][n_q_heads * head_dim].
+ * lens_out (NULL: not wanted; not lens itself) receives lens[b] + n_new[b].
+ * Rows past n_new are not read and their q_out rows stay as they were.
+ * PBD_STATUS_CAPACITY: lens, n_new or pos out of range, or no room in the table
+ * or in rope.  q, k, v, q_out and rope are 16-byte aligned, row_stride is a
+ * multiple of 4; q_out overlaps no input.  A page that is appended to belongs
+ * to one sequence.
+ */
+int pbd_paged_append(const pbd_pages* pages, int32_t batch, int32_t max_new,
+                     const float* q, const float* k, const float* v, int64_t row_stride,
+                     const int32_t* lens, const int32_t* n_new, const int32_t* pos,
+                     const void* q_norm, const void* k_norm, float eps,
+                     const float* rope, int32_t rope_len,
+                     float* q_out, int32_t* lens_out, pbd_stream_t stream);
+
+/*
+ * Attention of one new token per sequence over the lens[b] slots of its cache
+ * (the new token's own slot among them: append first).  Query head h reads KV
+ * head h * n_kv_heads / n_q_heads.  With w_i = exp(scale q.k_i) / sum_j exp(scale
+ * q.k_j): out[b][h] = sum_i w_i v_i, lse[b][h] = log sum_j exp(scale q.k_j)
+ * (natural; NULL: not wanted), and, if the cache has scores, score[b][kv head][i]
+ * += the sum of w_i over that KV head's query heads.  A sequence of no slots
+ * gives out = 0, lse = -inf.  Slots past lens[b] may hold anything.
+ * q: float, heads contiguous, q_stride floats from a sequence to the next
+ * (16-byte aligned, a multiple of 4).  out: float [batch][n_q_heads][head_dim],
+ * 16-byte aligned.  max_len: host bound on lens, in [1, table_width * page_size];
+ * the work is laid out for it.  PBD_STATUS_CAPACITY: lens[b] outside [0, max_len].
+ * Products and sums are held to fp32 rounding: a bf16 cache meets queries and
+ * weights carried as three bf16 terms each.  Results are bitwise the same from run
+ * to run, and do not depend on the other sequences of the batch but for its size.
+ * ws: 16-byte aligned, of at least pbd_paged_attention_workspace_bytes (0 if
+ * the arguments are invalid).
+ */
+size_t pbd_paged_attention_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t max_len);
+int pbd_paged_attention(const pbd_pages* pages, int32_t batch, const float* q, int64_t q_stride,
+                        const int32_t* lens, int32_t max_len, float scale,
+                        float* out, float* lse, void* ws, size_t ws_bytes, pbd_stream_t stream);
+
+/*
+ * Eviction by accumulated attention weight.  Each KV head of each sequence
+ * keeps min(keep[b], lens[b]) of its lens[b] slots: first those that always
+ * stay (slot_pos >= pos[b] - recent or slot_pos < sink; pos is the position of
+ * the next token; without slot_pos, recent and sink must be 0), then by
+ * descending score (NaN last); equal ones by ascending slot.  The kept slots at
+ * or past the new length move, K, V, score and position, into the evicted
+ * slots below it, the i-th (ascending) into the i-th; every other slot stays
+ * where it is.  score_out and slot_pos_out (the latter iff the cache has slot_pos)
+ * receive the first new-length entries, in the layout of score; each may be
+ * the cache's own array or must not overlap it.  new_lens[b] receives the new
+ * length; it may be lens.  max_len: host bound on lens, in [1, table_width *
+ * page_size].  PBD_STATUS_CAPACITY: lens[b] outside [0, max_len] or keep[b] < 0.
+ * The pages of the sequences must not be shared.
+ */
+size_t pbd_paged_evict_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t max_len);
+int pbd_paged_evict(const pbd_pages* pages, int32_t batch, const int32_t* lens, int32_t max_len,
+                    const int32_t* keep, const int32_t* pos, int32_t recent, int32_t sink,
+                    float* score_out, int32_t* slot_pos_out, int32_t* new_lens,
+                    void* ws, size_t ws_bytes, pbd_stream_t stream);
+
+/*
+ * Log probabilities under the softmax of each row of logits [rows][vocab]
+ * (elements of dtype, row_stride elements from a row to the next, any
+ * alignment), as the passes return them: logprob[r] of tokens[r] (both NULL:
+ * not wanted), the row's entropy in nats (NULL: not wanted), and its top_n
+ * most likely tokens in [0, 32] with their log probabilities, [rows][top_n] each,
+ * descending, the lower id first among equal logits.  A token of -1 marks a
+ * padding row (pbd_accept_commit's out_tokens past the accepted ones): it is
+ * skipped.  Any other token outside [0, vocab) raises PBD_STATUS_TOKEN in
+ * *status and skips the row.  Tokens whose logit is -inf (masked) or NaN are
+ * never among the most likely; missing ones have id -1 and log probability -inf.
+ * A row whose every logit is -inf has logprob -inf and entropy 0.  A row with a
+ * NaN or +inf has NaN logprob, entropy and top log probabilities.  The sums are
+ * taken relative to the row's maximum and without it, so that values near zero
+ * keep their precision.  Bitwise the same from run to run.
+ * ws: 16-byte aligned.
+ */
+size_t pbd_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top_n);
+int pbd_token_logprobs(int32_t rows, int32_t vocab, int32_t dtype, const void* logits, int64_t row_stride,
+                       const int32_t* tokens, int32_t top_n, float* logprob, float* entropy,
+                       int32_t* top_ids, float* top_logprobs, int32_t* status,
+                       void* ws, size_t ws_bytes, pbd_stream_t stream);
+
+/*
+ * The context's own KV cache as pages of 16 positions: fills dtype, heads,
+ * page_size, n_pages, strides, k and v of the host struct *out and clears the
+ * rest; the caller adds table, table_width and what else it wants.  Positions
+ * 16 i .. 16 i + 15 of sequence slot b are page b * n_kv_heads * ceil(max_seq / 16) + i.
+ */
+int pbd_context_pages(const pbd_ctx* ctx, pbd_pages* out);
+
+/*
+ * One greedy token for each sequence over a paged cache: the model's pass over
+ * token[b] at position pos[b], its K/V appended as slot cache_len[b] of every
+ * layer, attention over cache_len[b] + 1 slots (weights accumulated where the
+ * cache has scores).  After the pass token[b] is the argmax over the vocabulary
+ * (ties: lowest id), pos[b] and cache_len[b] one more (device int32 [batch],
+ * in/out): the call repeats itself, also as a captured graph.  cache_len may be
+ * less than pos once slots were evicted.  Layer l's cache is l * layer_stride
+ * elements past pages->k and v, its score and slot_pos l * state_layer_stride
+ * past theirs; dtype, heads and head_dim are the context's.  flags:
+ * PBD_PASS_ADAPTER_ON or _OFF (default off).  logits: NULL or float [batch][vocab].
+ * max_len: host bound on cache_len + 1, in [1, table_width * page_size].  A
+ * sequence with pos outside [0, max_seq), cache_len outside [0, max_len), a token
+ * outside the vocabulary or a bad page raises PBD_STATUS_CAPACITY, _TOKEN or
+ * _PAGE in the context's status word (pbd_sync_status) and is skipped: its
+ * cache, token, pos and cache_len stay; its logits are undefined.
+ * The context's own workspace is used too; pages->status is not.  On the
+ * context's own cache (pbd_context_pages) an unevicted sequence may go on with
+ * the other passes, with seq_len = pos and anchor = token.
+ */
+size_t pbd_decode_paged_workspace_bytes(const pbd_ctx* ctx, const pbd_pages* pages, int32_t batch, int32_t max_len);
+int pbd_decode_paged(pbd_ctx* ctx, const pbd_pages* pages, int32_t batch, int32_t* token, int32_t* pos,
+                     int32_t* cache_len, int32_t max_len, uint32_t flags, float* logits,
+                     void* ws, size_t ws_bytes, pbd_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Implementation controls.  The calls below are not part of the step's

@@ -40,6 +40,7 @@ PBD_STATUS_CAPACITY = 1
 PBD_STATUS_TOKEN = 2
 PBD_STATUS_FORCED_N = 4
 PBD_STATUS_TIMEOUT = 8
+PBD_STATUS_PAGE = 16
 
 EXPORTED = (
     "pbd_packed_weight_bytes", "pbd_kv_bytes", "pbd_workspace_bytes", "pbd_init_weights",
@@ -47,6 +48,9 @@ EXPORTED = (
     "pbd_verify_block", "pbd_verify_block_noalloc", "pbd_draft_block_unanchored", "pbd_verify_block_unanchored", "pbd_accept_commit",
     "pbd_sync_status", "pbd_set_attn_keys_per_split", "pbd_set_attn_query_split", "pbd_set_operand_precision",
     "pbd_set_pass_mode", "pbd_set_wait_limit", "pbd_profile_enable", "pbd_profile_read", "pbd_profile_stage_times", "pbd_last_error", "pbd_destroy",
+    "pbd_paged_append", "pbd_paged_attention", "pbd_paged_attention_workspace_bytes", "pbd_paged_evict",
+    "pbd_paged_evict_workspace_bytes", "pbd_token_logprobs", "pbd_token_logprobs_workspace_bytes",
+    "pbd_context_pages", "pbd_decode_paged", "pbd_decode_paged_workspace_bytes",
 )
 
 
@@ -72,6 +76,18 @@ class PbdWeights(ctypes.Structure):
                 ("layers", ctypes.POINTER(PbdLayerWeights))]
 
 
+class PbdPages(ctypes.Structure):
+    """pbd_pages; made by make_pages or Engine.pbd_context_pages, which keep the tensors alive."""
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+        ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("layer_stride", ctypes.c_int64),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+        ("table_width", ctypes.c_int32), ("score", ctypes.c_void_p), ("slot_pos", ctypes.c_void_p),
+        ("slot_stride", ctypes.c_int64), ("state_layer_stride", ctypes.c_int64), ("status", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -86,6 +102,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                            "(run paper_2607_12422_amd.build.build())")
     lib = ctypes.CDLL(p)
     vp, i32, u32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_size_t
+    i64, f32 = ctypes.c_int64, ctypes.c_float
     cfgp = ctypes.POINTER(PbdConfig)
     sig = {
         "pbd_packed_weight_bytes": (sz, [cfgp]),
@@ -113,6 +130,16 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                             ctypes.POINTER(ctypes.c_int64)]),
         "pbd_profile_stage_times": (ctypes.c_int, [vp, ctypes.POINTER(ctypes.c_uint64), i32,
                                                     ctypes.POINTER(i32)]),
+        "pbd_paged_append": (ctypes.c_int, [vp, i32, i32, vp, vp, vp, i64, vp, vp, vp, vp, vp, f32, vp, i32, vp, vp, vp]),
+        "pbd_paged_attention_workspace_bytes": (sz, [vp, i32, i32]),
+        "pbd_paged_attention": (ctypes.c_int, [vp, i32, vp, i64, vp, i32, f32, vp, vp, vp, sz, vp]),
+        "pbd_paged_evict_workspace_bytes": (sz, [vp, i32, i32]),
+        "pbd_paged_evict": (ctypes.c_int, [vp, i32, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]),
+        "pbd_token_logprobs_workspace_bytes": (sz, [i32, i32, i32]),
+        "pbd_token_logprobs": (ctypes.c_int, [i32, i32, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "pbd_context_pages": (ctypes.c_int, [vp, vp]),
+        "pbd_decode_paged_workspace_bytes": (sz, [vp, vp, i32, i32]),
+        "pbd_decode_paged": (ctypes.c_int, [vp, vp, i32, vp, vp, vp, i32, u32, vp, vp, sz, vp]),
         "pbd_last_error": (ctypes.c_char_p, [vp]),
         "pbd_destroy": (None, [vp]),
     }
@@ -177,6 +204,207 @@ def pbd_last_error(ctx=None) -> str:
 def _check(rc: int, ctx=None):
     if rc != PBD_OK:
         raise PbdError(rc, pbd_last_error(ctx))
+
+
+# -- operators over a paged KV cache, and log probabilities ----------------------------
+# The tensors of a call lie on one device; the stream is that device's current
+# one unless another is given.  Shapes and types are checked here, because the
+# library sees pointers only; the values are the library's to check.
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise PbdError(PBD_ERR_INVALID_ARG, what)
+
+
+def _dtype_id(t, what: str) -> int:
+    import torch
+    _need(t.dtype in (torch.float32, torch.bfloat16), f"{what} must be float32 or bfloat16")
+    return PBD_DTYPE_BF16 if t.dtype == torch.bfloat16 else PBD_DTYPE_F32
+
+
+def _i32(t, n: int, what: str, device):
+    """Pointer of a contiguous int32 device tensor of n elements (None: NULL)."""
+    import torch
+    if t is None:
+        return None
+    _need(t.dtype == torch.int32 and t.numel() == n and t.is_contiguous() and t.device == device,
+          f"{what} must be a contiguous int32 tensor of {n} elements on {device}")
+    return t.data_ptr()
+
+
+def _f32(t, n: int, what: str, device):
+    import torch
+    if t is None:
+        return None
+    _need(t.dtype == torch.float32 and t.numel() == n and t.is_contiguous() and t.device == device,
+          f"{what} must be a contiguous float32 tensor of {n} elements on {device}")
+    return t.data_ptr()
+
+
+def _space(ws, device):
+    """(pointer, bytes) of a workspace tensor."""
+    _need(ws is not None and ws.is_contiguous() and ws.device == device, f"ws must be a contiguous tensor on {device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _call(device, stream, fn, *args):
+    """fn(*args, stream) with the device current."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    st = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+    if device.index is None or device.index == torch.cuda.current_device():
+        rc = fn(*args, st)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, st)
+    _check(rc, None)
+
+
+def make_pages(k, v, table, n_q_heads: int, head_dim: int, score=None, slot_pos=None, status=None) -> PbdPages:
+    """pbd_pages of a cache of one layer, k and v [n_pages][n_kv_heads][page_size * head_dim], or of several,
+    [layers][n_pages][...]; table int32 [batch][pages]; score float32 and slot_pos int32 [batch][n_kv_heads][slots]
+    (layers first where k has them).  Pages and heads may have any strides, a page of a head is contiguous."""
+    import torch
+    _need(k.dim() in (3, 4) and v.shape == k.shape and v.dtype == k.dtype and v.stride() == k.stride(),
+          "k and v must be alike, [n_pages][n_kv_heads][page_size * head_dim], layers first")
+    _need(k.stride(-1) == 1, "a page of a head must be contiguous")
+    _need(table.dim() == 2 and table.dtype == torch.int32 and table.is_contiguous(),
+          "table must be a contiguous int32 tensor [batch][pages]")
+    _need(head_dim > 0 and k.shape[-1] % head_dim == 0, "a page does not hold whole positions")
+    B, H = table.shape[0], k.shape[-2]
+    p = PbdPages(dtype=_dtype_id(k, "k"), n_q_heads=n_q_heads, n_kv_heads=H, head_dim=head_dim,
+                 page_size=k.shape[-1] // head_dim, n_pages=k.shape[-3], page_stride=k.stride(-3),
+                 head_stride=k.stride(-2), layer_stride=k.stride(0) if k.dim() == 4 else 0, k=k.data_ptr(),
+                 v=v.data_ptr(), table=table.data_ptr(), table_width=table.shape[1])
+    _attach(p, k.device, B, k.shape[0] if k.dim() == 4 else None, score, slot_pos, status)
+    for t, what in ((v, "v"), (table, "table")):
+        _need(t.device == k.device, f"{what} must be on {k.device}")
+    p.keep = (k, v, table, score, slot_pos, status)
+    p.device, p.rows = k.device, B
+    return p
+
+
+def _attach(p: PbdPages, device, B: int, layers, score, slot_pos, status):
+    import torch
+    H, slots = p.n_kv_heads, None
+    for t, dt, what in ((score, torch.float32, "score"), (slot_pos, torch.int32, "slot_pos")):
+        if t is None:
+            continue
+        slots = t.shape[-1] if slots is None else slots
+        want = (B, H, slots) if layers is None else (layers, B, H, slots)
+        _need(t.dtype == dt and tuple(t.shape) == want and t.is_contiguous() and t.device == device,
+              f"{what} must be a contiguous {dt} tensor {list(want)} on {device}")
+        setattr(p, what, t.data_ptr())
+    if slots is not None:
+        p.slot_stride = slots
+        p.state_layer_stride = B * H * slots if layers is not None else 0
+    if status is not None:
+        p.status = _i32(status, 1, "status", device)
+
+
+def layer_pages(pages: PbdPages, layer: int) -> PbdPages:
+    """One layer of a cache of several."""
+    esz = 2 if pages.dtype == PBD_DTYPE_BF16 else 4
+    p = PbdPages.from_buffer_copy(pages)
+    p.k = pages.k + layer * pages.layer_stride * esz
+    p.v = pages.v + layer * pages.layer_stride * esz
+    for name in ("score", "slot_pos"):
+        if getattr(pages, name):
+            setattr(p, name, getattr(pages, name) + layer * pages.state_layer_stride * 4)
+    p.keep, p.device, p.rows = pages.keep, pages.device, pages.rows
+    return p
+
+
+def pbd_paged_attention_workspace_bytes(pages: PbdPages, batch: int, max_len: int) -> int:
+    return load_library().pbd_paged_attention_workspace_bytes(ctypes.byref(pages), batch, max_len)
+
+
+def pbd_paged_attention(pages: PbdPages, q, lens, max_len: int, out, ws, lse=None, scale: Optional[float] = None,
+                        stream=None):
+    """q float32 [batch][n_q_heads][head_dim] (any stride from a sequence to the next), lens int32 [batch]; out
+    float32 like q, lse float32 [batch][n_q_heads].  scale: 1 / sqrt(head_dim) if None."""
+    import torch
+    dev = pages.device
+    B, HQ, D = lens.numel(), pages.n_q_heads, pages.head_dim
+    _need(q.dtype == torch.float32 and tuple(q.shape) == (B, HQ, D) and q.stride(2) == 1 and q.stride(1) == D and
+          q.device == dev, "q must be float32 [batch][n_q_heads][head_dim], the heads of a sequence contiguous")
+    _need(B <= pages.rows, "the table has fewer rows than lens")
+    w, wb = _space(ws, dev)
+    _call(dev, stream, load_library().pbd_paged_attention, ctypes.byref(pages), B, q.data_ptr(),
+          q.stride(0) if B > 1 else HQ * D, _i32(lens, B, "lens", dev), max_len,
+          D ** -0.5 if scale is None else scale, _f32(out, B * HQ * D, "out", dev), _f32(lse, B * HQ, "lse", dev), w, wb)
+
+
+def pbd_paged_append(pages: PbdPages, k, v, lens, pos, rope, q=None, q_out=None, n_new=None, q_norm=None, k_norm=None,
+                     eps: float = 1e-6, len_out=None, stream=None):
+    """k, v float32 [batch][rows][n_kv_heads * head_dim] and q [batch][rows][n_q_heads * head_dim], all with the same
+    stride from a row to the next (columns of one projection); lens, pos, n_new, len_out int32 [batch]; rope float32
+    [positions][head_dim / 2][2]; q_norm, k_norm [head_dim] in the cache's type; q_out float32 like q, contiguous."""
+    import torch
+    dev = pages.device
+    B, R = k.shape[0], k.shape[1]
+    H, HQ, D = pages.n_kv_heads, pages.n_q_heads, pages.head_dim
+    stride = next((t.stride(1) for t in (k, v, q) if t is not None and R > 1),
+                  next((t.stride(0) for t in (k, v, q) if t is not None and B > 1), max(HQ, H) * D))
+    stride = stride if R > 1 or B > 1 else -(-stride // 4) * 4
+    for t, heads, what in ((k, H, "k"), (v, H, "v"), (q, HQ, "q")):
+        _need(t is None or (t.dtype == torch.float32 and tuple(t.shape) == (B, R, heads * D) and t.device == dev and
+                            t.stride(2) == 1 and (R == 1 or t.stride(1) == stride) and
+                            (B == 1 or t.stride(0) == R * stride)),
+              f"{what} must be float32 [batch][rows][heads * head_dim] with the row stride of k")
+    _need(B <= pages.rows, "the table has fewer rows than k")
+    _need(rope.dtype == torch.float32 and rope.is_contiguous() and rope.device == dev and
+          tuple(rope.shape[1:]) == (D // 2, 2), "rope must be contiguous float32 [positions][head_dim / 2][2]")
+    for t, what in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        _need(t is None or (_dtype_id(t, what) == pages.dtype and t.numel() == D and t.is_contiguous() and
+                            t.device == dev), f"{what} must be a contiguous [head_dim] tensor of the cache's type")
+    _call(dev, stream, load_library().pbd_paged_append, ctypes.byref(pages), B, R, _ptr(q), k.data_ptr(), v.data_ptr(),
+          stride, _i32(lens, B, "lens", dev), _i32(n_new, B, "n_new", dev), _i32(pos, B, "pos", dev), _ptr(q_norm),
+          _ptr(k_norm), eps, rope.data_ptr(), rope.shape[0], _f32(q_out, B * R * HQ * D, "q_out", dev),
+          _i32(len_out, B, "len_out", dev))
+
+
+def pbd_paged_evict_workspace_bytes(pages: PbdPages, batch: int, max_len: int) -> int:
+    return load_library().pbd_paged_evict_workspace_bytes(ctypes.byref(pages), batch, max_len)
+
+
+def pbd_paged_evict(pages: PbdPages, lens, max_len: int, keep, new_lens, ws, pos=None, recent: int = 0, sink: int = 0,
+                    score_out=None, slot_pos_out=None, stream=None):
+    """lens, keep, pos, new_lens int32 [batch]; score_out, slot_pos_out like the cache's score and slot_pos, which
+    they are if None."""
+    dev = pages.device
+    B = lens.numel()
+    _need(B <= pages.rows, "the table has fewer rows than lens")
+    n = pages.rows * pages.n_kv_heads * pages.slot_stride
+    so = pages.score if score_out is None else _f32(score_out, n, "score_out", dev)
+    po = pages.slot_pos if slot_pos_out is None else _i32(slot_pos_out, n, "slot_pos_out", dev)
+    w, wb = _space(ws, dev)
+    _call(dev, stream, load_library().pbd_paged_evict, ctypes.byref(pages), B, _i32(lens, B, "lens", dev), max_len,
+          _i32(keep, B, "keep", dev), _i32(pos, B, "pos", dev), recent, sink, so, po,
+          _i32(new_lens, B, "new_lens", dev), w, wb)
+
+
+def pbd_token_logprobs_workspace_bytes(rows: int, vocab: int, top_n: int) -> int:
+    return load_library().pbd_token_logprobs_workspace_bytes(rows, vocab, top_n)
+
+
+def pbd_token_logprobs(logits, tokens, logprob, ws, entropy=None, top_ids=None, top_logprobs=None, status=None,
+                       stream=None):
+    """logits float32 or bfloat16 [..., vocab] (rows at one stride), tokens int32 [rows] (-1: padding) and logprob
+    float32 [rows], or both None; entropy float32 [rows]; top_ids int32 and top_logprobs float32 [rows, n]."""
+    dev = logits.device
+    V = logits.shape[-1]
+    x = logits if logits.dim() == 2 else logits.view(-1, V)
+    R = x.shape[0]
+    _need(x.stride(1) == 1 or V == 1, "the logits of a row must be contiguous")
+    n = 0 if top_ids is None else top_ids.shape[-1]
+    w, wb = _space(ws, dev)
+    _call(dev, stream, load_library().pbd_token_logprobs, R, V, _dtype_id(x, "logits"), x.data_ptr(),
+          x.stride(0) if R > 1 else V, _i32(tokens, R, "tokens", dev), n, _f32(logprob, R, "logprob", dev),
+          _f32(entropy, R, "entropy", dev), _i32(top_ids, R * n, "top_ids", dev),
+          _f32(top_logprobs, R * n, "top_logprobs", dev), _i32(status, 1, "status", dev), w, wb)
 
 
 class Engine:
@@ -284,6 +512,37 @@ class Engine:
         B = int(seq_len.shape[0]) if batch is None else batch
         rc = self.lib.pbd_accept_commit(self.ctx, B, _ptr(draft), _ptr(verify), _ptr(forced_n), _ptr(seq_len),
                                         _ptr(anchor), _ptr(n_accepted), _ptr(out_tokens), _stream(stream))
+        _check(rc, self.ctx)
+
+    def pbd_context_pages(self, table=None, score=None, slot_pos=None) -> PbdPages:
+        """The context's own cache as pages; table: every position of every sequence slot if None."""
+        import torch
+        p = PbdPages()
+        _check(self.lib.pbd_context_pages(self.ctx, ctypes.byref(p)), self.ctx)
+        if table is None:
+            nblk = -(-self.pcfg.max_seq // 16)
+            slots = torch.arange(self.pcfg.max_batch, dtype=torch.int32, device=self.device)[:, None]
+            table = slots * (p.n_kv_heads * nblk) + torch.arange(nblk, dtype=torch.int32, device=self.device)
+        _need(table.dim() == 2 and table.dtype == torch.int32 and table.is_contiguous() and
+              table.device.type == self.device.type, "table must be a contiguous int32 tensor [batch][pages]")
+        p.table, p.table_width = table.data_ptr(), table.shape[1]
+        _attach(p, table.device, table.shape[0], self.cfg.n_layers, score, slot_pos, None)
+        p.keep = (self.kv, table, score, slot_pos)
+        p.device, p.rows = table.device, table.shape[0]
+        return p
+
+    def pbd_decode_paged_workspace_bytes(self, pages: PbdPages, batch: int, max_len: int) -> int:
+        return self.lib.pbd_decode_paged_workspace_bytes(self.ctx, ctypes.byref(pages), batch, max_len)
+
+    def pbd_decode_paged(self, pages: PbdPages, token, pos, cache_len, max_len: int, ws, logits=None,
+                         flags: int = PBD_PASS_DEFAULT, stream=None):
+        B = int(token.shape[0])
+        dev = pages.device
+        _need(B <= pages.rows, "the table has fewer rows than token")
+        w, wb = _space(ws, dev)
+        rc = self.lib.pbd_decode_paged(self.ctx, ctypes.byref(pages), B, _i32(token, B, "token", dev),
+                                       _i32(pos, B, "pos", dev), _i32(cache_len, B, "cache_len", dev), int(max_len),
+                                       flags, _f32(logits, B * self.cfg.vocab, "logits", dev), w, wb, _stream(stream))
         _check(rc, self.ctx)
 
     def pbd_sync_status(self, stream=None) -> int:

@@ -11,6 +11,7 @@
 
 #include "pbd_fused.h"
 #include "pbd_kernels.h"
+#include "pbd_paged.h"
 
 using namespace pbd;
 
@@ -318,6 +319,19 @@ int hip_fail(pbd_ctx* c, hipError_t e, const char* what) {
     return fail(c, PBD_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+}  // namespace
+
+int pbd::op_fail(int code, const char* msg) noexcept {
+    try {
+        g_init_error = msg;
+    } catch (...) {
+        g_init_error.clear();
+    }
+    return code;
+}
+
+namespace {
+
 #define PBD_HIP(ctx, expr, what)                               \
     do {                                                       \
         hipError_t _e = (expr);                                \
@@ -372,6 +386,17 @@ struct PassReq {
     // non-null: the pass's workspace regions live here instead of in the
     // context's workspace (the status word stays there); one kernel per operator
     char* scratch;
+    // non-null: one token per sequence over a paged cache (seq_len: positions)
+    const struct PagedPass* paged;
+};
+
+// The paged cache of a decode pass and the parts of its workspace.
+struct PagedPass {
+    const pbd_pages* pages;
+    int max_len;
+    PagedAttnPlan plan;
+    DecodeStepArgs step;
+    char* ws;                  // attention workspace
 };
 
 int run_pass(pbd_ctx* c, const PassReq& q, hipStream_t st) {
@@ -380,7 +405,7 @@ int run_pass(pbd_ctx* c, const PassReq& q, hipStream_t st) {
     char* pk = c->packed;
     const int dt = y.dtype;
     const bool pre = q.mode == PASS_PREFILL;         // prefill chunk: K/V appended first, chunk-mode attention
-    const int W = pre ? y.Wp : (q.no_anchor ? y.D : y.W), B = q.B, M = B * W, MT = cdiv(M, 16);
+    const int W = q.paged ? 1 : pre ? y.Wp : (q.no_anchor ? y.D : y.W), B = q.B, M = B * W, MT = cdiv(M, 16);
     const int lead = (pre || q.no_anchor) ? 0 : 1;
     const int QT = cdiv(y.G * W, 16);              // query tiles per (KV head, sequence)
     int kps = c->kps;
@@ -444,7 +469,7 @@ int run_pass(pbd_ctx* c, const PassReq& q, hipStream_t st) {
     as.embed = pk + y.p_embed; as.gain = pk + y.lay[0].attn_norm; as.x = x;
     as.op_hi = hi(y.w_xa); as.op_lo = lo(y.w_xa); as.op_f16 = h16 ? 1 : 0; as.sq = sq_a;
     const bool fused = y.fused_shape && c->fused_dev && c->pass_mode == 0 && !pre && B == 1 &&
-                       !q.anchor_cached && !q.no_anchor && split && !q.scratch;
+                       !q.anchor_cached && !q.no_anchor && split && !q.scratch && !q.paged;
     if (q.scratch) {
         // the split-K arrival counters must start at zero; the scratch keeps
         // whatever the last call on this device left (a fill kernel, not a
@@ -457,6 +482,7 @@ int run_pass(pbd_ctx* c, const PassReq& q, hipStream_t st) {
         as.fused_layers = q.n_layers > 0 ? q.n_layers : y.L;
     }
     PBD_TIMED(c, st, PBD_KCLASS_OTHER, launch_assemble(dt, as, B, st), "assemble");
+    if (q.paged) PBD_TIMED(c, st, PBD_KCLASS_OTHER, launch_decode_begin(q.paged->step, B, st), "decode begin");
 
     auto base_gemm = [&](FGemmArgs& g, size_t w_off, int tiles, int kb, const size_t* xop) {
         g = FGemmArgs{};
@@ -535,6 +561,41 @@ int run_pass(pbd_ctx* c, const PassReq& q, hipStream_t st) {
         b.out = g.out; b.ldo = g.ldo;                // STORE (q/k/v); the other projections use epilogues
         b.op_f16 = h16 ? 1 : 0;
         return b;
+    };
+    // the paged pass's cache update and attention of layer l, from the q/k/v
+    // projections to the O projection's operand
+    auto paged_layer = [&](int l) -> int {
+        const PagedPass& pp = *q.paged;
+        const Layout::LayerOff& lo_ = y.lay[l];
+        pbd_pages pg = *pp.pages;
+        const size_t cache = (size_t)l * (size_t)pg.layer_stride * y.esz;
+        pg.k = (char*)pg.k + cache;
+        pg.v = (char*)pg.v + cache;
+        if (pg.score) pg.score += (size_t)l * pg.state_layer_stride;
+        if (pg.slot_pos) pg.slot_pos += (size_t)l * pg.state_layer_stride;
+        pg.status = status;
+        const float* qkv = (const float*)(ws + y.w_qkv);
+        PagedAppendArgs pa{};
+        pa.pg = page_view(pg);
+        pa.n_q = y.NQ; pa.n_kv = y.NKV; pa.max_new = 1; pa.rope_len = y.max_seq;
+        pa.q = qkv; pa.k = qkv + y.NQ * y.HD; pa.v = qkv + (y.NQ + y.NKV) * y.HD; pa.row_stride = y.nqkv;
+        pa.lens = pp.step.len_old; pa.n_new = pp.step.n_new; pa.pos = pos0;
+        pa.q_norm = c->cfg.qk_norm ? pk + lo_.q_norm : nullptr;
+        pa.k_norm = c->cfg.qk_norm ? pk + lo_.k_norm : nullptr;
+        pa.eps = c->cfg.rms_eps; pa.rope = (const float2*)(pk + y.p_rope);
+        pa.q_out = (float*)(ws + y.w_attn_o);
+        PBD_TIMED(c, st, PBD_KCLASS_OTHER, launch_paged_append(dt, y.HD, pa, B, st), "append");
+        PagedAttnArgs at{};
+        at.pg = pa.pg;
+        at.n_q = y.NQ; at.n_kv = y.NKV; at.max_len = pp.max_len; at.q = pa.q_out; at.q_stride = (size_t)y.NQ * y.HD;
+        at.lens = pp.step.len_now; at.scale_log2 = (float)(1.0 / sqrt((double)y.HD) * 1.4426950408889634);
+        at.plan = pp.plan;
+        at.part_o = (float*)pp.ws; at.part_ml = (float*)(pp.ws + pp.plan.off_ml);
+        at.raw = pg.score ? (float*)(pp.ws + pp.plan.off_raw) : nullptr;
+        at.MT = MT; at.op_f16 = h16 ? 1 : 0; at.op_hi = hi(y.w_xo); at.op_lo = lo(y.w_xo);
+        PBD_TIMED(c, st, PBD_KCLASS_ATTN, launch_paged_attn_splits(dt, y.HD, at, B, st), "attention");
+        PBD_TIMED(c, st, PBD_KCLASS_COMBINE, launch_paged_attn_join(dt, y.HD, at, B, st), "attention join");
+        return PBD_OK;
     };
     // with the adapter, the large-M projection is two launches (timed
     // separately): the shrink of the projection's nsrc LoRA A matrices,
@@ -632,65 +693,70 @@ int run_pass(pbd_ctx* c, const PassReq& q, hipStream_t st) {
         else if (big) PBD_BIG(g, 3, EPI_STORE, "qkv gemm");
         else PBD_TIMED(c, st, PBD_KCLASS_GEMM, launch_fgemm(dt, g, EPI_STORE, st), "qkv gemm");
 
-        AttnArgs at{};
-        at.layer = l; at.max_batch = y.Bmax; at.n_q = y.NQ; at.n_kv = y.NKV; at.nblk = y.nblk; at.W = W; at.G = y.G;
-        at.nqkv = y.nqkv; at.kps = kps; at.s_launch = s_launch; at.n_qgrp = cdiv(QT, QTw);
-        at.full_from = q.causal ? W : (q.anchor_cached ? 1 : 0);
-        at.kv_rows = pre ? 0 : q.write_kv ? W : (q.anchor_cached ? 1 : 0);
-        at.chunk = pre ? 1 : 0;
-        at.qk_norm = c->cfg.qk_norm ? 1 : 0;
-        at.eps = c->cfg.rms_eps; at.scale_log2 = (float)(1.0 / sqrt((double)y.HD) * 1.4426950408889634);
-        at.smem_main = attn_smem_main(dt, y.HD, QTw);
-        at.pos0 = pos0; at.nrows = nrows; at.qkv = (const float*)(ws + y.w_qkv);
-        at.q_norm = pk + lo_.q_norm; at.k_norm = pk + lo_.k_norm; at.rope = (const float2*)(pk + y.p_rope);
-        at.kcache = c->kv; at.vcache = c->kv + y.kv_half;
-        at.part_o = (float*)(ws + y.w_attn_o); at.part_ml = (float*)(ws + y.w_attn_ml);
-        at.MT = MT; at.op_hi = hi(y.w_xo); at.op_lo = lo(y.w_xo);
-        // spare CUs during the attention warm the O, gate/up and down weights of
-        // this layer and the q/k/v weights of the next one, then the next
-        // layer's K/V of the batch's sequences when that slab is small
-        {
-            const size_t beg = lo_.o, end = l + 1 < L ? y.lay[l + 1].o : lo_.attn_norm;
-            const int slots = B * y.NKV * at.n_qgrp;
-            const int free_wg = 256 - s_launch * slots;
-            // (at more than two m-tiles only beside eight splits and more: there the
-            // GEMMs hide their weights' latency themselves, and a short attention
-            // ends after the warming; batch 4 of 50 .. 100 keys: 781 us over 14
-            // layers without, 843 with; batch 2 of 8192: 526 and 515; one
-            // sequence of 60: 909 and 847)
-            at.pf_x = slots > 0 && free_wg > slots && (!att_rows || MT <= 2 || s_launch > 8) ? free_wg / slots : 0;
-            size_t cap = (size_t)at.pf_x * slots * (att_rows ? (QT + 1) * 64 : 256) * 16 * 128;
-            if (dt == PBD_DTYPE_BF16) cap = std::min(cap, WARM_BYTES);
-            at.pf[0] = pk + beg;
-            at.pf_bytes[0] = std::min(end - beg, cap);
-            cap -= at.pf_bytes[0];
-            const size_t kv_seq = (size_t)y.NKV * y.nblk * 16 * y.HD * y.esz;   // one sequence's K (or V) of a layer
-            const size_t kv_b = (size_t)B * kv_seq;
-            if (l + 1 < L && kv_b <= ((size_t)16 << 20) && 2 * kv_b <= cap) {
-                const size_t off = (size_t)(l + 1) * y.Bmax * kv_seq;
-                at.pf[1] = c->kv + off;
-                at.pf[2] = c->kv + y.kv_half + off;
-                at.pf_bytes[1] = at.pf_bytes[2] = kv_b;
+        if (q.paged) {
+            const int rc = paged_layer(l);
+            if (rc) return rc;
+        } else {
+            AttnArgs at{};
+            at.layer = l; at.max_batch = y.Bmax; at.n_q = y.NQ; at.n_kv = y.NKV; at.nblk = y.nblk; at.W = W; at.G = y.G;
+            at.nqkv = y.nqkv; at.kps = kps; at.s_launch = s_launch; at.n_qgrp = cdiv(QT, QTw);
+            at.full_from = q.causal ? W : (q.anchor_cached ? 1 : 0);
+            at.kv_rows = pre ? 0 : q.write_kv ? W : (q.anchor_cached ? 1 : 0);
+            at.chunk = pre ? 1 : 0;
+            at.qk_norm = c->cfg.qk_norm ? 1 : 0;
+            at.eps = c->cfg.rms_eps; at.scale_log2 = (float)(1.0 / sqrt((double)y.HD) * 1.4426950408889634);
+            at.smem_main = attn_smem_main(dt, y.HD, QTw);
+            at.pos0 = pos0; at.nrows = nrows; at.qkv = (const float*)(ws + y.w_qkv);
+            at.q_norm = pk + lo_.q_norm; at.k_norm = pk + lo_.k_norm; at.rope = (const float2*)(pk + y.p_rope);
+            at.kcache = c->kv; at.vcache = c->kv + y.kv_half;
+            at.part_o = (float*)(ws + y.w_attn_o); at.part_ml = (float*)(ws + y.w_attn_ml);
+            at.MT = MT; at.op_hi = hi(y.w_xo); at.op_lo = lo(y.w_xo);
+            // spare CUs during the attention warm the O, gate/up and down weights of
+            // this layer and the q/k/v weights of the next one, then the next
+            // layer's K/V of the batch's sequences when that slab is small
+            {
+                const size_t beg = lo_.o, end = l + 1 < L ? y.lay[l + 1].o : lo_.attn_norm;
+                const int slots = B * y.NKV * at.n_qgrp;
+                const int free_wg = 256 - s_launch * slots;
+                // (at more than two m-tiles only beside eight splits and more: there the
+                // GEMMs hide their weights' latency themselves, and a short attention
+                // ends after the warming; batch 4 of 50 .. 100 keys: 781 us over 14
+                // layers without, 843 with; batch 2 of 8192: 526 and 515; one
+                // sequence of 60: 909 and 847)
+                at.pf_x = slots > 0 && free_wg > slots && (!att_rows || MT <= 2 || s_launch > 8) ? free_wg / slots : 0;
+                size_t cap = (size_t)at.pf_x * slots * (att_rows ? (QT + 1) * 64 : 256) * 16 * 128;
+                if (dt == PBD_DTYPE_BF16) cap = std::min(cap, WARM_BYTES);
+                at.pf[0] = pk + beg;
+                at.pf_bytes[0] = std::min(end - beg, cap);
+                cap -= at.pf_bytes[0];
+                const size_t kv_seq = (size_t)y.NKV * y.nblk * 16 * y.HD * y.esz;   // one sequence's K (or V) of a layer
+                const size_t kv_b = (size_t)B * kv_seq;
+                if (l + 1 < L && kv_b <= ((size_t)16 << 20) && 2 * kv_b <= cap) {
+                    const size_t off = (size_t)(l + 1) * y.Bmax * kv_seq;
+                    at.pf[1] = c->kv + off;
+                    at.pf[2] = c->kv + y.kv_half + off;
+                    at.pf_bytes[1] = at.pf_bytes[2] = kv_b;
+                }
             }
-        }
-        if (pre) {
-            KVWriteArgs kw{};
-            kw.layer = l; kw.max_batch = y.Bmax; kw.n_q = y.NQ; kw.n_kv = y.NKV; kw.nblk = y.nblk; kw.W = W;
-            kw.nqkv = y.nqkv; kw.qk_norm = c->cfg.qk_norm ? 1 : 0; kw.eps = c->cfg.rms_eps;
-            kw.pos0 = pos0; kw.nrows = nrows; kw.qkv = at.qkv; kw.k_norm = at.k_norm; kw.rope = at.rope;
-            kw.kcache = at.kcache; kw.vcache = at.vcache;
-            PBD_TIMED(c, st, PBD_KCLASS_OTHER, launch_kvwrite(dt, y.HD, kw, B, st), "prefill K/V");
-        }
-        if (att_rows) PBD_TIMED(c, st, PBD_KCLASS_ATTN, launch_attn_rows(at, QT, B, st), "attention");
-        else if (att_chunk) PBD_TIMED(c, st, PBD_KCLASS_ATTN, launch_attn_chunk(at, B, st), "attention");
-        else PBD_TIMED(c, st, PBD_KCLASS_ATTN, launch_attn(dt, y.HD, QTw, at, B, st), "attention");
+            if (pre) {
+                KVWriteArgs kw{};
+                kw.layer = l; kw.max_batch = y.Bmax; kw.n_q = y.NQ; kw.n_kv = y.NKV; kw.nblk = y.nblk; kw.W = W;
+                kw.nqkv = y.nqkv; kw.qk_norm = c->cfg.qk_norm ? 1 : 0; kw.eps = c->cfg.rms_eps;
+                kw.pos0 = pos0; kw.nrows = nrows; kw.qkv = at.qkv; kw.k_norm = at.k_norm; kw.rope = at.rope;
+                kw.kcache = at.kcache; kw.vcache = at.vcache;
+                PBD_TIMED(c, st, PBD_KCLASS_OTHER, launch_kvwrite(dt, y.HD, kw, B, st), "prefill K/V");
+            }
+            if (att_rows) PBD_TIMED(c, st, PBD_KCLASS_ATTN, launch_attn_rows(at, QT, B, st), "attention");
+            else if (att_chunk) PBD_TIMED(c, st, PBD_KCLASS_ATTN, launch_attn_chunk(at, B, st), "attention");
+            else PBD_TIMED(c, st, PBD_KCLASS_ATTN, launch_attn(dt, y.HD, QTw, at, B, st), "attention");
 
-        if (!att_chunk) {
-            CombineArgs cb{};
-            cb.W = W; cb.n_q = y.NQ; cb.head_dim = y.HD; cb.kps = kps; cb.s_launch = s_launch; cb.MT = MT;
-            cb.pos0 = pos0; cb.part_o = at.part_o; cb.part_ml = at.part_ml;
-            cb.op_hi = hi(y.w_xo); cb.op_lo = lo(y.w_xo); cb.op_f16 = h16 ? 1 : 0;
-            PBD_TIMED(c, st, PBD_KCLASS_COMBINE, launch_combine(dt, cb, M, st), "attention combine");
+            if (!att_chunk) {
+                CombineArgs cb{};
+                cb.W = W; cb.n_q = y.NQ; cb.head_dim = y.HD; cb.kps = kps; cb.s_launch = s_launch; cb.MT = MT;
+                cb.pos0 = pos0; cb.part_o = at.part_o; cb.part_ml = at.part_ml;
+                cb.op_hi = hi(y.w_xo); cb.op_lo = lo(y.w_xo); cb.op_f16 = h16 ? 1 : 0;
+                PBD_TIMED(c, st, PBD_KCLASS_COMBINE, launch_combine(dt, cb, M, st), "attention combine");
+            }
         }
 
         // O projection + residual; writes the MLP RMSNorm operand
@@ -798,6 +864,7 @@ int run_pass(pbd_ctx* c, const PassReq& q, hipStream_t st) {
     am.lead = lead; am.out0 = q.out0; am.out0_stride = y.D + 1;
     am.out_stride = q.no_anchor ? y.D + 1 : W; am.out_off = q.no_anchor ? 1 : 0;
     PBD_TIMED(c, st, PBD_KCLASS_OTHER, launch_argmax(am, st), "argmax");
+    if (q.paged) PBD_TIMED(c, st, PBD_KCLASS_OTHER, launch_decode_end(q.paged->step, B, st), "decode end");
     return PBD_OK;
 }
 #undef PBD_BIG
@@ -1216,6 +1283,77 @@ int pbd_accept_commit(pbd_ctx* c, int32_t batch, const int32_t* draft, const int
     a.n_acc = n_accepted; a.out = out_tokens; a.status = (int*)(c->ws + c->ly.w_status);
     PBD_HIP(c, launch_accept(a, (hipStream_t)stream), "accept");
     return PBD_OK;
+}
+
+int pbd_context_pages(const pbd_ctx* c, pbd_pages* out) {
+    int rc = check_ctx(c);
+    if (rc) return rc;
+    if (!out) return fail(const_cast<pbd_ctx*>(c), PBD_ERR_INVALID_ARG, "out is NULL");
+    const Layout& y = c->ly;
+    pbd_pages p{};
+    p.dtype = y.dtype; p.n_q_heads = y.NQ; p.n_kv_heads = y.NKV; p.head_dim = y.HD;
+    p.page_size = 16;
+    p.n_pages = ((y.Bmax - 1) * y.NKV + 1) * y.nblk;
+    p.page_stride = 16ll * y.HD;
+    p.head_stride = (long long)y.nblk * 16 * y.HD;
+    p.layer_stride = (long long)y.Bmax * y.NKV * y.nblk * 16 * y.HD;
+    p.k = c->kv;
+    p.v = c->kv + y.kv_half;
+    *out = p;
+    return PBD_OK;
+}
+
+size_t pbd_decode_paged_workspace_bytes(const pbd_ctx* c, const pbd_pages* pages, int32_t batch, int32_t max_len) {
+    char msg[192];
+    if (!c || batch < 1 || batch > c->cfg.max_batch || max_len < 1 || check_pages(pages, batch, max_len, msg)) return 0;
+    const PagedAttnPlan plan = paged_attn_plan(pages->dtype, pages->n_q_heads, pages->n_kv_heads, pages->head_dim,
+                                               batch, max_len, pages->score != nullptr);
+    return align_up(plan.bytes, 256) + align_up((size_t)batch * 3 * sizeof(int), 256);
+}
+
+int pbd_decode_paged(pbd_ctx* c, const pbd_pages* pages, int32_t batch, int32_t* token, int32_t* pos,
+                     int32_t* cache_len, int32_t max_len, uint32_t flags, float* logits, void* ws, size_t ws_bytes,
+                     pbd_stream_t stream) {
+    int rc = check_ctx(c);
+    if (rc) return rc;
+    if ((rc = check_batch(c, batch))) return rc;
+    char msg[192];
+    if ((rc = check_pages(pages, batch, max_len, msg))) return fail(c, rc, msg);
+    const Layout& y = c->ly;
+    if (!token || !pos || !cache_len || !ws) return fail(c, PBD_ERR_INVALID_ARG, "NULL pointer argument");
+    if (token == pos || token == cache_len || pos == cache_len)
+        return fail(c, PBD_ERR_INVALID_ARG, "token, pos and cache_len must be distinct");
+    if (max_len < 1) return fail(c, PBD_ERR_INVALID_ARG, "max_len must be >= 1");
+    if (pages->dtype != y.dtype || pages->n_q_heads != y.NQ || pages->n_kv_heads != y.NKV || pages->head_dim != y.HD)
+        return fail(c, PBD_ERR_SHAPE, "the cache's dtype, heads or head_dim are not the context's");
+    if (pages->layer_stride < 0 || pages->layer_stride % (16ll * y.HD) || (y.L > 1 && pages->layer_stride == 0))
+        return fail(c, PBD_ERR_INVALID_ARG, "layer_stride must be a positive multiple of 16 head_dim");
+    if ((pages->score || pages->slot_pos) && (pages->state_layer_stride < 0 || (y.L > 1 && pages->state_layer_stride == 0)))
+        return fail(c, PBD_ERR_INVALID_ARG, "state_layer_stride must be positive");
+    if ((size_t)ws & 15) return fail(c, PBD_ERR_INVALID_ARG, "ws must be 16-byte aligned");
+    if (flags & (PBD_PASS_MASK_BLOCK | PBD_PASS_MASK_CAUSAL))
+        return fail(c, PBD_ERR_INVALID_ARG, "a single token takes no mask flag");
+    bool adapter, causal;
+    if ((rc = resolve_flags(c, flags, false, true, adapter, causal))) return rc;
+    if (ws_bytes < pbd_decode_paged_workspace_bytes(c, pages, batch, max_len))
+        return fail(c, PBD_ERR_CAPACITY, "workspace smaller than pbd_decode_paged_workspace_bytes");
+    PagedPass pp{};
+    pp.pages = pages;
+    pp.max_len = max_len;
+    pp.plan = paged_attn_plan(y.dtype, y.NQ, y.NKV, y.HD, batch, max_len, pages->score != nullptr);
+    pp.ws = (char*)ws;
+    int* state = (int*)((char*)ws + align_up(pp.plan.bytes, 256));
+    pp.step.pg = page_view(*pages);
+    pp.step.pg.status = (int*)(c->ws + y.w_status);
+    pp.step.vocab = y.V; pp.step.max_seq = y.max_seq; pp.step.max_len = max_len;
+    pp.step.token = token; pp.step.pos = pos; pp.step.cache_len = cache_len;
+    pp.step.nrows = (int*)(c->ws + y.w_nrows);
+    pp.step.n_new = state; pp.step.len_old = state + batch; pp.step.len_now = state + 2 * batch;
+    PassReq q{};
+    q.mode = PASS_VERIFY; q.B = batch; q.seq_len = pos; q.anchor = token;
+    q.adapter = adapter; q.causal = true; q.write_kv = true; q.out_tokens = token; q.logits = logits;
+    q.paged = &pp;
+    return run_pass(c, q, (hipStream_t)stream);
 }
 
 int pbd_sync_status(pbd_ctx* c, pbd_stream_t stream, int32_t* status) {

@@ -1,0 +1,364 @@
+// Log probabilities of given tokens, entropy and top alternatives of rows of
+// logits: one pass over the logits.
+//
+// A row (or, where there are few rows, a part of one) is a work-group's.  Each
+// wave keeps a running maximum m, S' = sum exp(x - m) without one instance of
+// the maximum, and T = sum exp(x - m) (x - m); then
+//   log prob(t) = (x_t - m) - log(1 + S'),   entropy = log(1 + S') - T / (1 + S'),
+// sums of terms of one sign, so that a row whose maximum has nearly all of the
+// mass loses nothing to cancellation.
+//
+// The top n cost the pass nothing but a store: per thread and tile (32 elements)
+// the maximum is kept in LDS.  At most n - 1 elements exceed the n-th largest,
+// so the n-th largest of the 256 threads' maxima is a lower bound of it, and the
+// groups that reach the bound (about n of some thousands) are read again, the
+// elements that reach it ranked by (value, lower id).  Where too many reach it
+// (masses of equal logits) the row is scanned n times instead.
+#include "pbd_device.h"
+#include "pbd_launch.h"
+#include "pbd_paged.h"
+
+#include <algorithm>
+
+namespace pbd {
+namespace {
+
+constexpr int LP_T = 256;
+constexpr int GROUP = 32;                       // elements per thread and tile
+constexpr int TILE = LP_T * GROUP;
+constexpr int TILES_MAX = 20;                   // tiles of a part: their group maxima fit 20 KiB of LDS
+constexpr int GROUPS_CAP = 256, CAND_CAP = 512;
+constexpr int TOP_MAX = 32;
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LEAST = -1e30f;                 // bounds x - m where it is a factor: a masked token adds 0, not 0 * -inf
+
+typedef unsigned long long u64;
+
+struct Stat {
+    float m, s, t;
+};
+
+// exp(x), x <= 0 or NaN
+__device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
+__device__ __forceinline__ Stat join(Stat a, Stat b) {
+    if (b.m > a.m) {
+        const Stat c = a;
+        a = b;
+        b = c;
+    }
+    if (b.m == -INFINITY) {                      // nothing there, or NaN only
+        a.s += b.s;
+        a.t += b.t;
+        return a;
+    }
+    const float d = fmaxf(b.m - a.m, LEAST), f = exp_neg(d);
+    a.s += f * (b.s + 1.f);
+    a.t += f * (b.t + d * (b.s + 1.f));
+    return a;
+}
+
+__device__ __forceinline__ unsigned value_key(float x) {
+    const unsigned u = __float_as_uint(x + 0.f);
+    return u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float key_value(unsigned k) {
+    return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k);
+}
+// larger: the larger value, then the lower id; 0: none
+__device__ __forceinline__ u64 token_key(float x, int id) { return (u64)value_key(x) << 32 | (unsigned)~id; }
+
+template <typename T> struct Vec {
+    static constexpr int N = 16 / sizeof(T);
+};
+
+// The row as whole 16-byte vectors: vector i holds ids i N - off .. i N - off + N - 1.
+template <typename T>
+struct Row {
+    static constexpr int N = Vec<T>::N, PER = GROUP / N;
+    const T* p;                                  // the row's first element
+    int off, vocab;
+    __device__ Row(const void* logits, long long stride, int r, int v) : vocab(v) {
+        p = (const T*)logits + (long long)r * stride;
+        off = (int)(((size_t)p & 15) / sizeof(T));
+    }
+    // values of vector i; -inf outside the row, of which nothing is read
+    __device__ __forceinline__ void load(int i, float* x) const {
+        const int id = i * N - off;
+        if (id >= 0 && id + N <= vocab) {
+            const uint4 raw = *(const uint4*)(p + id);
+            T e[N];
+            __builtin_memcpy(e, &raw, 16);
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = to_f32(e[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = id + k >= 0 && id + k < vocab ? to_f32(p[id + k]) : -INFINITY;
+        }
+    }
+};
+
+__device__ __forceinline__ u64 wave_max64(u64 v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const u64 w = __shfl_xor(v, o, 64);
+        v = w > v ? w : v;
+    }
+    return v;
+}
+
+// Whether row r takes part (the same answer in every thread); first: reports.
+__device__ __forceinline__ bool row_ok(const LogprobArgs& a, int r, bool first) {
+    if (!a.tokens) return true;
+    const int t = a.tokens[r];
+    if (t >= 0 && t < a.vocab) return true;
+    if (t != -1 && first && threadIdx.x == 0 && a.status) atomicOr(a.status, PBD_STATUS_TOKEN);
+    return false;
+}
+
+template <typename T>
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int r, Stat st, const u64* top) {
+    const float s = st.m == INFINITY ? __builtin_nanf("") : st.s, lz = log1pf(s);
+    if (threadIdx.x == 0) {
+        if (a.logprob) {
+            const float x = to_f32(((const T*)a.logits)[(long long)r * a.row_stride + a.tokens[r]]);
+            a.logprob[r] = st.m == -INFINITY ? -INFINITY + s : (x - st.m) - lz;
+        }
+        if (a.entropy) a.entropy[r] = lz - st.t / (1.f + s);
+    }
+    for (int i = threadIdx.x; i < a.top_n; i += LP_T) {
+        const u64 k = top[i];
+        const bool none = k == 0;
+        a.top_ids[(size_t)r * a.top_n + i] = none ? -1 : (int)~(unsigned)k;
+        a.top_logprobs[(size_t)r * a.top_n + i] = none ? -INFINITY : (key_value((unsigned)(k >> 32)) - st.m) - lz;
+    }
+}
+
+struct Part {
+    Stat* stat;                                  // [rows][parts]
+    u64* top;                                    // [rows][parts][top_n]
+    int parts, tiles, per;                       // parts of a row, its tiles, tiles of a part
+};
+
+template <typename T>
+__global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
+    constexpr int N = Row<T>::N, PER = Row<T>::PER;
+    __shared__ float s_group[TILES_MAX * LP_T];
+    __shared__ u64 s_cand[CAND_CAP];
+    __shared__ int s_list[GROUPS_CAP];
+    __shared__ u64 s_top[TOP_MAX];
+    __shared__ Stat s_stat[4];
+    __shared__ u64 s_red[4];
+    __shared__ float s_max[LP_T];
+    __shared__ int s_groups, s_cands;
+    __shared__ float s_bound;
+    const int part = blockIdx.x % pt.parts, r = blockIdx.x / pt.parts, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    if (!row_ok(a, r, part == 0)) return;
+    const Row<T> row(a.logits, a.row_stride, r, a.vocab);
+    const int t0 = part * pt.per, t1 = min(pt.tiles, t0 + pt.per);
+    float m = -INFINITY, s = 0.f, t = 0.f, mine = -INFINITY;
+    for (int tile = t0; tile < t1; ++tile) {
+        float x[GROUP];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) row.load((tile * PER + i) * LP_T + tid, x + i * N);
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i) top = fmaxf(top, x[i]);
+        s_group[(tile - t0) * LP_T + tid] = top;
+        mine = fmaxf(mine, top);
+        top = wave_max(top);
+        if (top > m) {
+            if (m > -INFINITY) {
+                // lane 0 has the instance of the old maximum that the sum leaves out
+                const float d = fmaxf(m - top, LEAST), f = exp_neg(d), all = lane == 0 ? s + 1.f : s;
+                t = f * (t + d * all);
+                s = f * all;
+            }
+            m = top;
+            int at_max = 0;
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) {
+                const float d = x[i] - m, e = exp_neg(d);
+                const bool is = x[i] == m;
+                at_max += is;
+                s += is ? 0.f : e;
+                t += e * fmaxf(d, LEAST);
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) at_max += __shfl_xor(at_max, o, 64);
+            if (lane == 0) s += (float)(at_max - 1);
+        } else {
+            const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) {
+                const float d = x[i] - ref, e = exp_neg(d);
+                s += e;
+                t += e * fmaxf(d, LEAST);
+            }
+        }
+    }
+    s = wave_sum(s);
+    t = wave_sum(t);
+    if (lane == 0) s_stat[wave] = Stat{m, s, t};
+    s_max[tid] = mine;
+    if (tid == 0) s_groups = s_cands = 0;
+    if (tid < TOP_MAX) s_top[tid] = 0;
+    __syncthreads();
+    Stat st = s_stat[0];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) st = join(st, s_stat[w]);
+    const int n = a.top_n;
+    if (n > 0) {
+        if (wave == 0) {
+            // the n-th largest of the threads' maxima, bit by bit from the top
+            unsigned k[4], bound = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[i] = value_key(s_max[lane + 64 * i]);
+            for (int bit = 31; bit >= 0; --bit) {
+                const unsigned c = bound | 1u << bit;
+                int cnt = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) cnt += __popcll(__ballot(k[i] >= c));
+                if (cnt >= n) bound = c;
+            }
+            // (fewer than n threads with anything unmasked: everything unmasked)
+            if (lane == 0) s_bound = key_value(max(bound, value_key(-INFINITY) + 1u));
+        }
+        __syncthreads();
+        const float bound = s_bound;
+        for (int g = tid; g < (t1 - t0) * LP_T; g += LP_T)
+            if (s_group[g] >= bound) {
+                const int i = atomicAdd(&s_groups, 1);
+                if (i < GROUPS_CAP) s_list[i] = g;
+            }
+        __syncthreads();
+        const int groups = s_groups;
+        if (groups <= GROUPS_CAP) {
+            for (int q = tid; q < groups * PER; q += LP_T) {
+                const int g = s_list[q / PER];
+                const int vec = ((t0 + g / LP_T) * PER + q % PER) * LP_T + g % LP_T;
+                float x[N];
+                row.load(vec, x);
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    if (x[k] >= bound) {
+                        const int i = atomicAdd(&s_cands, 1);
+                        if (i < CAND_CAP) s_cand[i] = token_key(x[k], vec * N - row.off + k);
+                    }
+            }
+        }
+        __syncthreads();
+        const int cands = s_cands;
+        if (groups <= GROUPS_CAP && cands <= CAND_CAP) {
+            for (int i = tid; i < cands; i += LP_T) {
+                const u64 k = s_cand[i];
+                int rank = 0;
+                for (int j = 0; j < cands; ++j) rank += s_cand[j] > k;
+                if (rank < n) s_top[rank] = k;
+            }
+            __syncthreads();
+        } else {
+            u64 prev = ~0ull;
+            for (int i = 0; i < n && prev != 0; ++i) {
+                u64 best = 0;
+                for (int tile = t0; tile < t1; ++tile)
+                    if (s_group[(tile - t0) * LP_T + tid] >= bound)
+                        for (int v = 0; v < PER; ++v) {
+                            const int vec = (tile * PER + v) * LP_T + tid;
+                            float x[N];
+                            row.load(vec, x);
+#pragma unroll
+                            for (int k = 0; k < N; ++k)
+                                if (x[k] >= bound) {
+                                    const u64 key = token_key(x[k], vec * N - row.off + k);
+                                    if (key < prev && key > best) best = key;
+                                }
+                        }
+                best = wave_max64(best);
+                __syncthreads();
+                if (lane == 0) s_red[wave] = best;
+                __syncthreads();
+                best = s_red[0];
+#pragma unroll
+                for (int w = 1; w < 4; ++w) best = s_red[w] > best ? s_red[w] : best;
+                if (tid == 0) s_top[i] = best;
+                prev = best;
+            }
+            __syncthreads();
+        }
+    }
+    if (pt.parts == 1) {
+        write_row<T>(a, r, st, s_top);
+        return;
+    }
+    const size_t at = (size_t)r * pt.parts + part;
+    if (tid == 0) pt.stat[at] = st;
+    for (int i = tid; i < n; i += LP_T) pt.top[at * n + i] = s_top[i];
+}
+
+// Joins the parts of a row, in order; the rank of an alternative is the sum over
+// the parts of how many of theirs are above it, each found by bisection.
+template <typename T>
+__global__ __launch_bounds__(LP_T) void k_logprobs_join(LogprobArgs a, Part pt) {
+    __shared__ u64 s_top[TOP_MAX];
+    const int r = blockIdx.x;
+    if (!row_ok(a, r, false)) return;
+    const Stat* stat = pt.stat + (size_t)r * pt.parts;
+    Stat st = stat[0];
+    for (int p = 1; p < pt.parts; ++p) st = join(st, stat[p]);
+    if (threadIdx.x < TOP_MAX) s_top[threadIdx.x] = 0;
+    __syncthreads();
+    const u64* top = pt.top + (size_t)r * pt.parts * a.top_n;
+    const int n = a.top_n;
+    for (int i = threadIdx.x; i < pt.parts * n; i += LP_T) {
+        const u64 k = top[i];
+        if (k == 0) continue;
+        int rank = 0;
+        for (int p = 0; p < pt.parts && rank < n; ++p) {
+            int lo = 0, hi = n;                       // entries above k: top[p n + lo - 1] > k >= top[p n + hi]
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if (top[p * n + mid] > k) lo = mid + 1;
+                else hi = mid;
+            }
+            rank += lo;
+        }
+        if (rank < n) s_top[rank] = k;
+    }
+    __syncthreads();
+    write_row<T>(a, r, st, s_top);
+}
+
+constexpr int LP_GROUPS = 512;      // work-groups wanted
+
+Part plan(int rows, int vocab, int top_n, char* ws) {
+    Part p{};
+    p.tiles = (int)(((long long)vocab + 7 + TILE - 1) / TILE);     // up to 7 ids' room before an unaligned row
+    const int want = std::min(p.tiles, std::max((p.tiles + TILES_MAX - 1) / TILES_MAX, (LP_GROUPS + rows - 1) / rows));
+    p.per = (p.tiles + want - 1) / want;
+    p.parts = (p.tiles + p.per - 1) / p.per;
+    p.top = (u64*)ws;
+    p.stat = (Stat*)(ws + (size_t)rows * p.parts * top_n * sizeof(u64));
+    return p;
+}
+
+}  // namespace
+
+size_t logprob_ws_bytes(int rows, int vocab, int top_n) {
+    const Part p = plan(rows, vocab, top_n, nullptr);
+    return p.parts == 1 ? 16 : (size_t)rows * p.parts * (top_n * sizeof(u64) + sizeof(Stat));
+}
+
+hipError_t launch_logprobs(int dtype, const LogprobArgs& a, hipStream_t st) {
+    const Part p = plan(a.rows, a.vocab, a.top_n, a.ws);
+    const dim3 grid((unsigned)a.rows * p.parts);
+    if (dtype == PBD_DTYPE_BF16) PBD_LAUNCH((k_logprobs<bf16>), grid, dim3(LP_T), 0, st, a, p);
+    else PBD_LAUNCH((k_logprobs<float>), grid, dim3(LP_T), 0, st, a, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.parts == 1) return e;
+    if (dtype == PBD_DTYPE_BF16) PBD_LAUNCH((k_logprobs_join<bf16>), dim3(a.rows), dim3(LP_T), 0, st, a, p);
+    else PBD_LAUNCH((k_logprobs_join<float>), dim3(a.rows), dim3(LP_T), 0, st, a, p);
+    return hipGetLastError();
+}
+
+}  // namespace pbd

@@ -1,0 +1,648 @@
+// Appending to a paged KV cache, and the attention of one new token over it.
+//
+// A block of the cache holds 16 slots of one KV head: K as the fragments that
+// S^T = K Q^T takes as its A operand, V as the A operand of O^T = V^T P^T, so
+// every wave load is a contiguous 1 KiB (K) or 512 bytes (V, bf16) wherever its
+// page lies, and the weights come out of the score accumulators in the lanes
+// that the value product wants them in.
+#include "pbd_device.h"
+#include "pbd_launch.h"
+#include "pbd_paged.h"
+
+#include <algorithm>
+
+namespace pbd {
+namespace {
+
+__device__ __forceinline__ void raise(int* status, int bit) {
+    if (status) atomicOr(status, bit);
+}
+
+// Element offset of block `blk` (16 slots) of KV head h, whose page has this id.
+__device__ __forceinline__ long long block_offset(const PageView& pg, int id, int blk, int h, int block_elems) {
+    return (long long)id * pg.page_stride + (long long)h * pg.head_stride +
+           (long long)(blk & ((1 << pg.page_shift) - 1)) * block_elems;
+}
+
+// ---------------------------------------------------------------------------
+// Append.  16 lanes hold one row of one head (RowPrep: norm and rotation stay
+// in the lanes).  MANY rows a call: a work-group takes the 16 slots of one block
+// and one head, so that K leaves in runs of 16 bytes per slot next to each other
+// and V, whose layout runs along the slots, is turned in LDS and leaves in the
+// 4-slot groups of the layout.  Few rows: the 16 lane groups take 16 heads of one
+// row (a 16-slot work-group would idle 15 of its groups), and V leaves element
+// by element.
+// ---------------------------------------------------------------------------
+
+// Whether sequence b's append is valid, the same answer in every work-group;
+// the first one reports.
+__device__ __forceinline__ bool append_ok(const PagedAppendArgs& a, int b, int len, int n, int pos, bool report) {
+    int bad = 0;
+    if (len < 0 || n < 0 || n > a.max_new || len > a.pg.cap - n || pos < 0 || pos > a.rope_len - n) bad = PBD_STATUS_CAPACITY;
+    if (!bad && n > 0) {
+        const int sh = a.pg.page_shift + 4, p0 = len >> sh, p1 = (len + n - 1) >> sh;
+        bool hit = false;
+        for (int p = p0 + (int)(threadIdx.x & 63); p <= p1; p += 64) {
+            const int id = a.pg.table[(size_t)b * a.pg.table_width + p];
+            hit |= id < 0 || id >= a.pg.n_pages;
+        }
+        if (__any(hit)) bad = PBD_STATUS_PAGE;
+    }
+    if (bad && report && threadIdx.x == 0) raise(a.pg.status, bad);
+    return !bad;
+}
+
+template <typename T, int HD, bool MANY>
+__global__ __launch_bounds__(256) void k_paged_append(PagedAppendArgs a) {
+    constexpr int NP = HD / 32, HALF = HD / 2;
+    typedef T __attribute__((ext_vector_type(NP))) tv;
+    const int b = blockIdx.z, l16 = threadIdx.x & 15, grp = threadIdx.x >> 4;
+    const int len = a.lens[b], n = a.n_new ? a.n_new[b] : a.max_new, pos = a.pos[b];
+    const bool first = blockIdx.x == 0 && blockIdx.y == 0;
+    if (!append_ok(a, b, len, n, pos, first)) return;
+    if (first && threadIdx.x == 0 && a.lens_out) a.lens_out[b] = len + n;
+    // this lane group's row and head (heads: KV first, then queries)
+    int row, head;
+    if (MANY) {
+        row = (int)((len >> 4) + blockIdx.x) * 16 + grp - len;
+        head = blockIdx.y;
+    } else {
+        row = blockIdx.x;
+        head = blockIdx.y * 16 + grp;
+    }
+    const int heads = a.n_kv + (a.q ? a.n_q : 0);
+    const bool live = row >= 0 && row < n && head < heads;
+    const int slot = len + row;
+    const bool kv = head < a.n_kv;
+    const size_t r = ((size_t)b * a.max_new + (live ? row : 0)) * a.row_stride;
+    const float2* rope = a.rope + (size_t)(pos + (live ? row : 0)) * HALF;
+    T* vblk = nullptr;
+    __shared__ T s_v[MANY ? 16 * (HD + 8) : 1];
+    if (live && !kv) {
+        const int h = head - a.n_kv;
+        RowPrep<float, HD> rp;
+        Gains<T, HD> gn;
+        float gl[NP], gh[NP], lo[NP], hi[NP];
+        rp.load(a.q + r + (size_t)h * HD, rope, l16);
+        if (a.q_norm) gn.load(a.q_norm, l16);
+        gn.get(a.q_norm != nullptr, gl, gh);
+        rp.values(true, gl, gh, a.q_norm != nullptr, a.eps, lo, hi);
+        typedef float __attribute__((ext_vector_type(NP))) fv;
+        float* dst = a.q_out + (((size_t)b * a.max_new + row) * a.n_q + h) * HD + NP * l16;
+        fv x, y;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) { x[p] = lo[p]; y[p] = hi[p]; }
+        *(fv*)dst = x;
+        *(fv*)(dst + HALF) = y;
+    }
+    if (live && kv) {
+        const int blk = slot >> 4, key = slot & 15;
+        const int id = a.pg.table[(size_t)b * a.pg.table_width + (blk >> a.pg.page_shift)];
+        const long long off = block_offset(a.pg, id, blk, head, 16 * HD);
+        T* kblk = (T*)a.pg.k + off;
+        vblk = (T*)a.pg.v + off;
+        RowPrep<float, HD> rp;
+        Gains<T, HD> gn;
+        float gl[NP], gh[NP], lo[NP], hi[NP];
+        rp.load(a.k + r + (size_t)head * HD, rope, l16);
+        if (a.k_norm) gn.load(a.k_norm, l16);
+        typedef float __attribute__((ext_vector_type(NP))) fv;
+        const float* vs = a.v + r + (size_t)head * HD + NP * l16;
+        const fv v0 = *(const fv*)vs, v1 = *(const fv*)(vs + HALF);
+        gn.get(a.k_norm != nullptr, gl, gh);
+        rp.values(true, gl, gh, a.k_norm != nullptr, a.eps, lo, hi);
+        tv x, y;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) { x[p] = from_f32<T>(lo[p]); y[p] = from_f32<T>(hi[p]); }
+        *(tv*)(kblk + kblock_elem<T>(key, NP * l16)) = x;
+        *(tv*)(kblk + kblock_elem<T>(key, HALF + NP * l16)) = y;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const T e0 = from_f32<T>(v0[p]), e1 = from_f32<T>(v1[p]);
+            if (MANY) {
+                s_v[key * (HD + 8) + NP * l16 + p] = e0;
+                s_v[key * (HD + 8) + HALF + NP * l16 + p] = e1;
+            } else {
+                vblk[vblock_elem(key, NP * l16 + p)] = e0;
+                vblk[vblock_elem(key, HALF + NP * l16 + p)] = e1;
+            }
+        }
+        if (l16 == 0) {
+            const size_t at = ((size_t)b * a.n_kv + head) * a.pg.slot_stride + slot;
+            if (a.pg.score) a.pg.score[at] = 0.f;
+            if (a.pg.slot_pos) a.pg.slot_pos[at] = pos + row;
+        }
+    }
+    if (MANY && kv) {
+        // one head and block per work-group: every group's page is the same
+        __syncthreads();
+        const int s0 = ((len >> 4) + (int)blockIdx.x) * 16;      // the block's first slot
+        if (s0 >= len + n) return;
+        const int blk = s0 >> 4;
+        const int id = a.pg.table[(size_t)b * a.pg.table_width + (blk >> a.pg.page_shift)];
+        T* dst = (T*)a.pg.v + block_offset(a.pg, id, blk, head, 16 * HD);
+        for (int i = threadIdx.x; i < HD * 4; i += 256) {
+            // run i of the block: dims i / 64 * 16 + i % 16, slots 4 g .. 4 g + 3
+            const int dim = i / 64 * 16 + i % 16, g = i / 16 % 4;
+            typedef T __attribute__((ext_vector_type(4))) t4;
+            t4 x;
+            bool in[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int s = s0 + 4 * g + e;
+                in[e] = s >= len && s < len + n;
+                if (in[e]) x[e] = s_v[(4 * g + e) * (HD + 8) + dim];
+                else x[e] = from_f32<T>(0.f);
+            }
+            if (in[0] && in[3]) {                    // the live slots are one run
+                *(t4*)(dst + (size_t)i * 4) = x;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (in[e]) dst[(size_t)i * 4 + e] = x[e];
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Attention of one token over the cache, split over its length.
+//
+// A work-group takes kps slots of one KV head for up to 16 of its query heads;
+// its four waves take the 16 NB-slot steps of the split in turn, each with its
+// own running maximum and sum, and are joined in LDS.  K and V go from the cache
+// to registers once and straight into the matrix products: the next step's K is
+// requested while this step's softmax runs, the next V while the next scores do,
+// and the blocks' addresses are looked up once per split, 64 in the wave's lanes.
+// The products do 4 * 16 * head_dim flops a slot on matrix cores whatever the
+// number of heads that share a KV head, so that the cache's bytes are the bound.
+//
+// A bf16 cache: K and V are exact operands, and the query and the weights go in
+// as three bf16 terms each, which hold all 24 bits of their fp32 values, so that
+// the result has fp32 rounding only; the extra products hide behind the loads.
+// ---------------------------------------------------------------------------
+template <typename T, int HD> struct AttnShape;
+template <int HD> struct AttnShape<bf16, HD> {
+    static constexpr int NB = 2;            // blocks of 16 slots per step
+    typedef uint2 vraw;                     // one lane's V of a 16-dim tile
+};
+template <int HD> struct AttnShape<float, HD> {
+    static constexpr int NB = 1;
+    typedef uint4 vraw;
+};
+
+__device__ __forceinline__ void clear_past(uint2& v, int n) {      // keep the first n of four slots
+    if (n < 4) v.y &= n == 3 ? 0x0000ffffu : 0u;
+    if (n < 2) v.x &= n == 1 ? 0x0000ffffu : 0u;
+}
+__device__ __forceinline__ void clear_past(uint4& v, int n) {
+    if (n < 4) v.w = 0u;
+    if (n < 3) v.z = 0u;
+    if (n < 2) v.y = 0u;
+    if (n < 1) v.x = 0u;
+}
+
+// Two floats cut to bf16 (toward zero): three such terms hold all 24 bits.
+__device__ __forceinline__ unsigned high_halves(float a, float b) {
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+
+constexpr int ATT_WAVES = 4;
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256, 2) void k_paged_attn(PagedAttnArgs a) {
+    typedef AttnShape<T, HD> SH;
+    constexpr int NB = SH::NB, ND = HD / Elt<T>::FK, NT = HD / 16, EPL = Elt<T>::EPL;
+    constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
+    constexpr int LDO = HD + 4;
+    __shared__ float s_o[ATT_WAVES][16][LDO];
+    __shared__ float s_m[ATT_WAVES][16], s_l[ATT_WAVES][16];
+    __shared__ int s_bad;
+    const int split = blockIdx.x, b = blockIdx.z;
+    const int kvh = blockIdx.y / a.plan.tiles, tile = blockIdx.y % a.plan.tiles;
+    const int G = a.n_q / a.n_kv, nq = min(16, G - tile * 16), hq0 = kvh * G + tile * 16;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+    const int len = a.lens[b];
+    const int beg = split * a.plan.kps;
+    // (a length out of range is reported by the join)
+    if (len > a.max_len || beg >= len) return;
+    const int end = min(len, beg + a.plan.kps);
+    const int blk0 = beg >> 4, blk_last = (end - 1) >> 4;
+    const int steps = (blk_last - blk0 + NB) / NB;
+    const int mine = wave < steps ? (steps - wave + ATT_WAVES - 1) / ATT_WAVES : 0;
+    if (threadIdx.x == 0) s_bad = 0;
+    __syncthreads();
+    // lane i: the address of block i % NB of this wave's step i / NB (past the
+    // last one: the last, whose slots are masked)
+    const int my_blk = min(blk0 + (wave + ATT_WAVES * (lane / NB)) * NB + lane % NB, blk_last);
+    const int id = a.pg.table[(size_t)b * a.pg.table_width + (my_blk >> a.pg.page_shift)];
+    const bool bad = id < 0 || id >= a.pg.n_pages;
+    if (bad) s_bad = 1;
+    const long long off = block_offset(a.pg, bad ? 0 : id, my_blk, kvh, 16 * HD) * (long long)sizeof(T);
+    const int off_lo = (int)(off & 0xffffffffll), off_hi = (int)(off >> 32);
+    auto at = [&](int i) -> size_t {
+        return (size_t)(unsigned)__builtin_amdgcn_readlane(off_lo, i) |
+               (size_t)(unsigned)__builtin_amdgcn_readlane(off_hi, i) << 32;
+    };
+    uint4 kf[NB][ND];
+    typename SH::vraw vf[NB][NT];
+    auto load_k = [&](int j) {
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+            const char* p = a.pg.k + at(j * NB + c);
+#pragma unroll
+            for (int d = 0; d < ND; ++d) kf[c][d] = *(const uint4*)(p + d * 1024 + lane * 16);
+        }
+    };
+    auto load_v = [&](int j) {
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+            const char* p = a.pg.v + at(j * NB + c);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) vf[c][t] = *(const typename SH::vraw*)(p + (t * 64 + lane) * sizeof(typename SH::vraw));
+        }
+    };
+    if (mine > 0) {
+        load_k(0);
+        load_v(0);
+    }
+    // the query tile as the B operand: column = head, this lane's EPL dims per fragment
+    uint4 qf[TERMS][ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+        float x[EPL];
+        const float* src = a.q + (size_t)b * a.q_stride + (size_t)(hq0 + min(col, nq - 1)) * HD + d * Elt<T>::FK + g * EPL;
+#pragma unroll
+        for (int i = 0; i < EPL; i += 4) {
+            const float4 y = *(const float4*)(src + i);
+            x[i] = y.x; x[i + 1] = y.y; x[i + 2] = y.z; x[i + 3] = y.w;
+        }
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) x[i] = col < nq ? x[i] * a.scale_log2 : 0.f;
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+            T e[EPL];
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) {
+                e[i] = from_f32<T>(x[i]);
+                x[i] -= to_f32(e[i]);
+            }
+            __builtin_memcpy(&qf[t][d], e, 16);
+        }
+    }
+    float m = -INFINITY, l = 0.f;
+    f32x4 o[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < mine; ++j) {
+        const int slot0 = (blk0 + (wave + ATT_WAVES * j) * NB) * 16;
+        f32x4 sc[NB], lo[NB];
+#pragma unroll
+        for (int c = 0; c < NB; ++c) sc[c] = lo[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int c = 0; c < NB; ++c) {
+                mma_frag<T>(sc[c], kf[c][d], qf[0][d]);
+                if constexpr (TERMS == 3) {
+                    mma_frag<T>(lo[c], kf[c][d], qf[1][d]);
+                    mma_frag<T>(lo[c], kf[c][d], qf[2][d]);
+                }
+            }
+        mfma_settle();
+        if constexpr (TERMS == 3)
+#pragma unroll
+            for (int c = 0; c < NB; ++c) sc[c] += lo[c];
+        if (j + 1 < mine) load_k(j + 1);
+        if (slot0 + 16 * NB > end) {
+#pragma unroll
+            for (int c = 0; c < NB; ++c) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (slot0 + 16 * c + 4 * g + i >= end) sc[c][i] = -INFINITY;
+                // a masked slot may hold anything: its weight is 0, its value must be finite
+#pragma unroll
+                for (int t = 0; t < NT; ++t) clear_past(vf[c][t], end - (slot0 + 16 * c + 4 * g));
+            }
+        }
+        if (a.raw && col < nq) {
+#pragma unroll
+            for (int c = 0; c < NB; ++c)
+                if (slot0 + 16 * c < end)
+                    *(f32x4*)(a.raw + ((size_t)b * a.n_q + hq0 + col) * a.plan.len_pad + slot0 + 16 * c + 4 * g) = sc[c];
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < NB; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[c][i]);
+        top = fmaxf(m, xrow_max(top));
+        if (__any(top > m)) {
+            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[t] *= f;
+            m = top;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;      // every score so far is -inf: weights 0
+        f32x4 p[NB];
+#pragma unroll
+        for (int c = 0; c < NB; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[c][i] = __builtin_amdgcn_exp2f(sc[c][i] - ref);
+                l += p[c][i];
+            }
+        if constexpr (TERMS == 3) {
+            uint4 pt[TERMS];
+#pragma unroll
+            for (int u = 0; u < TERMS; ++u) {
+                pt[u] = uint4{high_halves(p[0][0], p[0][1]), high_halves(p[0][2], p[0][3]),
+                              high_halves(p[NB - 1][0], p[NB - 1][1]), high_halves(p[NB - 1][2], p[NB - 1][3])};
+#pragma unroll
+                for (int c = 0; c < NB; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[c][i] -= __uint_as_float(__float_as_uint(p[c][i]) & 0xffff0000u);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const uint4 v = uint4{vf[0][t].x, vf[0][t].y, vf[NB - 1][t].x, vf[NB - 1][t].y};
+#pragma unroll
+                for (int u = 0; u < TERMS; ++u) mma_frag<T>(o[t], v, pt[u]);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int c = 0; c < NB; ++c) mma_k4(o[t], vf[c][t], p[c]);
+        }
+        mfma_settle();
+        if (j + 1 < mine) load_v(j + 1);
+    }
+    l = xrow_sum(l);
+    if (g == 0) {
+        s_m[wave][col] = m;
+        s_l[wave][col] = l;
+    }
+    if (col < nq)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) *(f32x4*)&s_o[wave][col][t * 16 + 4 * g] = o[t];
+    __syncthreads();
+    const bool any_bad = s_bad != 0;
+    if (any_bad && threadIdx.x == 0) raise(a.pg.status, PBD_STATUS_PAGE);
+    for (int i = threadIdx.x; i < nq * (HD / 4); i += 256) {
+        const int q = i / (HD / 4), d = i % (HD / 4) * 4;
+        float M = s_m[0][q], L = 0.f;
+#pragma unroll
+        for (int w = 1; w < ATT_WAVES; ++w) M = fmaxf(M, s_m[w][q]);
+        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < ATT_WAVES; ++w) {
+            // a wave that saw nothing but -inf (or had no step) has a sum of 0 or NaN of its own
+            const float f = s_m[w][q] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_m[w][q] - M);
+            L += f * s_l[w][q];
+            acc += *(const f32x4*)&s_o[w][q][d] * f;
+        }
+        const size_t row = ((size_t)b * a.n_q + hq0 + q) * a.plan.splits + split;
+        *(f32x4*)(a.part_o + row * HD + d) = acc;
+        if (d == 0) {
+            a.part_ml[row * 2] = any_bad ? __builtin_nanf("") : M;
+            a.part_ml[row * 2 + 1] = L;
+        }
+    }
+}
+
+// Joins the splits of one query head (work-groups x < n_q), in split order: the
+// same sums whatever ran first.  Work-groups past them (weights accumulated):
+// SCORE_SLOTS slots of one KV head each, whose kept scores become weights under
+// the head's whole sum.
+constexpr int SCORE_SLOTS = 1024;
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a) {
+    constexpr int LANES = HD / 4, GROUPS = 256 / LANES;
+    __shared__ f32x4 s_o[GROUPS][LANES];
+    __shared__ float s_max[16], s_inv[16];
+    const int b = blockIdx.y;
+    const int len = a.lens[b];
+    if (len < 0 || len > a.max_len) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) raise(a.pg.status, PBD_STATUS_CAPACITY);
+        return;
+    }
+    const int n = (len + a.plan.kps - 1) / a.plan.kps;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    // the maximum and the sum over all splits of head h; whether a page was bad
+    auto total = [&](int h, float& M, float& L) -> bool {
+        const float* ml = a.part_ml + ((size_t)b * a.n_q + h) * a.plan.splits * 2;
+        float mx = -INFINITY;
+        bool bad = false;
+        for (int s = lane; s < n; s += 64) {
+            const float x = ml[2 * s];
+            bad |= x != x;
+            mx = fmaxf(mx, x);
+        }
+        M = wave_max(mx);
+        float sum = 0.f;
+        for (int s = lane; s < n; s += 64) {
+            const float x = ml[2 * s];
+            sum += ml[2 * s + 1] * (x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x - M));
+        }
+        L = wave_sum(sum);
+        return __any(bad);
+    };
+    if ((int)blockIdx.x >= a.n_q) {
+        const int chunks = (a.max_len + SCORE_SLOTS - 1) / SCORE_SLOTS;
+        const int kvh = ((int)blockIdx.x - a.n_q) / chunks, c = ((int)blockIdx.x - a.n_q) % chunks;
+        const int G = a.n_q / a.n_kv, beg = c * SCORE_SLOTS, end = min(len, beg + SCORE_SLOTS);
+        if (beg >= end) return;
+        float* dst = a.pg.score + ((size_t)b * a.n_kv + kvh) * a.pg.slot_stride;
+        float sum[SCORE_SLOTS / 256];
+#pragma unroll
+        for (int i = 0; i < SCORE_SLOTS / 256; ++i) sum[i] = 0.f;
+        bool bad = false;
+        for (int q0 = 0; q0 < G; q0 += 16) {
+            const int nq = min(16, G - q0);
+            __syncthreads();
+            for (int q = wave; q < nq; q += 4) {
+                float M, L;
+                const bool x = total(kvh * G + q0 + q, M, L);
+                if (lane == 0) {
+                    s_max[q] = M;
+                    s_inv[q] = 1.f / L;
+                }
+                bad |= x;
+            }
+            __syncthreads();
+            for (int q = 0; q < nq; ++q) {
+                const float* raw = a.raw + ((size_t)b * a.n_q + kvh * G + q0 + q) * a.plan.len_pad;
+                const float ref = s_max[q], inv = s_inv[q];
+#pragma unroll
+                for (int i = 0; i < SCORE_SLOTS / 256; ++i) {
+                    const int s = beg + i * 256 + threadIdx.x;
+                    if (s < end) sum[i] += __builtin_amdgcn_exp2f(raw[s] - ref) * inv;
+                }
+            }
+        }
+        if (__syncthreads_or(bad)) return;
+#pragma unroll
+        for (int i = 0; i < SCORE_SLOTS / 256; ++i) {
+            const int s = beg + i * 256 + threadIdx.x;
+            if (s < end) dst[s] += sum[i];
+        }
+        return;
+    }
+    const int h = blockIdx.x;
+    float M, L;
+    if (total(h, M, L)) return;
+    const int grp = threadIdx.x / LANES, d = threadIdx.x % LANES;
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    const size_t row = ((size_t)b * a.n_q + h) * a.plan.splits;
+    for (int s = grp; s < n; s += GROUPS) {
+        const float x = a.part_ml[(row + s) * 2];
+        acc += *(const f32x4*)(a.part_o + (row + s) * HD + 4 * d) *
+               (x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x - M));
+    }
+    s_o[grp][d] = acc;
+    __syncthreads();
+    if (grp != 0) return;
+    acc = s_o[0][d];
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i) acc += s_o[i][d];
+    const float inv = n == 0 ? 0.f : 1.f / L;
+    acc *= inv;
+    if (a.out) *(f32x4*)(a.out + ((size_t)b * a.n_q + h) * HD + 4 * d) = acc;
+    if (a.lse && d == 0)
+        a.lse[(size_t)b * a.n_q + h] = n == 0 ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f;
+    if (a.op_hi) {
+        // the O projection's operand (row b, k = h HD + dim): four dims of a lane's run
+        const size_t e = xfrag_elem<T>(b, h * HD + 4 * d, a.MT);
+        if (sizeof(T) == 2 && a.op_f16) {
+            _Float16* hi = (_Float16*)a.op_hi;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) hi[e + i] = (_Float16)acc[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put_operand((T*)a.op_hi, (T*)a.op_lo, e + i, acc[i]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The decode pass's sequence state.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(64) void k_decode_begin(DecodeStepArgs a) {
+    const int b = blockIdx.x;
+    const int len = a.cache_len[b], pos = a.pos[b], tok = a.token[b];
+    int bad = 0;
+    if (pos < 0 || pos >= a.max_seq || len < 0 || len >= a.max_len) bad |= PBD_STATUS_CAPACITY;
+    if (tok < 0 || tok >= a.vocab) bad |= PBD_STATUS_TOKEN;
+    if (!bad) {
+        bool hit = false;
+        for (int p = threadIdx.x; p <= len >> (a.pg.page_shift + 4); p += 64) {
+            const int id = a.pg.table[(size_t)b * a.pg.table_width + p];
+            hit |= id < 0 || id >= a.pg.n_pages;
+        }
+        if (__any(hit)) bad = PBD_STATUS_PAGE;
+    }
+    if (threadIdx.x != 0) return;
+    if (bad) {
+        raise(a.pg.status, bad);
+        a.nrows[b] = 0;
+    }
+    a.n_new[b] = bad ? 0 : 1;
+    a.len_old[b] = bad ? 0 : len;
+    a.len_now[b] = bad ? 0 : len + 1;
+}
+
+__global__ __launch_bounds__(64) void k_decode_end(DecodeStepArgs a, int batch) {
+    const int b = blockIdx.x * 64 + threadIdx.x;
+    if (b < batch && a.n_new[b]) {
+        a.pos[b] += 1;
+        a.cache_len[b] += 1;
+    }
+}
+
+}  // namespace
+
+PageView page_view(const pbd_pages& p) {
+    PageView v{};
+    while (16 << v.page_shift < p.page_size) ++v.page_shift;
+    v.n_pages = p.n_pages; v.table_width = p.table_width;
+    v.cap = p.table_width * p.page_size;
+    if (p.score || p.slot_pos) v.cap = (int)std::min<long long>(v.cap, p.slot_stride);
+    v.page_stride = p.page_stride; v.head_stride = p.head_stride;
+    v.k = (char*)p.k; v.v = (char*)p.v; v.table = p.table;
+    v.score = p.score; v.slot_pos = p.slot_pos; v.slot_stride = p.slot_stride;
+    v.status = p.status;
+    return v;
+}
+
+constexpr int FEW_ROWS = 8;       // rows per sequence below which a work-group takes heads instead of slots
+
+hipError_t launch_paged_append(int dtype, int head_dim, const PagedAppendArgs& a, int batch, hipStream_t st) {
+    const int heads = a.n_kv + (a.q ? a.n_q : 0);
+    const bool many = a.max_new >= FEW_ROWS;
+    const dim3 grid = many ? dim3((a.max_new + 14) / 16 + 1, heads, batch) : dim3(std::max(1, a.max_new), (heads + 15) / 16, batch);
+#define PBD_APPEND(T, HD)                                                                     \
+    do {                                                                                      \
+        if (many) PBD_LAUNCH((k_paged_append<T, HD, true>), grid, dim3(256), 0, st, a);       \
+        else PBD_LAUNCH((k_paged_append<T, HD, false>), grid, dim3(256), 0, st, a);           \
+        return hipGetLastError();                                                             \
+    } while (0)
+    if (dtype == PBD_DTYPE_BF16 && head_dim == 128) PBD_APPEND(bf16, 128);
+    if (dtype == PBD_DTYPE_BF16) PBD_APPEND(bf16, 64);
+    if (head_dim == 128) PBD_APPEND(float, 128);
+    PBD_APPEND(float, 64);
+#undef PBD_APPEND
+}
+
+constexpr int KPS_MAX = 4096;     // a wave's lanes hold the addresses of 64 blocks: 4 waves, 16 slots each
+constexpr int ATT_GROUPS = 1024;  // work-groups wanted
+
+PagedAttnPlan paged_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int max_len, bool scored) {
+    PagedAttnPlan p{};
+    p.tiles = (n_q / n_kv + 15) / 16;
+    const int step = dtype == PBD_DTYPE_BF16 ? 128 : 64;           // slots that the four waves take at a time
+    const long long all = (long long)batch * n_kv * p.tiles * max_len;
+    const long long kps = std::min<long long>(KPS_MAX, (all + ATT_GROUPS - 1) / ATT_GROUPS);
+    p.kps = (int)std::max<long long>(step, (kps + step - 1) / step * step);
+    p.splits = (max_len + p.kps - 1) / p.kps;
+    p.len_pad = (max_len + 15) / 16 * 16;
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    const size_t rows = (size_t)batch * n_q * p.splits;
+    p.off_ml = up(rows * head_dim * 4);
+    p.off_raw = p.off_ml + up(rows * 2 * 4);
+    p.bytes = p.off_raw + (scored ? up((size_t)batch * n_q * p.len_pad * 4) : 0);
+    return p;
+}
+
+#define PBD_BY_TYPE(KERNEL, GRID)                                                                           \
+    do {                                                                                                    \
+        if (dtype == PBD_DTYPE_BF16 && head_dim == 128) PBD_LAUNCH((KERNEL<bf16, 128>), GRID, dim3(256), 0, st, a); \
+        else if (dtype == PBD_DTYPE_BF16) PBD_LAUNCH((KERNEL<bf16, 64>), GRID, dim3(256), 0, st, a);        \
+        else if (head_dim == 128) PBD_LAUNCH((KERNEL<float, 128>), GRID, dim3(256), 0, st, a);              \
+        else PBD_LAUNCH((KERNEL<float, 64>), GRID, dim3(256), 0, st, a);                                    \
+        return hipGetLastError();                                                                           \
+    } while (0)
+
+hipError_t launch_paged_attn_splits(int dtype, int head_dim, const PagedAttnArgs& a, int batch, hipStream_t st) {
+    PBD_BY_TYPE(k_paged_attn, dim3(a.plan.splits, a.n_kv * a.plan.tiles, batch));
+}
+
+hipError_t launch_paged_attn_join(int dtype, int head_dim, const PagedAttnArgs& a, int batch, hipStream_t st) {
+    const int chunks = a.raw ? (a.max_len + SCORE_SLOTS - 1) / SCORE_SLOTS : 0;
+    PBD_BY_TYPE(k_paged_join, dim3(a.n_q + chunks * a.n_kv, batch));
+}
+#undef PBD_BY_TYPE
+
+hipError_t launch_decode_begin(const DecodeStepArgs& a, int batch, hipStream_t st) {
+    PBD_LAUNCH(k_decode_begin, dim3(batch), dim3(64), 0, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_decode_end(const DecodeStepArgs& a, int batch, hipStream_t st) {
+    PBD_LAUNCH(k_decode_end, dim3((batch + 63) / 64), dim3(64), 0, st, a, batch);
+    return hipGetLastError();
+}
+
+}  // namespace pbd

@@ -1,0 +1,232 @@
+"""pbd_paged_attention against a plain form in 64 bits: lengths from none to
+long ones, head layouts, page sizes and strides, both types, accumulated
+weights, and what must not be read."""
+import math
+
+import pytest
+import torch
+
+import paged_ref as ref
+from paper_2607_12422_amd import binding as pbd
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+DEV = "cuda:0"
+
+
+class Call:
+    """One cache, queries and outputs on the GPU."""
+
+    def __init__(self, cache, G, scored=False, max_len=None, q_pad=0, seed=1, gain=1.0):
+        g = torch.Generator().manual_seed(seed)
+        self.cache, self.B, HQ = cache, len(cache.lens), cache.H * G
+        self.q = torch.randn(self.B, HQ, cache.D, generator=g) * gain
+        k, v, table = cache.to(DEV)
+        self.max_len = max_len or cache.width * cache.page
+        self.score0 = torch.rand(self.B, cache.H, self.max_len + 5, generator=g) if scored else None
+        self.score = self.score0.to(DEV) if scored else None
+        self.status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        self.pages = pbd.make_pages(k, v, table, n_q_heads=HQ, head_dim=cache.D, score=self.score, status=self.status)
+        flat = torch.full((self.B, HQ * cache.D + q_pad), math.nan, device=DEV)
+        flat[:, : HQ * cache.D] = self.q.to(DEV).flatten(1)
+        self.dq = flat[:, : HQ * cache.D].view(self.B, HQ, cache.D) if q_pad == 0 else \
+            flat[:, : HQ * cache.D].unflatten(1, (HQ, cache.D))
+        self.lens = torch.tensor(cache.lens, dtype=torch.int32, device=DEV)
+        self.out = torch.full((self.B, HQ, cache.D), 77.0, device=DEV)
+        self.lse = torch.full((self.B, HQ), 77.0, device=DEV)
+        n = pbd.pbd_paged_attention_workspace_bytes(self.pages, self.B, self.max_len)
+        assert n > 0
+        self.ws = torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV)      # NaN wherever it is read unwritten
+
+    def run(self, **kw):
+        pbd.pbd_paged_attention(self.pages, self.dq, self.lens, self.max_len, self.out, self.ws, lse=self.lse, **kw)
+        torch.cuda.synchronize()
+
+    def check(self, scale=None, skip=()):
+        want = ref.attention(self.cache, self.q, scale or self.cache.D ** -0.5)
+        out, lse = self.out.double().cpu(), self.lse.double().cpu()
+        for b, (n, r) in enumerate(zip(self.cache.lens, want)):
+            if b in skip:
+                assert torch.all(out[b] == 77.0) and torch.all(lse[b] == 77.0)
+                continue
+            if n == 0:
+                assert torch.all(out[b] == 0) and torch.all(lse[b] == -math.inf)
+            else:
+                assert torch.all((out[b] - r["out"]).abs() <= r["out_tol"]), (b, n, (out[b] - r["out"]).abs().max())
+                assert torch.all((lse[b] - r["lse"]).abs() <= r["lse_tol"]), (b, n)
+            if self.score is not None:
+                got, s0 = self.score[b].double().cpu(), self.score0[b].double()
+                assert torch.equal(got[:, n:], s0[:, n:])
+                # one rounding of the sum into the score
+                tol = r["w_tol"] + (s0[:, :n] + r["w"]) * ref.U
+                assert torch.all((got[:, :n] - s0[:, :n] - r["w"]).abs() <= tol), (b, n)
+
+
+LENS = [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300, 513]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("scored", [False, True])
+def test_lengths(dtype, D, scored):
+    c = Call(ref.Cache(LENS, 2, D, dtype, seed=D), 2, scored)
+    c.run()
+    c.check()
+    assert int(c.status) == 0
+
+
+@pytest.mark.parametrize("H,G", [(1, 1), (3, 3), (8, 2), (2, 8), (1, 16), (2, 17), (1, 40), (1, 80)])
+def test_head_layouts(H, G):
+    for dtype, D in ((BF, 128), (F32, 64)):
+        c = Call(ref.Cache([200, 77], H, D, dtype, seed=G), G, scored=True)
+        c.run()
+        c.check()
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 256, 4096])
+@pytest.mark.parametrize("major", ["page", "head"])
+def test_pages_and_strides(page, major):
+    c = Call(ref.Cache([130, 1, 0, 259], 3, 64, BF, page=page, major=major, seed=page), 4, scored=True, q_pad=12)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("B,n", [(1, 4096), (1, 33001), (3, 9000), (40, 700)])
+def test_splits(B, n):
+    """Few and many splits of a length, the last one ragged."""
+    lens = [n - 17 * b for b in range(B)]
+    c = Call(ref.Cache(lens, 2, 128, BF, page=64, seed=n), 2, scored=B < 4)
+    c.run()
+    c.check()
+
+
+def test_a_bound_longer_than_any_sequence():
+    c = Call(ref.Cache([5, 40], 2, 128, BF, room=5000), 2, scored=True)
+    assert c.max_len > 5000
+    c.run()
+    c.check()
+
+
+def test_sharp_and_flat_weights():
+    """Scores up to some hundreds (one slot takes all) and of 0 (equal weights)."""
+    for gain in (0.0, 40.0):
+        c = Call(ref.Cache([1, 100, 1000], 2, 128, BF, seed=5), 4, scored=True, gain=gain)
+        c.run()
+        c.check()
+
+
+def test_scale_and_stream():
+    c = Call(ref.Cache([100, 3], 2, 128, BF), 2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    c.run(scale=0.3, stream=side)
+    side.synchronize()
+    c.check(scale=0.3)
+
+
+def test_infinities_and_nan_of_live_slots_reach_the_output():
+    """A NaN value reaches its dim of every head that reads it; an infinite one likewise."""
+    cache = ref.Cache([40, 40], 1, 64, F32)
+    cache.dv[0, 0, 7, 3] = math.nan
+    cache.dv[1, 0, 39, 5] = math.inf
+    for b in range(2):
+        cache.put(b, 0, cache.dk[b, :, :40], cache.dv[b, :, :40])
+    c = Call(cache, 2)
+    c.run()
+    out = c.out.cpu()
+    assert torch.isnan(out[0, :, 3]).all() and torch.isinf(out[1, :, 5]).all()
+    assert torch.isfinite(out[0, :, :3]).all() and torch.isfinite(out[1, :, 6:]).all()
+
+
+def test_bitwise_the_same_again_and_beside_other_sequences():
+    cache = ref.Cache([500, 77, 1200], 2, 128, BF, seed=3)
+    c = Call(cache, 2)
+    c.run()
+    first = c.out.clone()
+    c.run()
+    assert torch.equal(first, c.out)
+    other = torch.tensor([1, 77, 30], dtype=torch.int32, device=DEV)
+    c.lens = other
+    c.run()
+    assert torch.equal(first[1], c.out[1])
+
+
+def test_shared_pages():
+    """Two sequences over the same pages, of different lengths."""
+    cache = ref.Cache([300, 300], 2, 128, BF, seed=9)
+    cache.table[1] = cache.table[0]
+    cache.dk[1], cache.dv[1] = cache.dk[0], cache.dv[0]
+    cache.lens = [300, 123]
+    c = Call(cache, 2)
+    c.run()
+    c.check()
+
+
+def test_offsets_past_32_bits():
+    """A pool of more than 2^31 elements (2^32 bytes), its last pages in use."""
+    H, D, page, n = 8, 128, 64, 2 ** 31 // (8 * 128 * 64) + 40
+    small = ref.Cache([1000], H, D, BF, page=page, seed=11)
+    k = torch.empty(n, H, page * D, dtype=BF, device=DEV)
+    v = torch.empty(n, H, page * D, dtype=BF, device=DEV)
+    last = torch.arange(n - small.width, n)
+    for pool, src in ((k, small.k), (v, small.v)):
+        pool[last] = src[small.table[0].long()].to(DEV)
+    c = Call(small, 2)
+    table = last.to(torch.int32).to(DEV).view(1, -1)
+    c.pages = pbd.make_pages(k, v, table, n_q_heads=2 * H, head_dim=D, status=c.status)
+    c.run()
+    c.check()
+
+
+def test_lengths_out_of_range_skip_the_sequence():
+    c = Call(ref.Cache([100, 60, 50], 2, 64, BF), 2, scored=True)
+    good = c.lens.clone()
+    c.lens = torch.tensor([100, c.max_len + 1, -1], dtype=torch.int32, device=DEV)
+    c.cache.lens = [100, 0, 0]
+    c.run()
+    c.check(skip=(1, 2))
+    assert int(c.status) == pbd.PBD_STATUS_CAPACITY
+    assert torch.equal(c.score.cpu()[1:], c.score0[1:])
+    c.lens = good
+
+
+def test_bad_pages_skip_the_sequence():
+    c = Call(ref.Cache([100, 1100], 2, 64, BF), 2, scored=True)
+    k, v, table = c.pages.keep[:3]
+    for bad in (-1, k.shape[0], 2 ** 31 - 1, -2 ** 31):
+        t = table.clone()
+        t[1, 40] = bad
+        c.status.zero_()
+        c.out.fill_(77.0)
+        c.lse.fill_(77.0)
+        c.score.copy_(c.score0)
+        c.pages = pbd.make_pages(k, v, t, n_q_heads=4, head_dim=64, score=c.score, status=c.status)
+        c.run()
+        want = ref.attention(c.cache, c.q, 64 ** -0.5)[0]
+        assert torch.all((c.out[0].double().cpu() - want["out"]).abs() <= want["out_tol"])
+        assert torch.all(c.out[1] == 77.0) and torch.all(c.lse[1] == 77.0)
+        assert torch.equal(c.score[1].cpu(), c.score0[1])
+        assert int(c.status) == pbd.PBD_STATUS_PAGE
+
+
+def test_captured_and_replayed():
+    """A replay reads the lengths and queries of its time; two graphs with a workspace each, in turn."""
+    calls = [Call(ref.Cache([400, 90], 2, 128, BF, seed=s), 2, scored=True, seed=s) for s in (1, 2)]
+    graphs = []
+    for c in calls:
+        c.run()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            pbd.pbd_paged_attention(c.pages, c.dq, c.lens, c.max_len, c.out, c.ws, lse=c.lse)
+        graphs.append(g)
+    for n in (400, 17, 0, 233):
+        for c, g in zip(calls, graphs):
+            c.lens[0] = n
+            c.cache.lens[0] = n
+            c.score.copy_(c.score0)
+            c.out.fill_(77.0)
+            g.replay()
+        torch.cuda.synchronize()
+        for c in calls:
+            c.check()
