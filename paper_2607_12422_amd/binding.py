@@ -209,7 +209,9 @@ def _check(rc: int, ctx=None):
 # -- operators over a paged KV cache, and log probabilities ----------------------------
 # The tensors of a call lie on one device; the stream is that device's current
 # one unless another is given.  Shapes and types are checked here, because the
-# library sees pointers only; the values are the library's to check.
+# library sees pointers only; the values are the library's to check.  A decode
+# step makes these calls one after another with little work on the device, so
+# their own time counts: messages are made where a check fails only.
 
 
 def _need(ok: bool, what: str):
@@ -218,90 +220,107 @@ def _need(ok: bool, what: str):
 
 
 def _dtype_id(t, what: str) -> int:
-    import torch
-    _need(t.dtype in (torch.float32, torch.bfloat16), f"{what} must be float32 or bfloat16")
-    return PBD_DTYPE_BF16 if t.dtype == torch.bfloat16 else PBD_DTYPE_F32
+    d = str(t.dtype)
+    _need(d in ("torch.float32", "torch.bfloat16"), f"{what} must be float32 or bfloat16")
+    return PBD_DTYPE_BF16 if d == "torch.bfloat16" else PBD_DTYPE_F32
 
 
-def _i32(t, n: int, what: str, device):
-    """Pointer of a contiguous int32 device tensor of n elements (None: NULL)."""
-    import torch
+def _i32(t, n: int, what: str, device: int):
+    """Pointer of a contiguous int32 tensor of n elements on a device (-1: the host; None: NULL)."""
     if t is None:
         return None
-    _need(t.dtype == torch.int32 and t.numel() == n and t.is_contiguous() and t.device == device,
-          f"{what} must be a contiguous int32 tensor of {n} elements on {device}")
+    if t.dtype is not _torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        raise PbdError(PBD_ERR_INVALID_ARG, f"{what} must be a contiguous int32 tensor of {n} elements, with the others")
     return t.data_ptr()
 
 
-def _f32(t, n: int, what: str, device):
-    import torch
+def _f32(t, n: int, what: str, device: int):
     if t is None:
         return None
-    _need(t.dtype == torch.float32 and t.numel() == n and t.is_contiguous() and t.device == device,
-          f"{what} must be a contiguous float32 tensor of {n} elements on {device}")
+    if t.dtype is not _torch.float32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        raise PbdError(PBD_ERR_INVALID_ARG, f"{what} must be a contiguous float32 tensor of {n} elements, with the others")
     return t.data_ptr()
 
 
-def _space(ws, device):
+def _space(ws, device: int):
     """(pointer, bytes) of a workspace tensor."""
-    _need(ws is not None and ws.is_contiguous() and ws.device == device, f"ws must be a contiguous tensor on {device}")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    if ws is None or not ws.is_contiguous() or ws.get_device() != device:
+        raise PbdError(PBD_ERR_INVALID_ARG, "ws must be a contiguous tensor, with the others")
+    return ws.data_ptr(), ws.nbytes
 
 
-def _call(device, stream, fn, *args):
+def _call(device: int, stream, fn, *args):
     """fn(*args, stream) with the device current."""
-    import torch
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    st = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
-    if device.index is None or device.index == torch.cuda.current_device():
+        st = _raw_stream(device)
+    else:
+        st = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+    if device == _torch.cuda.current_device():
         rc = fn(*args, st)
     else:
-        with torch.cuda.device(device):
+        with _torch.cuda.device(device):
             rc = fn(*args, st)
-    _check(rc, None)
+    if rc != PBD_OK:
+        _check(rc, None)
+
+
+def _raw_stream(device: int) -> int:
+    """The device's current stream: torch's own short way to the handle, where it has one (0.1 us against 1.1)."""
+    short = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
+    return short(device) if short else _torch.cuda.current_stream(device).cuda_stream
+
+
+class _LazyTorch:
+    """torch, imported when an operator first needs it (the module's other users may not)."""
+
+    def __getattr__(self, name):
+        import torch
+        global _torch
+        _torch = torch
+        return getattr(torch, name)
+
+
+_torch = _LazyTorch()
 
 
 def make_pages(k, v, table, n_q_heads: int, head_dim: int, score=None, slot_pos=None, status=None) -> PbdPages:
     """pbd_pages of a cache of one layer, k and v [n_pages][n_kv_heads][page_size * head_dim], or of several,
     [layers][n_pages][...]; table int32 [batch][pages]; score float32 and slot_pos int32 [batch][n_kv_heads][slots]
     (layers first where k has them).  Pages and heads may have any strides, a page of a head is contiguous."""
-    import torch
     _need(k.dim() in (3, 4) and v.shape == k.shape and v.dtype == k.dtype and v.stride() == k.stride(),
           "k and v must be alike, [n_pages][n_kv_heads][page_size * head_dim], layers first")
     _need(k.stride(-1) == 1, "a page of a head must be contiguous")
-    _need(table.dim() == 2 and table.dtype == torch.int32 and table.is_contiguous(),
-          "table must be a contiguous int32 tensor [batch][pages]")
     _need(head_dim > 0 and k.shape[-1] % head_dim == 0, "a page does not hold whole positions")
-    B, H = table.shape[0], k.shape[-2]
-    p = PbdPages(dtype=_dtype_id(k, "k"), n_q_heads=n_q_heads, n_kv_heads=H, head_dim=head_dim,
+    dev = k.get_device()
+    p = PbdPages(dtype=_dtype_id(k, "k"), n_q_heads=n_q_heads, n_kv_heads=k.shape[-2], head_dim=head_dim,
                  page_size=k.shape[-1] // head_dim, n_pages=k.shape[-3], page_stride=k.stride(-3),
                  head_stride=k.stride(-2), layer_stride=k.stride(0) if k.dim() == 4 else 0, k=k.data_ptr(),
-                 v=v.data_ptr(), table=table.data_ptr(), table_width=table.shape[1])
-    _attach(p, k.device, B, k.shape[0] if k.dim() == 4 else None, score, slot_pos, status)
-    for t, what in ((v, "v"), (table, "table")):
-        _need(t.device == k.device, f"{what} must be on {k.device}")
-    p.keep = (k, v, table, score, slot_pos, status)
-    p.device, p.rows = k.device, B
-    return p
+                 v=v.data_ptr())
+    _need(v.get_device() == dev, "k and v must be on one device")
+    return _attach(p, dev, k.shape[0] if k.dim() == 4 else None, table, score, slot_pos, status, (k, v))
 
 
-def _attach(p: PbdPages, device, B: int, layers, score, slot_pos, status):
-    import torch
-    H, slots = p.n_kv_heads, None
-    for t, dt, what in ((score, torch.float32, "score"), (slot_pos, torch.int32, "slot_pos")):
+def _attach(p: PbdPages, device: int, layers, table, score, slot_pos, status, keep) -> PbdPages:
+    _need(table.dim() == 2 and table.dtype == _torch.int32 and table.is_contiguous() and table.get_device() == device,
+          "table must be a contiguous int32 tensor [batch][pages] with the cache")
+    p.table, p.table_width = table.data_ptr(), table.shape[1]
+    B, H, slots = table.shape[0], p.n_kv_heads, None
+    for t, dt, what in ((score, _torch.float32, "score"), (slot_pos, _torch.int32, "slot_pos")):
         if t is None:
             continue
         slots = t.shape[-1] if slots is None else slots
         want = (B, H, slots) if layers is None else (layers, B, H, slots)
-        _need(t.dtype == dt and tuple(t.shape) == want and t.is_contiguous() and t.device == device,
-              f"{what} must be a contiguous {dt} tensor {list(want)} on {device}")
+        _need(t.dtype == dt and tuple(t.shape) == want and t.is_contiguous() and t.get_device() == device,
+              f"{what} must be a contiguous {dt} tensor {list(want)} with the cache")
         setattr(p, what, t.data_ptr())
     if slots is not None:
         p.slot_stride = slots
         p.state_layer_stride = B * H * slots if layers is not None else 0
     if status is not None:
         p.status = _i32(status, 1, "status", device)
+    p.keep = keep + (table, score, slot_pos, status)
+    p.device, p.rows, p.ref = device, B, ctypes.byref(p)
+    return p
 
 
 def layer_pages(pages: PbdPages, layer: int) -> PbdPages:
@@ -313,7 +332,7 @@ def layer_pages(pages: PbdPages, layer: int) -> PbdPages:
     for name in ("score", "slot_pos"):
         if getattr(pages, name):
             setattr(p, name, getattr(pages, name) + layer * pages.state_layer_stride * 4)
-    p.keep, p.device, p.rows = pages.keep, pages.device, pages.rows
+    p.keep, p.device, p.rows, p.ref = pages.keep, pages.device, pages.rows, ctypes.byref(p)
     return p
 
 
@@ -325,14 +344,16 @@ def pbd_paged_attention(pages: PbdPages, q, lens, max_len: int, out, ws, lse=Non
                         stream=None):
     """q float32 [batch][n_q_heads][head_dim] (any stride from a sequence to the next), lens int32 [batch]; out
     float32 like q, lse float32 [batch][n_q_heads].  scale: 1 / sqrt(head_dim) if None."""
-    import torch
-    dev = pages.device
-    B, HQ, D = lens.numel(), pages.n_q_heads, pages.head_dim
-    _need(q.dtype == torch.float32 and tuple(q.shape) == (B, HQ, D) and q.stride(2) == 1 and q.stride(1) == D and
-          q.device == dev, "q must be float32 [batch][n_q_heads][head_dim], the heads of a sequence contiguous")
-    _need(B <= pages.rows, "the table has fewer rows than lens")
+    dev, HQ, D = pages.device, pages.n_q_heads, pages.head_dim
+    B = lens.numel()
+    if (q.dtype is not _torch.float32 or q.shape != (B, HQ, D) or q.stride(2) != 1 or (q.stride(1) != D and HQ > 1) or
+            q.get_device() != dev):
+        raise PbdError(PBD_ERR_INVALID_ARG,
+                       "q must be float32 [batch][n_q_heads][head_dim], the heads of a sequence contiguous")
+    if B > pages.rows:
+        raise PbdError(PBD_ERR_INVALID_ARG, "the table has fewer rows than lens")
     w, wb = _space(ws, dev)
-    _call(dev, stream, load_library().pbd_paged_attention, ctypes.byref(pages), B, q.data_ptr(),
+    _call(dev, stream, load_library().pbd_paged_attention, pages.ref, B, q.data_ptr(),
           q.stride(0) if B > 1 else HQ * D, _i32(lens, B, "lens", dev), max_len,
           D ** -0.5 if scale is None else scale, _f32(out, B * HQ * D, "out", dev), _f32(lse, B * HQ, "lse", dev), w, wb)
 
@@ -342,25 +363,26 @@ def pbd_paged_append(pages: PbdPages, k, v, lens, pos, rope, q=None, q_out=None,
     """k, v float32 [batch][rows][n_kv_heads * head_dim] and q [batch][rows][n_q_heads * head_dim], all with the same
     stride from a row to the next (columns of one projection); lens, pos, n_new, len_out int32 [batch]; rope float32
     [positions][head_dim / 2][2]; q_norm, k_norm [head_dim] in the cache's type; q_out float32 like q, contiguous."""
-    import torch
-    dev = pages.device
+    dev, H, HQ, D = pages.device, pages.n_kv_heads, pages.n_q_heads, pages.head_dim
     B, R = k.shape[0], k.shape[1]
-    H, HQ, D = pages.n_kv_heads, pages.n_q_heads, pages.head_dim
-    stride = next((t.stride(1) for t in (k, v, q) if t is not None and R > 1),
-                  next((t.stride(0) for t in (k, v, q) if t is not None and B > 1), max(HQ, H) * D))
-    stride = stride if R > 1 or B > 1 else -(-stride // 4) * 4
-    for t, heads, what in ((k, H, "k"), (v, H, "v"), (q, HQ, "q")):
-        _need(t is None or (t.dtype == torch.float32 and tuple(t.shape) == (B, R, heads * D) and t.device == dev and
-                            t.stride(2) == 1 and (R == 1 or t.stride(1) == stride) and
-                            (B == 1 or t.stride(0) == R * stride)),
-              f"{what} must be float32 [batch][rows][heads * head_dim] with the row stride of k")
-    _need(B <= pages.rows, "the table has fewer rows than k")
-    _need(rope.dtype == torch.float32 and rope.is_contiguous() and rope.device == dev and
-          tuple(rope.shape[1:]) == (D // 2, 2), "rope must be contiguous float32 [positions][head_dim / 2][2]")
+    # rows lie at one stride: that of the rows, or of the sequences where each has one
+    stride = k.stride(1) if R > 1 else k.stride(0) if B > 1 else max(HQ, H) * D
+    for t, width, what in ((k, H * D, "k"), (v, H * D, "v"), (q, HQ * D, "q")):
+        if t is not None and (t.dtype is not _torch.float32 or t.shape != (B, R, width) or t.stride(2) != 1 or
+                              (R > 1 and t.stride(1) != stride) or (B > 1 and t.stride(0) != R * stride) or
+                              t.get_device() != dev):
+            raise PbdError(PBD_ERR_INVALID_ARG,
+                           f"{what} must be float32 [batch][rows][{width}] with the row stride of k")
+    if B > pages.rows:
+        raise PbdError(PBD_ERR_INVALID_ARG, "the table has fewer rows than k")
+    if (rope.dtype is not _torch.float32 or not rope.is_contiguous() or rope.get_device() != dev or
+            rope.shape[1:] != (D // 2, 2)):
+        raise PbdError(PBD_ERR_INVALID_ARG, "rope must be contiguous float32 [positions][head_dim / 2][2]")
     for t, what in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-        _need(t is None or (_dtype_id(t, what) == pages.dtype and t.numel() == D and t.is_contiguous() and
-                            t.device == dev), f"{what} must be a contiguous [head_dim] tensor of the cache's type")
-    _call(dev, stream, load_library().pbd_paged_append, ctypes.byref(pages), B, R, _ptr(q), k.data_ptr(), v.data_ptr(),
+        if t is not None and (t.numel() != D or not t.is_contiguous() or t.get_device() != dev or
+                              t.dtype is not (_torch.bfloat16 if pages.dtype == PBD_DTYPE_BF16 else _torch.float32)):
+            raise PbdError(PBD_ERR_INVALID_ARG, f"{what} must be a contiguous [head_dim] tensor of the cache's type")
+    _call(dev, stream, load_library().pbd_paged_append, pages.ref, B, R, _ptr(q), k.data_ptr(), v.data_ptr(),
           stride, _i32(lens, B, "lens", dev), _i32(n_new, B, "n_new", dev), _i32(pos, B, "pos", dev), _ptr(q_norm),
           _ptr(k_norm), eps, rope.data_ptr(), rope.shape[0], _f32(q_out, B * R * HQ * D, "q_out", dev),
           _i32(len_out, B, "len_out", dev))
@@ -376,12 +398,13 @@ def pbd_paged_evict(pages: PbdPages, lens, max_len: int, keep, new_lens, ws, pos
     they are if None."""
     dev = pages.device
     B = lens.numel()
-    _need(B <= pages.rows, "the table has fewer rows than lens")
+    if B > pages.rows:
+        raise PbdError(PBD_ERR_INVALID_ARG, "the table has fewer rows than lens")
     n = pages.rows * pages.n_kv_heads * pages.slot_stride
     so = pages.score if score_out is None else _f32(score_out, n, "score_out", dev)
     po = pages.slot_pos if slot_pos_out is None else _i32(slot_pos_out, n, "slot_pos_out", dev)
     w, wb = _space(ws, dev)
-    _call(dev, stream, load_library().pbd_paged_evict, ctypes.byref(pages), B, _i32(lens, B, "lens", dev), max_len,
+    _call(dev, stream, load_library().pbd_paged_evict, pages.ref, B, _i32(lens, B, "lens", dev), max_len,
           _i32(keep, B, "keep", dev), _i32(pos, B, "pos", dev), recent, sink, so, po,
           _i32(new_lens, B, "new_lens", dev), w, wb)
 
@@ -394,14 +417,15 @@ def pbd_token_logprobs(logits, tokens, logprob, ws, entropy=None, top_ids=None, 
                        stream=None):
     """logits float32 or bfloat16 [..., vocab] (rows at one stride), tokens int32 [rows] (-1: padding) and logprob
     float32 [rows], or both None; entropy float32 [rows]; top_ids int32 and top_logprobs float32 [rows, n]."""
-    dev = logits.device
-    V = logits.shape[-1]
-    x = logits if logits.dim() == 2 else logits.view(-1, V)
-    R = x.shape[0]
-    _need(x.stride(1) == 1 or V == 1, "the logits of a row must be contiguous")
+    dev = logits.get_device()
+    x = logits if logits.dim() == 2 else logits.view(-1, logits.shape[-1])
+    R, V = x.shape
+    dt = PBD_DTYPE_F32 if x.dtype is _torch.float32 else _dtype_id(x, "logits")
+    if x.stride(1) != 1 and V > 1:
+        raise PbdError(PBD_ERR_INVALID_ARG, "the logits of a row must be contiguous")
     n = 0 if top_ids is None else top_ids.shape[-1]
     w, wb = _space(ws, dev)
-    _call(dev, stream, load_library().pbd_token_logprobs, R, V, _dtype_id(x, "logits"), x.data_ptr(),
+    _call(dev, stream, load_library().pbd_token_logprobs, R, V, dt, x.data_ptr(),
           x.stride(0) if R > 1 else V, _i32(tokens, R, "tokens", dev), n, _f32(logprob, R, "logprob", dev),
           _f32(entropy, R, "entropy", dev), _i32(top_ids, R * n, "top_ids", dev),
           _f32(top_logprobs, R * n, "top_logprobs", dev), _i32(status, 1, "status", dev), w, wb)
@@ -523,21 +547,14 @@ class Engine:
             nblk = -(-self.pcfg.max_seq // 16)
             slots = torch.arange(self.pcfg.max_batch, dtype=torch.int32, device=self.device)[:, None]
             table = slots * (p.n_kv_heads * nblk) + torch.arange(nblk, dtype=torch.int32, device=self.device)
-        _need(table.dim() == 2 and table.dtype == torch.int32 and table.is_contiguous() and
-              table.device.type == self.device.type, "table must be a contiguous int32 tensor [batch][pages]")
-        p.table, p.table_width = table.data_ptr(), table.shape[1]
-        _attach(p, table.device, table.shape[0], self.cfg.n_layers, score, slot_pos, None)
-        p.keep = (self.kv, table, score, slot_pos)
-        p.device, p.rows = table.device, table.shape[0]
-        return p
+        return _attach(p, self.kv.get_device(), self.cfg.n_layers, table, score, slot_pos, None, (self.kv,))
 
     def pbd_decode_paged_workspace_bytes(self, pages: PbdPages, batch: int, max_len: int) -> int:
         return self.lib.pbd_decode_paged_workspace_bytes(self.ctx, ctypes.byref(pages), batch, max_len)
 
     def pbd_decode_paged(self, pages: PbdPages, token, pos, cache_len, max_len: int, ws, logits=None,
                          flags: int = PBD_PASS_DEFAULT, stream=None):
-        B = int(token.shape[0])
-        dev = pages.device
+        B, dev = int(token.shape[0]), pages.device
         _need(B <= pages.rows, "the table has fewer rows than token")
         w, wb = _space(ws, dev)
         rc = self.lib.pbd_decode_paged(self.ctx, ctypes.byref(pages), B, _i32(token, B, "token", dev),

@@ -82,21 +82,42 @@ struct Row {
         p = (const T*)logits + (long long)r * stride;
         off = (int)(((size_t)p & 15) / sizeof(T));
     }
-    // values of vector i; -inf outside the row, of which nothing is read
-    __device__ __forceinline__ void load(int i, float* x) const {
+    // vector i, all of it in the row
+    __device__ __forceinline__ uint4 whole(int i) const { return *(const uint4*)(p + ((long long)i * N - off)); }
+    // vector i; -inf outside the row, of which nothing is read
+    __device__ __forceinline__ uint4 any(int i) const {
         const int id = i * N - off;
-        if (id >= 0 && id + N <= vocab) {
-            const uint4 raw = *(const uint4*)(p + id);
-            T e[N];
-            __builtin_memcpy(e, &raw, 16);
+        if (id >= 0 && id + N <= vocab) return whole(i);
+        T e[N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) x[k] = to_f32(e[k]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) x[k] = id + k >= 0 && id + k < vocab ? to_f32(p[id + k]) : -INFINITY;
-        }
+        for (int k = 0; k < N; ++k) e[k] = id + k >= 0 && id + k < vocab ? p[id + k] : from_f32<T>(-INFINITY);
+        uint4 raw;
+        __builtin_memcpy(&raw, e, 16);
+        return raw;
     }
+    // whether every vector of a tile lies in the row
+    __device__ __forceinline__ bool inner(int tile) const {
+        return (tile > 0 || off == 0) && (tile + 1) * TILE - off <= vocab;
+    }
+    static __device__ __forceinline__ void values(const uint4& raw, float* x) {
+        T e[N];
+        __builtin_memcpy(e, &raw, 16);
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = to_f32(e[k]);
+    }
+    __device__ __forceinline__ void load(int i, float* x) const { values(any(i), x); }
 };
+
+// Maximum over the wave, in every lane (DPP inside the 16-lane rows, then permlane swaps).
+__device__ __forceinline__ float wave_max_dpp(float v) {
+#define PBD_STEP(CTRL) v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false)))
+    PBD_STEP(0xB1);      // lane ^ 1
+    PBD_STEP(0x4E);      // lane ^ 2
+    PBD_STEP(0x141);     // half-row mirror
+    PBD_STEP(0x140);     // row mirror
+#undef PBD_STEP
+    return xrow_max(v);
+}
 
 __device__ __forceinline__ u64 wave_max64(u64 v) {
 #pragma unroll
@@ -157,16 +178,28 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
     const Row<T> row(a.logits, a.row_stride, r, a.vocab);
     const int t0 = part * pt.per, t1 = min(pt.tiles, t0 + pt.per);
     float m = -INFINITY, s = 0.f, t = 0.f, mine = -INFINITY;
+    uint4 next[PER];
+    auto fetch = [&](int tile) {
+        if (row.inner(tile)) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) next[i] = row.whole((tile * PER + i) * LP_T + tid);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) next[i] = row.any((tile * PER + i) * LP_T + tid);
+        }
+    };
+    fetch(t0);
     for (int tile = t0; tile < t1; ++tile) {
         float x[GROUP];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) row.load((tile * PER + i) * LP_T + tid, x + i * N);
+        for (int i = 0; i < PER; ++i) Row<T>::values(next[i], x + i * N);
+        if (tile + 1 < t1) fetch(tile + 1);
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < GROUP; ++i) top = fmaxf(top, x[i]);
         s_group[(tile - t0) * LP_T + tid] = top;
         mine = fmaxf(mine, top);
-        top = wave_max(top);
+        top = wave_max_dpp(top);
         if (top > m) {
             if (m > -INFINITY) {
                 // lane 0 has the instance of the old maximum that the sum leaves out
@@ -296,34 +329,68 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
     for (int i = tid; i < n; i += LP_T) pt.top[at * n + i] = s_top[i];
 }
 
-// Joins the parts of a row, in order; the rank of an alternative is the sum over
-// the parts of how many of theirs are above it, each found by bisection.
+// Joins the parts of a row, in order.  Every part's j best are there, so the least
+// of the parts' j-th best has j parts above or at it: with j = ceil(n / parts) it
+// is a lower bound of the n-th best, and only what reaches it is ranked.
 template <typename T>
 __global__ __launch_bounds__(LP_T) void k_logprobs_join(LogprobArgs a, Part pt) {
     __shared__ u64 s_top[TOP_MAX];
-    const int r = blockIdx.x;
+    __shared__ u64 s_cand[CAND_CAP];
+    __shared__ u64 s_low[4];
+    __shared__ int s_cands;
+    const int r = blockIdx.x, tid = threadIdx.x;
     if (!row_ok(a, r, false)) return;
+    const int n = a.top_n, all = pt.parts * n;
+    const u64* top = pt.top + (size_t)r * all;
+    constexpr int KEEP = 2;
+    u64 mine[KEEP];
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) mine[i] = tid + i * LP_T < all ? top[tid + i * LP_T] : 0;
+    // (all threads hold the row's statistics; the parts in order)
     const Stat* stat = pt.stat + (size_t)r * pt.parts;
     Stat st = stat[0];
     for (int p = 1; p < pt.parts; ++p) st = join(st, stat[p]);
-    if (threadIdx.x < TOP_MAX) s_top[threadIdx.x] = 0;
-    __syncthreads();
-    const u64* top = pt.top + (size_t)r * pt.parts * a.top_n;
-    const int n = a.top_n;
-    for (int i = threadIdx.x; i < pt.parts * n; i += LP_T) {
-        const u64 k = top[i];
-        if (k == 0) continue;
-        int rank = 0;
-        for (int p = 0; p < pt.parts && rank < n; ++p) {
-            int lo = 0, hi = n;                       // entries above k: top[p n + lo - 1] > k >= top[p n + hi]
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (top[p * n + mid] > k) lo = mid + 1;
-                else hi = mid;
-            }
-            rank += lo;
+    if (tid < TOP_MAX) s_top[tid] = 0;
+    if (tid == 0) s_cands = 0;
+    if (n > 0) {
+        const int j = (n + pt.parts - 1) / pt.parts;
+        u64 low = ~0ull;
+        for (int p = tid; p < pt.parts; p += LP_T) {
+            const u64 k = top[p * n + j - 1];
+            low = k < low ? k : low;
         }
-        if (rank < n) s_top[rank] = k;
+        low = ~wave_max64(~low);
+        if ((tid & 63) == 0) s_low[tid >> 6] = low;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) low = s_low[w] < low ? s_low[w] : low;
+        auto push = [&](u64 k) {
+            if (k == 0 || k < low) return;
+            const int i = atomicAdd(&s_cands, 1);
+            if (i < CAND_CAP) s_cand[i] = k;
+        };
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) push(mine[i]);
+        for (int i = tid + KEEP * LP_T; i < all; i += LP_T) push(top[i]);
+        __syncthreads();
+        const int cands = s_cands;
+        if (cands <= CAND_CAP) {
+            for (int i = tid; i < cands; i += LP_T) {
+                const u64 k = s_cand[i];
+                int rank = 0;
+                for (int q = 0; q < cands; ++q) rank += s_cand[q] > k;
+                if (rank < n) s_top[rank] = k;
+            }
+        } else {
+            // (a part with most of the best ones: rank against every entry)
+            for (int i = tid; i < all; i += LP_T) {
+                const u64 k = top[i];
+                if (k == 0 || k < low) continue;
+                int rank = 0;
+                for (int q = 0; q < all && rank < n; ++q) rank += top[q] > k;
+                if (rank < n) s_top[rank] = k;
+            }
+        }
     }
     __syncthreads();
     write_row<T>(a, r, st, s_top);
