@@ -119,6 +119,8 @@ __device__ __forceinline__ float wave_max_dpp(float v) {
     return xrow_max(v);
 }
 
+__device__ __forceinline__ float wave_sum_dpp(float v) { return xrow_sum(row16_sum(v)); }
+
 __device__ __forceinline__ u64 wave_max64(u64 v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -137,14 +139,16 @@ __device__ __forceinline__ bool row_ok(const LogprobArgs& a, int r, bool first) 
     return false;
 }
 
+// The logit of the row's token, for thread 0.
 template <typename T>
-__device__ __forceinline__ void write_row(const LogprobArgs& a, int r, Stat st, const u64* top) {
+__device__ __forceinline__ float chosen_logit(const LogprobArgs& a, int r) {
+    return a.logprob && threadIdx.x == 0 ? to_f32(((const T*)a.logits)[(long long)r * a.row_stride + a.tokens[r]]) : 0.f;
+}
+
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int r, Stat st, float chosen, const u64* top) {
     const float s = st.m == INFINITY ? __builtin_nanf("") : st.s, lz = log1pf(s);
     if (threadIdx.x == 0) {
-        if (a.logprob) {
-            const float x = to_f32(((const T*)a.logits)[(long long)r * a.row_stride + a.tokens[r]]);
-            a.logprob[r] = st.m == -INFINITY ? -INFINITY + s : (x - st.m) - lz;
-        }
+        if (a.logprob) a.logprob[r] = st.m == -INFINITY ? -INFINITY + s : (chosen - st.m) - lz;
         if (a.entropy) a.entropy[r] = lz - st.t / (1.f + s);
     }
     for (int i = threadIdx.x; i < a.top_n; i += LP_T) {
@@ -161,10 +165,11 @@ struct Part {
     int parts, tiles, per;                       // parts of a row, its tiles, tiles of a part
 };
 
-template <typename T>
+// ONE: parts of one tile, whose values stay in registers for the alternatives.
+template <typename T, bool ONE>
 __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
     constexpr int N = Row<T>::N, PER = Row<T>::PER;
-    __shared__ float s_group[TILES_MAX * LP_T];
+    __shared__ float s_group[ONE ? LP_T : TILES_MAX * LP_T];
     __shared__ u64 s_cand[CAND_CAP];
     __shared__ int s_list[GROUPS_CAP];
     __shared__ u64 s_top[TOP_MAX];
@@ -174,9 +179,8 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
     __shared__ int s_groups, s_cands;
     __shared__ float s_bound;
     const int part = blockIdx.x % pt.parts, r = blockIdx.x / pt.parts, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    if (!row_ok(a, r, part == 0)) return;
     const Row<T> row(a.logits, a.row_stride, r, a.vocab);
-    const int t0 = part * pt.per, t1 = min(pt.tiles, t0 + pt.per);
+    const int t0 = ONE ? part : part * pt.per, t1 = ONE ? t0 + 1 : min(pt.tiles, t0 + pt.per);
     float m = -INFINITY, s = 0.f, t = 0.f, mine = -INFINITY;
     uint4 next[PER];
     auto fetch = [&](int tile) {
@@ -189,16 +193,22 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
         }
     };
     fetch(t0);
+    // (after the first loads are on their way)
+    if (!row_ok(a, r, part == 0)) return;
+    float x1[ONE ? GROUP : 1];
     for (int tile = t0; tile < t1; ++tile) {
         float x[GROUP];
 #pragma unroll
         for (int i = 0; i < PER; ++i) Row<T>::values(next[i], x + i * N);
-        if (tile + 1 < t1) fetch(tile + 1);
+        if (!ONE && tile + 1 < t1) fetch(tile + 1);
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < GROUP; ++i) top = fmaxf(top, x[i]);
         s_group[(tile - t0) * LP_T + tid] = top;
         mine = fmaxf(mine, top);
+        if constexpr (ONE)
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) x1[i] = x[i];
         top = wave_max_dpp(top);
         if (top > m) {
             if (m > -INFINITY) {
@@ -217,9 +227,8 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
                 s += is ? 0.f : e;
                 t += e * fmaxf(d, LEAST);
             }
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) at_max += __shfl_xor(at_max, o, 64);
-            if (lane == 0) s += (float)(at_max - 1);
+            const float all_max = wave_sum_dpp((float)at_max);
+            if (lane == 0) s += all_max - 1.f;
         } else {
             const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
@@ -230,8 +239,9 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
             }
         }
     }
-    s = wave_sum(s);
-    t = wave_sum(t);
+    const float chosen = pt.parts == 1 ? chosen_logit<T>(a, r) : 0.f;
+    s = wave_sum_dpp(s);
+    t = wave_sum_dpp(t);
     if (lane == 0) s_stat[wave] = Stat{m, s, t};
     s_max[tid] = mine;
     if (tid == 0) s_groups = s_cands = 0;
@@ -259,26 +269,34 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
         }
         __syncthreads();
         const float bound = s_bound;
-        for (int g = tid; g < (t1 - t0) * LP_T; g += LP_T)
-            if (s_group[g] >= bound) {
-                const int i = atomicAdd(&s_groups, 1);
-                if (i < GROUPS_CAP) s_list[i] = g;
-            }
-        __syncthreads();
-        const int groups = s_groups;
-        if (groups <= GROUPS_CAP) {
-            for (int q = tid; q < groups * PER; q += LP_T) {
-                const int g = s_list[q / PER];
-                const int vec = ((t0 + g / LP_T) * PER + q % PER) * LP_T + g % LP_T;
-                float x[N];
-                row.load(vec, x);
+        auto push = [&](float y, int id) {
+            const int i = atomicAdd(&s_cands, 1);
+            if (i < CAND_CAP) s_cand[i] = token_key(y, id);
+        };
+        int groups = 0;
+        if constexpr (ONE) {
+            if (mine >= bound)
 #pragma unroll
-                for (int k = 0; k < N; ++k)
-                    if (x[k] >= bound) {
-                        const int i = atomicAdd(&s_cands, 1);
-                        if (i < CAND_CAP) s_cand[i] = token_key(x[k], vec * N - row.off + k);
-                    }
-            }
+                for (int k = 0; k < GROUP; ++k)
+                    if (x1[k] >= bound) push(x1[k], ((t0 * PER + k / N) * LP_T + tid) * N - row.off + k % N);
+        } else {
+            for (int g = tid; g < (t1 - t0) * LP_T; g += LP_T)
+                if (s_group[g] >= bound) {
+                    const int i = atomicAdd(&s_groups, 1);
+                    if (i < GROUPS_CAP) s_list[i] = g;
+                }
+            __syncthreads();
+            groups = s_groups;
+            if (groups <= GROUPS_CAP)
+                for (int q = tid; q < groups * PER; q += LP_T) {
+                    const int g = s_list[q / PER];
+                    const int vec = ((t0 + g / LP_T) * PER + q % PER) * LP_T + g % LP_T;
+                    float y[N];
+                    row.load(vec, y);
+#pragma unroll
+                    for (int k = 0; k < N; ++k)
+                        if (y[k] >= bound) push(y[k], vec * N - row.off + k);
+                }
         }
         __syncthreads();
         const int cands = s_cands;
@@ -298,12 +316,12 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
                     if (s_group[(tile - t0) * LP_T + tid] >= bound)
                         for (int v = 0; v < PER; ++v) {
                             const int vec = (tile * PER + v) * LP_T + tid;
-                            float x[N];
-                            row.load(vec, x);
+                            float y[N];
+                            row.load(vec, y);
 #pragma unroll
                             for (int k = 0; k < N; ++k)
-                                if (x[k] >= bound) {
-                                    const u64 key = token_key(x[k], vec * N - row.off + k);
+                                if (y[k] >= bound) {
+                                    const u64 key = token_key(y[k], vec * N - row.off + k);
                                     if (key < prev && key > best) best = key;
                                 }
                         }
@@ -321,7 +339,7 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
         }
     }
     if (pt.parts == 1) {
-        write_row<T>(a, r, st, s_top);
+        write_row(a, r, st, chosen, s_top);
         return;
     }
     const size_t at = (size_t)r * pt.parts + part;
@@ -337,6 +355,7 @@ __global__ __launch_bounds__(LP_T) void k_logprobs_join(LogprobArgs a, Part pt) 
     __shared__ u64 s_top[TOP_MAX];
     __shared__ u64 s_cand[CAND_CAP];
     __shared__ u64 s_low[4];
+    __shared__ Stat s_stat[4];
     __shared__ int s_cands;
     const int r = blockIdx.x, tid = threadIdx.x;
     if (!row_ok(a, r, false)) return;
@@ -346,10 +365,15 @@ __global__ __launch_bounds__(LP_T) void k_logprobs_join(LogprobArgs a, Part pt) 
     u64 mine[KEEP];
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) mine[i] = tid + i * LP_T < all ? top[tid + i * LP_T] : 0;
-    // (all threads hold the row's statistics; the parts in order)
+    const float chosen = chosen_logit<T>(a, r);
+    // the parts' statistics: a thread's in order, then a tree over the threads
     const Stat* stat = pt.stat + (size_t)r * pt.parts;
-    Stat st = stat[0];
-    for (int p = 1; p < pt.parts; ++p) st = join(st, stat[p]);
+    Stat st{-INFINITY, 0.f, 0.f};
+    for (int p = tid; p < pt.parts; p += LP_T) st = join(st, stat[p]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1)
+        st = join(st, Stat{__shfl_xor(st.m, o, 64), __shfl_xor(st.s, o, 64), __shfl_xor(st.t, o, 64)});
+    if ((tid & 63) == 0) s_stat[tid >> 6] = st;
     if (tid < TOP_MAX) s_top[tid] = 0;
     if (tid == 0) s_cands = 0;
     if (n > 0) {
@@ -393,7 +417,10 @@ __global__ __launch_bounds__(LP_T) void k_logprobs_join(LogprobArgs a, Part pt) 
         }
     }
     __syncthreads();
-    write_row<T>(a, r, st, s_top);
+    st = s_stat[0];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) st = join(st, s_stat[w]);
+    write_row(a, r, st, chosen, s_top);
 }
 
 constexpr int LP_GROUPS = 512;      // work-groups wanted
@@ -419,8 +446,10 @@ size_t logprob_ws_bytes(int rows, int vocab, int top_n) {
 hipError_t launch_logprobs(int dtype, const LogprobArgs& a, hipStream_t st) {
     const Part p = plan(a.rows, a.vocab, a.top_n, a.ws);
     const dim3 grid((unsigned)a.rows * p.parts);
-    if (dtype == PBD_DTYPE_BF16) PBD_LAUNCH((k_logprobs<bf16>), grid, dim3(LP_T), 0, st, a, p);
-    else PBD_LAUNCH((k_logprobs<float>), grid, dim3(LP_T), 0, st, a, p);
+    if (dtype == PBD_DTYPE_BF16 && p.per == 1) PBD_LAUNCH((k_logprobs<bf16, true>), grid, dim3(LP_T), 0, st, a, p);
+    else if (dtype == PBD_DTYPE_BF16) PBD_LAUNCH((k_logprobs<bf16, false>), grid, dim3(LP_T), 0, st, a, p);
+    else if (p.per == 1) PBD_LAUNCH((k_logprobs<float, true>), grid, dim3(LP_T), 0, st, a, p);
+    else PBD_LAUNCH((k_logprobs<float, false>), grid, dim3(LP_T), 0, st, a, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
     if (dtype == PBD_DTYPE_BF16) PBD_LAUNCH((k_logprobs_join<bf16>), dim3(a.rows), dim3(LP_T), 0, st, a, p);

@@ -26,8 +26,13 @@ int hip_result(hipError_t e, const char* what) {
     return op_fail(PBD_ERR_HIP, msg);
 }
 
-size_t evict_count_offset(const pbd_pages& p, int batch, int max_len) {
+// Workspace of an eviction: the moves, the blocks' first ones, the counts.
+size_t evict_blocks_offset(const pbd_pages& p, int batch, int max_len) {
     return up256((size_t)batch * p.n_kv_heads * paged_evict_list(max_len) * 2 * sizeof(int));
+}
+size_t evict_count_offset(const pbd_pages& p, int batch, int max_len) {
+    return evict_blocks_offset(p, batch, max_len) +
+           up256((size_t)batch * p.n_kv_heads * paged_evict_blocks(max_len) * sizeof(int));
 }
 
 // The cache's description with a bound on the slots a call uses (0: none given).
@@ -168,6 +173,8 @@ int pbd_paged_evict(const pbd_pages* pages, int32_t batch, const int32_t* lens, 
     a.lens = lens; a.keep = keep; a.pos = pos; a.score_out = score_out; a.slot_pos_out = slot_pos_out;
     a.new_lens = new_lens;
     a.moves = (int*)ws; a.list = (int)paged_evict_list(max_len);
+    a.block_first = (int*)((char*)ws + evict_blocks_offset(*pages, batch, max_len));
+    a.blocks = (int)paged_evict_blocks(max_len);
     a.count = (int*)((char*)ws + evict_count_offset(*pages, batch, max_len));
     return hip_result(launch_paged_evict(pages->dtype, pages->head_dim, a, batch, (hipStream_t)stream), "evict");
 }

@@ -92,8 +92,11 @@ struct PagedEvictArgs {
     int* moves;                 // workspace: [B][n_kv][list] (destination, source) pairs
     int list;                   // pairs per list
     int* count;                 // [B][n_kv] pairs, then [B] new lengths (-1: skipped)
+    int* block_first;           // [B][n_kv][blocks] the first pair that goes to each 16-slot block, then their number
+    int blocks;
 };
-size_t paged_evict_list(int max_len);   // pairs a list holds
+size_t paged_evict_list(int max_len);     // pairs a list holds
+size_t paged_evict_blocks(int max_len);   // entries of block_first
 hipError_t launch_paged_evict(int dtype, int head_dim, const PagedEvictArgs& a, int batch, hipStream_t st);
 
 struct LogprobArgs {
