@@ -31,28 +31,39 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Exclusive prefix of v over the work-group's waves (v: one value per wave);
-// every thread of wave w gets the sum over waves < w.
-__device__ __forceinline__ int waves_before(int v, int* s, int wave, int lane) {
-    __syncthreads();
-    if (lane == 0) s[wave] = v;
-    __syncthreads();
-    int x = 0;
-    for (int w = 0; w < wave; ++w) x += s[w];
-    return x;
+// Inclusive sum over the lanes below and this one (DPP: inside the 16-lane rows, then
+// across them).
+__device__ __forceinline__ int wave_scan(int v) {
+#define PBD_STEP(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false)
+    PBD_STEP(0x111, 0xF);    // row_shr:1
+    PBD_STEP(0x112, 0xF);    // row_shr:2
+    PBD_STEP(0x114, 0xF);    // row_shr:4
+    PBD_STEP(0x118, 0xF);    // row_shr:8
+    PBD_STEP(0x142, 0xA);    // row_bcast:15 into rows 1 and 3
+    PBD_STEP(0x143, 0xC);    // row_bcast:31 into rows 2 and 3
+#undef PBD_STEP
+    return v;
+}
+
+// Set bits of a lane mask below this lane.
+__device__ __forceinline__ int bits_below(unsigned long long m) {
+    return __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
 }
 
 // Which slots stay, and the list of moves.  One work-group per KV head and
 // sequence: the K-th largest key by three counting passes over its bits (11, 11
-// and 10), then each wave walks its run of slots in order, so that equal keys,
-// evicted slots and moving slots get their ranks in ascending order.  The keys
-// are read once and stay in registers, KEYS groups of 64 slots a wave (KEYS 0:
-// longer caches, whose keys every walk reads again).
-template <int KEYS>
+// and 10), then each wave counts and writes its run of slots in order, so that
+// equal keys, evicted slots and moving slots get their ranks in ascending order.
+// The keys are read once and stay in registers, KEYS groups of 64 slots a wave
+// (KEYS 0: longer caches, whose keys every walk reads again).  Accumulated
+// weights crowd a few exponents, so that a wave's lanes would queue at one bin:
+// each bin has COPIES counters, a lane's by its number.
+template <int KEYS, int COPIES>
 __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
-    __shared__ unsigned s_hist[BINS];
-    __shared__ int s_w[SEL_W];
-    __shared__ unsigned s_bin, s_above;
+    __shared__ __align__(16) unsigned s_hist[BINS * COPIES];
+    __shared__ int s_w[3][SEL_W];
+    __shared__ unsigned s_bin[3], s_above[3];
+    __shared__ int4 s_run[SEL_W];
     const int h = blockIdx.x, b = blockIdx.y;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int len = a.lens[b], want = a.keep[b];
@@ -67,29 +78,42 @@ __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
     // each wave's run of 64-slot groups: lane's slot of group j, its key
     const int groups = bad ? 0 : (len + 63) / 64, per = (groups + SEL_W - 1) / SEL_W;
     const int first = wave * per * 64 + lane;
+    auto make_key = [&](float s, int p) -> unsigned { return p >= last || p < a.sink ? STAYS : score_key(s); };
     auto read_key = [&](int i) -> unsigned {
         if (i >= len) return 0u;
-        const float s = score[i];
-        if (slot_pos) {
-            const int p = slot_pos[i];
-            if (p >= last || p < a.sink) return STAYS;
-        }
-        return score_key(s);
+        return slot_pos ? make_key(score[i], slot_pos[i]) : score_key(score[i]);
     };
     unsigned reg[KEYS > 0 ? KEYS : 1];
     if constexpr (KEYS > 0) {
+        // STEP groups' loads out at a time, of slots that exist (past the last one: the last)
+        constexpr int STEP = KEYS < 8 ? KEYS : 8;
 #pragma unroll
-        for (int j = 0; j < KEYS; ++j) {
-            reg[j] = j < per ? read_key(first + j * 64) : 0u;
-            if (j % 8 == 7) __builtin_amdgcn_sched_barrier(0);    // eight groups' loads at a time
+        for (int j0 = 0; j0 < KEYS; j0 += STEP) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (j0 >= per) break;
+            float s[STEP];
+            int p[STEP];
+#pragma unroll
+            for (int j = 0; j < STEP; ++j) s[j] = score[min(first + (j0 + j) * 64, len - 1)];
+            if (slot_pos) {
+#pragma unroll
+                for (int j = 0; j < STEP; ++j) p[j] = slot_pos[min(first + (j0 + j) * 64, len - 1)];
+#pragma unroll
+                for (int j = 0; j < STEP; ++j) reg[j0 + j] = make_key(s[j], p[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < STEP; ++j) reg[j0 + j] = score_key(s[j]);
+            }
         }
     }
     // f(slot, key, whether the slot exists) for this lane's slots, ascending
     auto walk = [&](auto f) {
         if constexpr (KEYS > 0) {
+            int i = first;
+            asm volatile("" : "+v"(i));             // (the slots' numbers are not kept from walk to walk)
 #pragma unroll
             for (int j = 0; j < KEYS; ++j)
-                if (j < per) f(first + j * 64, reg[j], first + j * 64 < len);
+                if (j < per) f(i + j * 64, reg[j], i + j * 64 < len);
         } else {
             for (int j = 0; j < per; ++j) f(first + j * 64, read_key(first + j * 64), first + j * 64 < len);
         }
@@ -116,81 +140,93 @@ __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
     if (tid == 0 && h == 0) *new_len = K;
     int* moves = a.moves + ((size_t)b * a.n_kv + h) * a.list * 2;
     int* block_first = a.block_first + ((size_t)b * a.n_kv + h) * a.blocks;
-    float* so = a.score_out + at;
-    int* po = slot_pos ? a.slot_pos_out + at : nullptr;
     if (K == 0 || K == len) {
         if (tid == 0) *count = 0;
-        if (so != score)
-            for (int i = tid; i < K; i += SEL_T) so[i] = score[i];
-        if (po && po != slot_pos)
-            for (int i = tid; i < K; i += SEL_T) po[i] = slot_pos[i];
         return;
     }
     // the K-th largest key T; `need` of the keys equal to it stay
     unsigned T = 0;
     int need = K;
+    for (int i = tid; i < BINS * COPIES / 4; i += SEL_T) ((uint4*)s_hist)[i] = uint4{0u, 0u, 0u, 0u};
+    __syncthreads();
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : BINS;
         const int top = pass == 0 ? 32 : pass == 1 ? 21 : 10;    // bits below the ones already fixed
-        for (int i = tid; i < BINS; i += SEL_T) s_hist[i] = 0;
-        __syncthreads();
         walk([&](int, unsigned u, bool in) {
-            if (in && (pass == 0 || u >> top == T >> top)) atomicAdd(&s_hist[u >> shift & (bins - 1)], 1u);
+            if (in && (pass == 0 || u >> top == T >> top))
+                atomicAdd(&s_hist[(u >> shift & (bins - 1)) * COPIES + (lane & (COPIES - 1))], 1u);
         });
         __syncthreads();
-        // two bins a thread, from the highest down
+        // two bins a thread, from the highest down; cleared for the next pass
         const int b0 = BINS - 1 - 2 * tid;
-        const int c0 = s_hist[b0], c1 = s_hist[b0 - 1];
-        int x = c0 + c1;
+        typedef unsigned __attribute__((ext_vector_type(COPIES))) copies;
+        copies* own = (copies*)(s_hist + (b0 - 1) * COPIES);
+        int c[2] = {0, 0};
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int y = __shfl_up(x, o, 64);
-            if (lane >= o) x += y;
+        for (int i = 0; i < 2; ++i) {
+            const copies x = own[i];
+            own[i] = copies(0u);
+#pragma unroll
+            for (int k = 0; k < COPIES; ++k) c[1 - i] += x[k];
         }
-        const int before = waves_before(__shfl(x, 63, 64), s_w, wave, lane) + x - c0 - c1;
-        if (before < need && before + c0 >= need) {
-            s_bin = b0;
-            s_above = before;
-        } else if (before + c0 < need && before + c0 + c1 >= need) {
-            s_bin = b0 - 1;
-            s_above = before + c0;
+        const int x = wave_scan(c[0] + c[1]);
+        if (lane == 63) s_w[pass][wave] = x;
+        __syncthreads();
+        // (lanes 0 .. 15 hold the waves' totals; the last lane of the row their sum)
+        const int w = lane < wave ? s_w[pass][lane & 15] : 0;
+        const int before = x - c[0] - c[1] + __builtin_amdgcn_readlane(wave_scan(w), 15);
+        if (before < need && before + c[0] >= need) {
+            s_bin[pass] = b0;
+            s_above[pass] = before;
+        } else if (before + c[0] < need && before + c[0] + c[1] >= need) {
+            s_bin[pass] = b0 - 1;
+            s_above[pass] = before + c[0];
         }
         __syncthreads();
-        T |= s_bin << shift;
-        need -= s_above;
-        __syncthreads();
+        T |= s_bin[pass] << shift;
+        need -= s_above[pass];
     }
-    const unsigned long long below = (1ull << lane) - 1;
-    int ties = 0;
-    walk([&](int, unsigned u, bool in) { ties += __popcll(__ballot(in && u == T)); });
-    const int tie0 = waves_before(ties, s_w, wave, lane);
-    // evicted and moving slots: counted for the ranks that each run begins with, then written
-    int tie = tie0, holes = 0, movers = 0;
+    // of each wave's run: the slots that stay for certain, below the new length and
+    // past it, and those with the key T, of which the first `need` of all stay
+    int4 run{0, 0, 0, 0};
     walk([&](int i, unsigned u, bool in) {
-        const unsigned long long eq = __ballot(in && u == T);
-        const bool stays = in && (u > T || (u == T && tie + __popcll(eq & below) < need));
-        tie += __popcll(eq);
-        holes += __popcll(__ballot(i < K && !stays));
-        movers += __popcll(__ballot(i >= K && stays));
+        const int i0 = i - lane;                    // the group's first slot: most groups lie on one side
+        if (i0 < K) {
+            run.x += __popcll(__ballot(i < K && u > T));
+            run.y += __popcll(__ballot(i < K && u == T));
+        }
+        if (i0 + 64 > K) {
+            run.z += __popcll(__ballot(in && i >= K && u > T));
+            run.w += __popcll(__ballot(in && i >= K && u == T));
+        }
     });
-    int hole = waves_before(holes, s_w, wave, lane), mover = waves_before(movers, s_w, wave, lane);
-    tie = tie0;
+    if (lane == 0) s_run[wave] = run;
+    __syncthreads();
+    int tie = 0, hole = 0, mover = 0;
+    for (int w = 0; w < wave; ++w) {
+        const int4 r = s_run[w];
+        const int low = min(max(need - tie, 0), r.y), high = min(max(need - tie - r.y, 0), r.w);
+        tie += r.y + r.w;
+        hole += min(max(K - w * per * 64, 0), per * 64) - r.x - low;
+        mover += r.z + high;
+    }
     walk([&](int i, unsigned u, bool in) {
         const unsigned long long eq = __ballot(in && u == T);
-        const bool stays = in && (u > T || (u == T && tie + __popcll(eq & below) < need));
+        const bool stays = in && (u > T || (u == T && tie + bits_below(eq) < need));
         tie += __popcll(eq);
-        const unsigned long long hm = __ballot(i < K && !stays), mm = __ballot(i >= K && stays);
-        const int rank = hole + __popcll(hm & below);
-        if (i < K && (i & 15) == 0) block_first[i >> 4] = rank;
-        if (i < K && !stays) moves[2 * rank] = i;
-        if (i >= K && stays) moves[2 * (mover + __popcll(mm & below)) + 1] = i;
-        hole += __popcll(hm);
-        mover += __popcll(mm);
-        // what stays is copied here, what moves with its K and V
-        if (i < K && stays) {
-            if (so != score) so[i] = score[i];
-            if (po && po != slot_pos) po[i] = slot_pos[i];
+        const int i0 = i - lane;
+        if (i0 < K) {
+            const unsigned long long m = __ballot(i < K && !stays);
+            const int rank = hole + bits_below(m);
+            if (i < K && (i & 15) == 0) block_first[i >> 4] = rank;
+            if (i < K && !stays) moves[2 * rank] = i;
+            hole += __popcll(m);
+        }
+        if (i0 + 64 > K) {
+            const unsigned long long m = __ballot(i >= K && stays);
+            if (i >= K && stays) moves[2 * (mover + bits_below(m)) + 1] = i;
+            mover += __popcll(m);
         }
     });
     if (tid == SEL_T - 1) {                     // the last wave ends at the total
@@ -199,13 +235,13 @@ __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
     }
 }
 
-// The moves, by the block they go to: a wave takes blocks of 16 slots, whose lines
+// The moves, by the block they go to: a wave takes one of 16 slots, whose lines
 // no other wave writes.  A lane's K piece (16 bytes of one slot) comes from the
 // slot's own place or from the slot that moves in; a V run (4 slots of one dim)
 // is put together from up to four.  The block is read and written whole where
 // WHOLE slots or more of it are replaced (its lines are touched anyway, and a
 // line written whole need not be read back for the bytes between).
-constexpr int MOVE_WAVES = 4, MOVE_BLOCKS = 4, WHOLE = 3;
+constexpr int MOVE_WAVES = 4, WHOLE = 3;
 
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_evict_move(PagedEvictArgs a) {
@@ -215,78 +251,84 @@ __global__ __launch_bounds__(256) void k_evict_move(PagedEvictArgs a) {
     __shared__ int s_slot[MOVE_WAVES][16];          // its slot there; -1: slot i keeps its own
     const int h = blockIdx.y, b = blockIdx.z, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int l16 = lane & 15, g = lane >> 4;
+    const int blk = blockIdx.x * MOVE_WAVES + wave;
     const int K = a.count[(size_t)gridDim.z * a.n_kv + b];
+    const int moved = a.count[(size_t)b * a.n_kv + h];
     if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0 && K >= 0) a.new_lens[b] = K;
-    if (a.count[(size_t)b * a.n_kv + h] == 0) return;
+    if (blk * 16 >= K) return;
     const int* moves = a.moves + ((size_t)b * a.n_kv + h) * a.list * 2;
-    const int* block_first = a.block_first + ((size_t)b * a.n_kv + h) * a.blocks;
+    const int* block_first = a.block_first + ((size_t)b * a.n_kv + h) * a.blocks + blk;
     const int* tab = a.pg.table + (size_t)b * a.pg.table_width;
     const long long at = ((long long)b * a.n_kv + h) * a.pg.slot_stride;
-    auto block = [&](int blk) -> long long {
-        return (long long)tab[blk >> a.pg.page_shift] * a.pg.page_stride + (long long)h * a.pg.head_stride +
-               (long long)(blk & ((1 << a.pg.page_shift) - 1)) * (16 * HD);
+    auto block = [&](int i) -> long long {
+        return (long long)tab[i >> a.pg.page_shift] * a.pg.page_stride + (long long)h * a.pg.head_stride +
+               (long long)(i & ((1 << a.pg.page_shift) - 1)) * (16 * HD);
     };
-    const int n_blk = (K + 15) >> 4;
-    const int blk0 = (blockIdx.x * MOVE_WAVES + wave) * MOVE_BLOCKS;
-    for (int blk = blk0; blk < min(n_blk, blk0 + MOVE_BLOCKS); ++blk) {
-        const int r0 = block_first[blk], n = block_first[blk + 1] - r0;
-        if (n == 0) continue;
-        wave_sync();
-        if (lane < 16) s_slot[wave][lane] = -1;
-        wave_sync();
-        if (lane < n) {
-            const int2 mv = *(const int2*)(moves + 2 * (r0 + lane));
-            s_from[wave][mv.x & 15] = block(mv.y >> 4);
-            s_slot[wave][mv.x & 15] = mv.y & 15;
-            a.score_out[at + mv.x] = a.pg.score[at + mv.y];
-            if (a.slot_pos_out) a.slot_pos_out[at + mv.x] = a.pg.slot_pos[at + mv.y];
-        }
-        wave_sync();
-        const bool whole = n >= WHOLE;
-        const long long d = block(blk);
-        {
-            const int from = s_slot[wave][l16];
-            const T* src = (const T*)a.pg.k + (from < 0 ? d + l16 * EPL : s_from[wave][l16] + from * EPL);
-            T* dst = (T*)a.pg.k + d + l16 * EPL;
-            if (whole || from >= 0) {
-                constexpr int STEP = NK > 4 ? 4 : NK;
+    const long long d = block(blk);
+    int n = 0, r0 = 0;
+    if (moved > 0) {
+        r0 = block_first[0];
+        n = block_first[1] - r0;
+    }
+    if (lane < 16) s_slot[wave][lane] = -1;
+    wave_sync();
+    if (lane < n) {
+        const int2 mv = *(const int2*)(moves + 2 * (r0 + lane));
+        s_from[wave][mv.x & 15] = block(mv.y >> 4);
+        s_slot[wave][mv.x & 15] = mv.y & 15;
+        a.score_out[at + mv.x] = a.pg.score[at + mv.y];
+        if (a.slot_pos_out) a.slot_pos_out[at + mv.x] = a.pg.slot_pos[at + mv.y];
+    }
+    wave_sync();
+    if (lane < 16 && blk * 16 + lane < K && s_slot[wave][lane] < 0) {
+        const long long i = at + blk * 16 + lane;
+        if (a.score_out != a.pg.score) a.score_out[i] = a.pg.score[i];
+        if (a.slot_pos_out && a.slot_pos_out != a.pg.slot_pos) a.slot_pos_out[i] = a.pg.slot_pos[i];
+    }
+    if (n == 0) return;
+    const bool whole = n >= WHOLE;
+    {
+        const int from = s_slot[wave][l16];
+        const T* src = (const T*)a.pg.k + (from < 0 ? d + l16 * EPL : s_from[wave][l16] + from * EPL);
+        T* dst = (T*)a.pg.k + d + l16 * EPL;
+        if (whole || from >= 0) {
+            constexpr int STEP = NK > 4 ? 4 : NK;
 #pragma unroll
-                for (int i0 = 0; i0 < NK; i0 += STEP) {
-                    uint4 x[STEP];
+            for (int i0 = 0; i0 < NK; i0 += STEP) {
+                uint4 x[STEP];
 #pragma unroll
-                    for (int i = 0; i < STEP; ++i) x[i] = *(const uint4*)(src + ((i0 + i) * 4 + g) * 16 * EPL);
+                for (int i = 0; i < STEP; ++i) x[i] = *(const uint4*)(src + ((i0 + i) * 4 + g) * 16 * EPL);
 #pragma unroll
-                    for (int i = 0; i < STEP; ++i) *(uint4*)(dst + ((i0 + i) * 4 + g) * 16 * EPL) = x[i];
-                }
+                for (int i = 0; i < STEP; ++i) *(uint4*)(dst + ((i0 + i) * 4 + g) * 16 * EPL) = x[i];
             }
         }
-        {
-            int from[4];
-            const T* src[4];
-            bool some = false;
+    }
+    {
+        int from[4];
+        const T* src[4];
+        bool some = false;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                from[e] = s_slot[wave][4 * g + e];
-                some |= from[e] >= 0;
-                src[e] = (const T*)a.pg.v + s_from[wave][4 * g + e] + vblock_elem(from[e] & 15, l16);
-            }
-            T* dst = (T*)a.pg.v + d + lane * 4;
-            if (whole || some) {
-                constexpr int STEP = NT * sizeof(T) > 16 ? NT / 2 : NT;       // tiles whose loads are out together
+        for (int e = 0; e < 4; ++e) {
+            from[e] = s_slot[wave][4 * g + e];
+            some |= from[e] >= 0;
+            src[e] = (const T*)a.pg.v + s_from[wave][4 * g + e] + vblock_elem(from[e] & 15, l16);
+        }
+        T* dst = (T*)a.pg.v + d + lane * 4;
+        if (whole || some) {
+            constexpr int STEP = NT * sizeof(T) > 16 ? NT / 2 : NT;       // tiles whose loads are out together
 #pragma unroll
-                for (int i0 = 0; i0 < NT; i0 += STEP) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    t4 x[STEP];
+            for (int i0 = 0; i0 < NT; i0 += STEP) {
+                __builtin_amdgcn_sched_barrier(0);
+                t4 x[STEP];
 #pragma unroll
-                    for (int i = 0; i < STEP; ++i) x[i] = *(const t4*)(dst + (i0 + i) * 256);
+                for (int i = 0; i < STEP; ++i) x[i] = *(const t4*)(dst + (i0 + i) * 256);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (from[e] >= 0)
+                for (int e = 0; e < 4; ++e)
+                    if (from[e] >= 0)
 #pragma unroll
-                            for (int i = 0; i < STEP; ++i) x[i][e] = src[e][(i0 + i) * 256];
+                        for (int i = 0; i < STEP; ++i) x[i][e] = src[e][(i0 + i) * 256];
 #pragma unroll
-                    for (int i = 0; i < STEP; ++i) *(t4*)(dst + (i0 + i) * 256) = x[i];
-                }
+                for (int i = 0; i < STEP; ++i) *(t4*)(dst + (i0 + i) * 256) = x[i];
             }
         }
     }
@@ -299,15 +341,14 @@ size_t paged_evict_blocks(int max_len) { return ((size_t)max_len + 15) / 16 + 1;
 
 hipError_t launch_paged_evict(int dtype, int head_dim, const PagedEvictArgs& a, int batch, hipStream_t st) {
     const dim3 sel(a.n_kv, batch);
-    if (a.max_len <= 2 * SEL_T) PBD_LAUNCH((k_evict_select<2>), sel, dim3(SEL_T), 0, st, a);
-    else if (a.max_len <= 8 * SEL_T) PBD_LAUNCH((k_evict_select<8>), sel, dim3(SEL_T), 0, st, a);
-    else if (a.max_len <= 24 * SEL_T) PBD_LAUNCH((k_evict_select<24>), sel, dim3(SEL_T), 0, st, a);
-    else if (a.max_len <= 40 * SEL_T) PBD_LAUNCH((k_evict_select<40>), sel, dim3(SEL_T), 0, st, a);
-    else PBD_LAUNCH((k_evict_select<0>), sel, dim3(SEL_T), 0, st, a);
+    if (a.max_len <= 2 * SEL_T) PBD_LAUNCH((k_evict_select<2, 1>), sel, dim3(SEL_T), 0, st, a);
+    else if (a.max_len <= 8 * SEL_T) PBD_LAUNCH((k_evict_select<8, 4>), sel, dim3(SEL_T), 0, st, a);
+    else if (a.max_len <= 24 * SEL_T) PBD_LAUNCH((k_evict_select<24, 4>), sel, dim3(SEL_T), 0, st, a);
+    else if (a.max_len <= 64 * SEL_T) PBD_LAUNCH((k_evict_select<64, 4>), sel, dim3(SEL_T), 0, st, a);
+    else PBD_LAUNCH((k_evict_select<0, 4>), sel, dim3(SEL_T), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int per = MOVE_WAVES * MOVE_BLOCKS;
-    const dim3 grid((a.blocks - 1 + per - 1) / per, a.n_kv, batch);
+    const dim3 grid((a.blocks - 1 + MOVE_WAVES - 1) / MOVE_WAVES, a.n_kv, batch);
     if (dtype == PBD_DTYPE_BF16 && head_dim == 128) PBD_LAUNCH((k_evict_move<bf16, 128>), grid, dim3(256), 0, st, a);
     else if (dtype == PBD_DTYPE_BF16) PBD_LAUNCH((k_evict_move<bf16, 64>), grid, dim3(256), 0, st, a);
     else if (head_dim == 128) PBD_LAUNCH((k_evict_move<float, 128>), grid, dim3(256), 0, st, a);
