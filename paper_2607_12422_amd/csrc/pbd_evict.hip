@@ -299,7 +299,7 @@ __global__ __launch_bounds__(256) void k_evict_move(PagedEvictArgs a) {
 #pragma unroll
                 for (int i = 0; i < STEP; ++i) x[i] = *(const uint4*)(src + ((i0 + i) * 4 + g) * 16 * EPL);
 #pragma unroll
-                for (int i = 0; i < STEP; ++i) *(uint4*)(dst + ((i0 + i) * 4 + g) * 16 * EPL) = x[i];
+                for (int i = 0; i < STEP; ++i) store_once(dst + ((i0 + i) * 4 + g) * 16 * EPL, x[i]);
             }
         }
     }
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(256) void k_evict_move(PagedEvictArgs a) {
 #pragma unroll
                         for (int i = 0; i < STEP; ++i) x[i][e] = src[e][(i0 + i) * 256];
 #pragma unroll
-                for (int i = 0; i < STEP; ++i) *(t4*)(dst + (i0 + i) * 256) = x[i];
+                for (int i = 0; i < STEP; ++i) store_once(dst + (i0 + i) * 256, x[i]);
             }
         }
     }

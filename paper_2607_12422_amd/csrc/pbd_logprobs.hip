@@ -83,7 +83,7 @@ struct Row {
         off = (int)(((size_t)p & 15) / sizeof(T));
     }
     // vector i, all of it in the row
-    __device__ __forceinline__ uint4 whole(int i) const { return *(const uint4*)(p + ((long long)i * N - off)); }
+    __device__ __forceinline__ uint4 whole(int i) const { return load_once<uint4>(p + ((long long)i * N - off)); }
     // vector i; -inf outside the row, of which nothing is read
     __device__ __forceinline__ uint4 any(int i) const {
         const int id = i * N - off;
@@ -165,7 +165,7 @@ struct Part {
     int parts, tiles, per;                       // parts of a row, its tiles, tiles of a part
 };
 
-// ONE: parts of one tile, whose values stay in registers for the alternatives.
+// ONE: parts of one tile, whose values are still in registers for the alternatives.
 template <typename T, bool ONE>
 __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
     constexpr int N = Row<T>::N, PER = Row<T>::PER;
@@ -195,7 +195,6 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
     fetch(t0);
     // (after the first loads are on their way)
     if (!row_ok(a, r, part == 0)) return;
-    float x1[ONE ? GROUP : 1];
     for (int tile = t0; tile < t1; ++tile) {
         float x[GROUP];
 #pragma unroll
@@ -206,10 +205,8 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
         for (int i = 0; i < GROUP; ++i) top = fmaxf(top, x[i]);
         s_group[(tile - t0) * LP_T + tid] = top;
         mine = fmaxf(mine, top);
-        if constexpr (ONE)
-#pragma unroll
-            for (int i = 0; i < GROUP; ++i) x1[i] = x[i];
-        top = wave_max_dpp(top);
+        // (the same in every lane: a scalar, so that the branch is one)
+        top = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(wave_max_dpp(top))));
         if (top > m) {
             if (m > -INFINITY) {
                 // lane 0 has the instance of the old maximum that the sum leaves out
@@ -218,25 +215,22 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
                 s = f * all;
             }
             m = top;
+            // the new one's instances add 1 each, but for one: out of the sums below
             int at_max = 0;
 #pragma unroll
             for (int i = 0; i < GROUP; ++i) {
-                const float d = x[i] - m, e = exp_neg(d);
                 const bool is = x[i] == m;
-                at_max += is;
-                s += is ? 0.f : e;
-                t += e * fmaxf(d, LEAST);
+                at_max += __popcll(__ballot(is));
+                x[i] = is ? -INFINITY : x[i];
             }
-            const float all_max = wave_sum_dpp((float)at_max);
-            if (lane == 0) s += all_max - 1.f;
-        } else {
-            const float ref = m == -INFINITY ? 0.f : m;
+            if (lane == 0) s += (float)(at_max - 1);
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-            for (int i = 0; i < GROUP; ++i) {
-                const float d = x[i] - ref, e = exp_neg(d);
-                s += e;
-                t += e * fmaxf(d, LEAST);
-            }
+        for (int i = 0; i < GROUP; ++i) {
+            const float d = x[i] - ref, e = exp_neg(d);
+            s += e;
+            t += e * fmaxf(d, LEAST);
         }
     }
     const float chosen = pt.parts == 1 ? chosen_logit<T>(a, r) : 0.f;
@@ -275,10 +269,20 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
         };
         int groups = 0;
         if constexpr (ONE) {
-            if (mine >= bound)
+            // few threads have such values: their places first, then the values again
+            unsigned found = 0;
 #pragma unroll
-                for (int k = 0; k < GROUP; ++k)
-                    if (x1[k] >= bound) push(x1[k], ((t0 * PER + k / N) * LP_T + tid) * N - row.off + k % N);
+            for (int i = 0; i < PER; ++i) {
+                float y[N];
+                Row<T>::values(next[i], y);
+#pragma unroll
+                for (int k = 0; k < N; ++k) found |= (y[k] >= bound ? 1u : 0u) << (i * N + k);
+            }
+            while (found) {
+                const int k = __ffs(found) - 1, id = ((t0 * PER + k / N) * LP_T + tid) * N - row.off + k % N;
+                found &= found - 1;
+                push(to_f32(row.p[id]), id);
+            }
         } else {
             for (int g = tid; g < (t1 - t0) * LP_T; g += LP_T)
                 if (s_group[g] >= bound) {

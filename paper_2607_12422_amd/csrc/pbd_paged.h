@@ -12,6 +12,25 @@
 
 namespace pbd {
 
+// A load of data that the kernel reads once: kept out of the caches' way.
+template <typename V>
+__device__ __forceinline__ V load_once(const void* p) {
+    typedef unsigned __attribute__((ext_vector_type(sizeof(V) / 4))) words;
+    const words w = __builtin_nontemporal_load((const words*)p);
+    V v;
+    __builtin_memcpy(&v, &w, sizeof v);
+    return v;
+}
+
+// A store of data that no later access of the kernel touches.
+template <typename V>
+__device__ __forceinline__ void store_once(void* p, const V& v) {
+    typedef unsigned __attribute__((ext_vector_type(sizeof(V) / 4))) words;
+    words w;
+    __builtin_memcpy(&w, &v, sizeof v);
+    __builtin_nontemporal_store(w, (words*)p);
+}
+
 // One layer's paged cache as the kernels address it.
 struct PageView {
     int page_shift;             // log2 of the 16-slot blocks of a page
