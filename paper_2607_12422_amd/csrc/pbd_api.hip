@@ -594,7 +594,8 @@ int run_pass(pbd_ctx* c, const PassReq& q, hipStream_t st) {
         at.raw = pg.score ? (float*)(pp.ws + pp.plan.off_raw) : nullptr;
         at.MT = MT; at.op_f16 = h16 ? 1 : 0; at.op_hi = hi(y.w_xo); at.op_lo = lo(y.w_xo);
         PBD_TIMED(c, st, PBD_KCLASS_ATTN, launch_paged_attn_splits(dt, y.HD, at, B, st), "attention");
-        PBD_TIMED(c, st, PBD_KCLASS_COMBINE, launch_paged_attn_join(dt, y.HD, at, B, st), "attention join");
+        if (!pp.plan.direct)
+            PBD_TIMED(c, st, PBD_KCLASS_COMBINE, launch_paged_attn_join(dt, y.HD, at, B, st), "attention join");
         return PBD_OK;
     };
     // with the adapter, the large-M projection is two launches (timed

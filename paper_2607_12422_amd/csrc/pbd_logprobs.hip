@@ -10,13 +10,15 @@
 //
 // The top n cost the pass nothing but a store: per thread and tile (32 elements)
 // the maximum is kept in LDS.  At most n - 1 elements exceed the n-th largest,
-// so the n-th largest of the 256 threads' maxima is a lower bound of it, and the
-// groups that reach the bound (about n of some thousands) are read again, the
-// elements that reach it ranked by (value, lower id).  Where too many reach it
+// so the n-th largest of 64 maxima of disjoint parts is a lower bound of it, and
+// the groups that reach the bound (about 1.2 n of some thousands) are read again,
+// the elements that reach it ranked by (value, lower id).  Where too many reach it
 // (masses of equal logits) the row is scanned n times instead.
 #include "pbd_device.h"
 #include "pbd_launch.h"
 #include "pbd_paged.h"
+
+#include <float.h>
 
 #include <algorithm>
 
@@ -130,10 +132,9 @@ __device__ __forceinline__ u64 wave_max64(u64 v) {
     return v;
 }
 
-// Whether row r takes part (the same answer in every thread); first: reports.
-__device__ __forceinline__ bool row_ok(const LogprobArgs& a, int r, bool first) {
-    if (!a.tokens) return true;
-    const int t = a.tokens[r];
+// Whether the row of token t (0 without tokens) takes part, the same answer in every
+// thread; first: reports.
+__device__ __forceinline__ bool row_ok(const LogprobArgs& a, int t, bool first) {
     if (t >= 0 && t < a.vocab) return true;
     if (t != -1 && first && threadIdx.x == 0 && a.status) atomicOr(a.status, PBD_STATUS_TOKEN);
     return false;
@@ -141,8 +142,8 @@ __device__ __forceinline__ bool row_ok(const LogprobArgs& a, int r, bool first) 
 
 // The logit of the row's token, for thread 0.
 template <typename T>
-__device__ __forceinline__ float chosen_logit(const LogprobArgs& a, int r) {
-    return a.logprob && threadIdx.x == 0 ? to_f32(((const T*)a.logits)[(long long)r * a.row_stride + a.tokens[r]]) : 0.f;
+__device__ __forceinline__ float chosen_logit(const LogprobArgs& a, int r, int t) {
+    return a.logprob && threadIdx.x == 0 ? to_f32(((const T*)a.logits)[(long long)r * a.row_stride + t]) : 0.f;
 }
 
 __device__ __forceinline__ void write_row(const LogprobArgs& a, int r, Stat st, float chosen, const u64* top) {
@@ -176,8 +177,8 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
     __shared__ Stat s_stat[4];
     __shared__ u64 s_red[4];
     __shared__ float s_max[LP_T];
+    __shared__ __align__(16) float s_sup[4][64];
     __shared__ int s_groups, s_cands;
-    __shared__ float s_bound;
     const int part = blockIdx.x % pt.parts, r = blockIdx.x / pt.parts, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const Row<T> row(a.logits, a.row_stride, r, a.vocab);
     const int t0 = ONE ? part : part * pt.per, t1 = ONE ? t0 + 1 : min(pt.tiles, t0 + pt.per);
@@ -192,9 +193,11 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
             for (int i = 0; i < PER; ++i) next[i] = row.any((tile * PER + i) * LP_T + tid);
         }
     };
+    const int token = a.tokens ? a.tokens[r] : 0;
     fetch(t0);
     // (after the first loads are on their way)
-    if (!row_ok(a, r, part == 0)) return;
+    if (!row_ok(a, token, part == 0)) return;
+    const float chosen = pt.parts == 1 ? chosen_logit<T>(a, r, token) : 0.f;
     for (int tile = t0; tile < t1; ++tile) {
         float x[GROUP];
 #pragma unroll
@@ -233,7 +236,6 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
             t += e * fmaxf(d, LEAST);
         }
     }
-    const float chosen = pt.parts == 1 ? chosen_logit<T>(a, r) : 0.f;
     s = wave_sum_dpp(s);
     t = wave_sum_dpp(t);
     if (lane == 0) s_stat[wave] = Stat{m, s, t};
@@ -246,23 +248,24 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
     for (int w = 1; w < 4; ++w) st = join(st, s_stat[w]);
     const int n = a.top_n;
     if (n > 0) {
-        if (wave == 0) {
-            // the n-th largest of the threads' maxima, bit by bit from the top
-            unsigned k[4], bound = 0;
+        // the n-th largest of 64 maxima, each of four threads (every wave for itself): the
+        // one that fewer than n exceed and at least n reach
+        float own = s_max[lane];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) k[i] = value_key(s_max[lane + 64 * i]);
-            for (int bit = 31; bit >= 0; --bit) {
-                const unsigned c = bound | 1u << bit;
-                int cnt = 0;
+        for (int w = 1; w < 4; ++w) own = fmaxf(own, s_max[lane + 64 * w]);
+        s_sup[wave][lane] = own;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        int above = 0, reach = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) cnt += __popcll(__ballot(k[i] >= c));
-                if (cnt >= n) bound = c;
-            }
-            // (fewer than n threads with anything unmasked: everything unmasked)
-            if (lane == 0) s_bound = key_value(max(bound, value_key(-INFINITY) + 1u));
+        for (int i = 0; i < 16; ++i) {
+            const float4 o = *(const float4*)&s_sup[wave][4 * i];
+            above += (o.x > own) + (o.y > own) + (o.z > own) + (o.w > own);
+            reach += (o.x >= own) + (o.y >= own) + (o.z >= own) + (o.w >= own);
         }
-        __syncthreads();
-        const float bound = s_bound;
+        const unsigned long long hit = __ballot(above < n && reach >= n);
+        const float nth = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(own), __ffsll(hit) - 1));
+        // (nothing unmasked in some of them: everything unmasked)
+        const float bound = fmaxf(nth, -FLT_MAX);
         auto push = [&](float y, int id) {
             const int i = atomicAdd(&s_cands, 1);
             if (i < CAND_CAP) s_cand[i] = token_key(y, id);
@@ -362,18 +365,22 @@ __global__ __launch_bounds__(LP_T) void k_logprobs_join(LogprobArgs a, Part pt) 
     __shared__ Stat s_stat[4];
     __shared__ int s_cands;
     const int r = blockIdx.x, tid = threadIdx.x;
-    if (!row_ok(a, r, false)) return;
     const int n = a.top_n, all = pt.parts * n;
     const u64* top = pt.top + (size_t)r * all;
+    const Stat* stat = pt.stat + (size_t)r * pt.parts;
+    // every load that needs no other one's answer, before any is used (of a skipped row
+    // nothing was written, and nothing read here is used)
+    const int token = a.tokens ? a.tokens[r] : 0;
     constexpr int KEEP = 2;
-    u64 mine[KEEP];
+    u64 mine[KEEP], low = ~0ull;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) mine[i] = tid + i * LP_T < all ? top[tid + i * LP_T] : 0;
-    const float chosen = chosen_logit<T>(a, r);
+    Stat st = tid < pt.parts ? stat[tid] : Stat{-INFINITY, 0.f, 0.f};
+    if (n > 0 && tid < pt.parts) low = top[tid * n + (n + pt.parts - 1) / pt.parts - 1];
+    if (!row_ok(a, token, false)) return;
+    const float chosen = chosen_logit<T>(a, r, token);
     // the parts' statistics: a thread's in order, then a tree over the threads
-    const Stat* stat = pt.stat + (size_t)r * pt.parts;
-    Stat st{-INFINITY, 0.f, 0.f};
-    for (int p = tid; p < pt.parts; p += LP_T) st = join(st, stat[p]);
+    for (int p = tid + LP_T; p < pt.parts; p += LP_T) st = join(st, stat[p]);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1)
         st = join(st, Stat{__shfl_xor(st.m, o, 64), __shfl_xor(st.s, o, 64), __shfl_xor(st.t, o, 64)});
@@ -382,8 +389,7 @@ __global__ __launch_bounds__(LP_T) void k_logprobs_join(LogprobArgs a, Part pt) 
     if (tid == 0) s_cands = 0;
     if (n > 0) {
         const int j = (n + pt.parts - 1) / pt.parts;
-        u64 low = ~0ull;
-        for (int p = tid; p < pt.parts; p += LP_T) {
+        for (int p = tid + LP_T; p < pt.parts; p += LP_T) {
             const u64 k = top[p * n + j - 1];
             low = k < low ? k : low;
         }

@@ -72,6 +72,7 @@ struct PagedAttnPlan {
     int tiles;                  // tiles of 16 query heads per KV head
     int kps;                    // slots per split
     int splits;                 // splits of max_len slots
+    bool direct;                // one split and no weights kept: it writes the output, no join
     int len_pad;                // slots per row of the kept raw scores
     size_t off_ml, off_raw, bytes;   // workspace: partial outputs first
 };
@@ -95,7 +96,7 @@ struct PagedAttnArgs {
     void* op_hi;
     void* op_lo;
 };
-// the splits' partial sums, then their join
+// the splits' partial sums, then their join (nothing to do where the plan is direct)
 hipError_t launch_paged_attn_splits(int dtype, int head_dim, const PagedAttnArgs& a, int batch, hipStream_t st);
 hipError_t launch_paged_attn_join(int dtype, int head_dim, const PagedAttnArgs& a, int batch, hipStream_t st);
 

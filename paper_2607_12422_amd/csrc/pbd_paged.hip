@@ -208,6 +208,28 @@ __device__ __forceinline__ unsigned high_halves(float a, float b) {
     return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 
+// Four dims (from d on) of a query head's output: its weighted sum over the sum of
+// its weights, and the head's log sum (by d = 0); none: a sequence of no slots.
+template <typename T, int HD>
+__device__ __forceinline__ void finish(const PagedAttnArgs& a, int b, int h, int d, f32x4 acc, float M, float L, bool none) {
+    acc *= none ? 0.f : 1.f / L;
+    if (a.out) *(f32x4*)(a.out + ((size_t)b * a.n_q + h) * HD + d) = acc;
+    if (a.lse && d == 0)
+        a.lse[(size_t)b * a.n_q + h] = none ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f;
+    if (a.op_hi) {
+        // the O projection's operand (row b, k = h HD + dim): four dims of a lane's run
+        const size_t e = xfrag_elem<T>(b, h * HD + d, a.MT);
+        if (sizeof(T) == 2 && a.op_f16) {
+            _Float16* hi = (_Float16*)a.op_hi;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) hi[e + i] = (_Float16)acc[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put_operand((T*)a.op_hi, (T*)a.op_lo, e + i, acc[i]);
+        }
+    }
+}
+
 constexpr int ATT_WAVES = 4;
 
 template <typename T, int HD>
@@ -225,7 +247,19 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(PagedAttnArgs a) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
     const int len = a.lens[b];
     const int beg = split * a.plan.kps;
-    // (a length out of range is reported by the join)
+    if (a.plan.direct) {
+        // no join follows: invalid and empty sequences end here
+        if (len < 0 || len > a.max_len) {
+            if (blockIdx.y == 0 && threadIdx.x == 0) raise(a.pg.status, PBD_STATUS_CAPACITY);
+            return;
+        }
+        if (len == 0) {
+            for (int i = threadIdx.x; i < nq * (HD / 4); i += 256)
+                finish<T, HD>(a, b, hq0 + i / (HD / 4), i % (HD / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, 0.f, 0.f, true);
+            return;
+        }
+    }
+    // (otherwise the join reports a length out of range)
     if (len > a.max_len || beg >= len) return;
     const int end = min(len, beg + a.plan.kps);
     const int blk0 = beg >> 4, blk_last = (end - 1) >> 4;
@@ -404,6 +438,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(PagedAttnArgs a) {
             L += f * s_l[w][q];
             acc += *(const f32x4*)&s_o[w][q][d] * f;
         }
+        if (a.plan.direct) {
+            if (!any_bad) finish<T, HD>(a, b, hq0 + q, d, acc, M, L, false);
+            continue;
+        }
         const size_t row = ((size_t)b * a.n_q + hq0 + q) * a.plan.splits + split;
         *(f32x4*)(a.part_o + row * HD + d) = acc;
         if (d == 0) {
@@ -509,23 +547,7 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a) {
     acc = s_o[0][d];
 #pragma unroll
     for (int i = 1; i < GROUPS; ++i) acc += s_o[i][d];
-    const float inv = n == 0 ? 0.f : 1.f / L;
-    acc *= inv;
-    if (a.out) *(f32x4*)(a.out + ((size_t)b * a.n_q + h) * HD + 4 * d) = acc;
-    if (a.lse && d == 0)
-        a.lse[(size_t)b * a.n_q + h] = n == 0 ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f;
-    if (a.op_hi) {
-        // the O projection's operand (row b, k = h HD + dim): four dims of a lane's run
-        const size_t e = xfrag_elem<T>(b, h * HD + 4 * d, a.MT);
-        if (sizeof(T) == 2 && a.op_f16) {
-            _Float16* hi = (_Float16*)a.op_hi;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) hi[e + i] = (_Float16)acc[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) put_operand((T*)a.op_hi, (T*)a.op_lo, e + i, acc[i]);
-        }
-    }
+    finish<T, HD>(a, b, h, 4 * d, acc, M, L, n == 0);
 }
 
 // ---------------------------------------------------------------------------
@@ -599,6 +621,11 @@ hipError_t launch_paged_append(int dtype, int head_dim, const PagedAppendArgs& a
 
 constexpr int KPS_MAX = 4096;     // a wave's lanes hold the addresses of 64 blocks: 4 waves, 16 slots each
 constexpr int ATT_GROUPS = 1024;  // work-groups wanted
+// Slots up to which one work-group takes a whole sequence and no join follows
+// (captured: 16 / 8 heads of 128 in bf16, 384 slots 7.0 us against 8.0 split, 512
+// slots 8.0 and 8.0, 768 9.9 and 8.1; 4 / 2 heads of 64 in fp32, 128 slots 4.6 and
+// 6.5, 384 8.2 and 6.8, but called one by one 7.0 and 9.0: a launch less).
+constexpr int DIRECT_LEN = 384;
 
 PagedAttnPlan paged_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int max_len, bool scored) {
     PagedAttnPlan p{};
@@ -607,13 +634,16 @@ PagedAttnPlan paged_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int ba
     const long long all = (long long)batch * n_kv * p.tiles * max_len;
     const long long kps = std::min<long long>(KPS_MAX, (all + ATT_GROUPS - 1) / ATT_GROUPS);
     p.kps = (int)std::max<long long>(step, (kps + step - 1) / step * step);
+    if (!scored && max_len <= DIRECT_LEN) p.kps = DIRECT_LEN;
     p.splits = (max_len + p.kps - 1) / p.kps;
+    p.direct = p.splits == 1 && !scored;
     p.len_pad = (max_len + 15) / 16 * 16;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    const size_t rows = (size_t)batch * n_q * p.splits;
+    const size_t rows = p.direct ? 0 : (size_t)batch * n_q * p.splits;
     p.off_ml = up(rows * head_dim * 4);
     p.off_raw = p.off_ml + up(rows * 2 * 4);
     p.bytes = p.off_raw + (scored ? up((size_t)batch * n_q * p.len_pad * 4) : 0);
+    if (p.bytes == 0) p.bytes = 256;                               // (a size of 0 says invalid)
     return p;
 }
 
@@ -632,6 +662,7 @@ hipError_t launch_paged_attn_splits(int dtype, int head_dim, const PagedAttnArgs
 
 hipError_t launch_paged_attn_join(int dtype, int head_dim, const PagedAttnArgs& a, int batch, hipStream_t st) {
     const int chunks = a.raw ? (a.max_len + SCORE_SLOTS - 1) / SCORE_SLOTS : 0;
+    if (a.plan.direct) return hipSuccess;
     PBD_BY_TYPE(k_paged_join, dim3(a.n_q + chunks * a.n_kv, batch));
 }
 #undef PBD_BY_TYPE
