@@ -233,11 +233,12 @@ __device__ __forceinline__ void finish(const PagedAttnArgs& a, int b, int h, int
 constexpr int ATT_WAVES = 4;
 
 template <typename T, int HD>
-__global__ __launch_bounds__(256, 2) void k_paged_attn(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, 3) void k_paged_attn(PagedAttnArgs a) {
     typedef AttnShape<T, HD> SH;
     constexpr int NB = SH::NB, ND = HD / Elt<T>::FK, NT = HD / 16, EPL = Elt<T>::EPL;
     constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
     constexpr int LDO = HD + 4;
+    __shared__ uint4 s_q[TERMS][ND][64];             // the query tile as the B operand
     __shared__ float s_o[ATT_WAVES][16][LDO];
     __shared__ float s_m[ATT_WAVES][16], s_l[ATT_WAVES][16];
     __shared__ int s_bad;
@@ -266,13 +267,11 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(PagedAttnArgs a) {
     const int steps = (blk_last - blk0 + NB) / NB;
     const int mine = wave < steps ? (steps - wave + ATT_WAVES - 1) / ATT_WAVES : 0;
     if (threadIdx.x == 0) s_bad = 0;
-    __syncthreads();
     // lane i: the address of block i % NB of this wave's step i / NB (past the
     // last one: the last, whose slots are masked)
     const int my_blk = min(blk0 + (wave + ATT_WAVES * (lane / NB)) * NB + lane % NB, blk_last);
     const int id = a.pg.table[(size_t)b * a.pg.table_width + (my_blk >> a.pg.page_shift)];
     const bool bad = id < 0 || id >= a.pg.n_pages;
-    if (bad) s_bad = 1;
     const long long off = block_offset(a.pg, bad ? 0 : id, my_blk, kvh, 16 * HD) * (long long)sizeof(T);
     const int off_lo = (int)(off & 0xffffffffll), off_hi = (int)(off >> 32);
     auto at = [&](int i) -> size_t {
@@ -301,10 +300,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(PagedAttnArgs a) {
         load_k(0);
         load_v(0);
     }
-    // the query tile as the B operand: column = head, this lane's EPL dims per fragment
-    uint4 qf[TERMS][ND];
-#pragma unroll
-    for (int d = 0; d < ND; ++d) {
+    // the query tile as the B operand: column = head, a lane's EPL dims per fragment;
+    // in LDS, whence every wave takes it each step: in registers it cost a third of
+    // the waves that a CU has room for
+    for (int d = wave; d < ND; d += ATT_WAVES) {
         float x[EPL];
         const float* src = a.q + (size_t)b * a.q_stride + (size_t)(hq0 + min(col, nq - 1)) * HD + d * Elt<T>::FK + g * EPL;
 #pragma unroll
@@ -322,9 +321,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(PagedAttnArgs a) {
                 e[i] = from_f32<T>(x[i]);
                 x[i] -= to_f32(e[i]);
             }
-            __builtin_memcpy(&qf[t][d], e, 16);
+            uint4 f;
+            __builtin_memcpy(&f, e, 16);
+            s_q[t][d][lane] = f;
         }
     }
+    lds_sync();
+    if (bad) s_bad = 1;
     float m = -INFINITY, l = 0.f;
     f32x4 o[NT];
 #pragma unroll
@@ -338,10 +341,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(PagedAttnArgs a) {
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int c = 0; c < NB; ++c) {
-                mma_frag<T>(sc[c], kf[c][d], qf[0][d]);
+                mma_frag<T>(sc[c], kf[c][d], s_q[0][d][lane]);
                 if constexpr (TERMS == 3) {
-                    mma_frag<T>(lo[c], kf[c][d], qf[1][d]);
-                    mma_frag<T>(lo[c], kf[c][d], qf[2][d]);
+                    mma_frag<T>(lo[c], kf[c][d], s_q[1][d][lane]);
+                    mma_frag<T>(lo[c], kf[c][d], s_q[2][d][lane]);
                 }
             }
         mfma_settle();
