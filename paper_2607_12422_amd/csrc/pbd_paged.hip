@@ -25,13 +25,14 @@ __device__ __forceinline__ long long block_offset(const PageView& pg, int id, in
 }
 
 // ---------------------------------------------------------------------------
-// Append.  16 lanes hold one row of one head (RowPrep: norm and rotation stay
-// in the lanes).  MANY rows a call: a work-group takes the 16 slots of one block
-// and one head, so that K leaves in runs of 16 bytes per slot next to each other
-// and V, whose layout runs along the slots, is turned in LDS and leaves in the
-// 4-slot groups of the layout.  Few rows: the 16 lane groups take 16 heads of one
-// row (a 16-slot work-group would idle 15 of its groups), and V leaves element
-// by element.
+// Append.  16 lanes hold one row of one head (the norm and the rotation stay in the
+// lanes).  k_paged_append_rows: a work-group takes the 16 slots of one block and
+// several heads, whose rows are all requested before the first is used and share
+// the rotation; K leaves in runs of 16 bytes per slot next to each other, and V,
+// whose layout runs along the slots, is turned in LDS and leaves in the layout's
+// 4-slot groups.  k_paged_append_few: the 16 lane groups take 16 heads of one row
+// (15 of a 16-slot work-group's would idle), and V leaves element by element.
+// Both move rows x (Hq (8) + Hkv (8 + 2 esz)) x head_dim bytes, and no more.
 // ---------------------------------------------------------------------------
 
 // Whether sequence b's append is valid, the same answer in every work-group;
@@ -52,98 +53,146 @@ __device__ __forceinline__ bool append_ok(const PagedAppendArgs& a, int b, int l
     return !bad;
 }
 
-template <typename T, int HD, bool MANY>
-__global__ __launch_bounds__(256) void k_paged_append(PagedAppendArgs a) {
+// A row of one head in 16 lanes: lane l16 has dims NP l16 .. + NP of both halves.
+template <int HD>
+struct HeadRow {
+    static constexpr int NP = HD / 32, HALF = HD / 2;
+    typedef float __attribute__((ext_vector_type(NP))) fv;
+    typedef float __attribute__((ext_vector_type(2 * NP))) fv2;
+    fv lo, hi;
+    __device__ __forceinline__ void load(const float* row, int l16) {
+        lo = *(const fv*)(row + NP * l16);
+        hi = *(const fv*)(row + HALF + NP * l16);
+    }
+    __device__ __forceinline__ void store(float* row, int l16) const {
+        *(fv*)(row + NP * l16) = lo;
+        *(fv*)(row + HALF + NP * l16) = hi;
+    }
+    __device__ __forceinline__ void norm(const fv& g_lo, const fv& g_hi, float eps) {
+        float ss = 0.f;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) ss += lo[p] * lo[p] + hi[p] * hi[p];
+        const float r = rsqrtf(row16_sum(ss) / (float)HD + eps);
+        lo = lo * r * g_lo;
+        hi = hi * r * g_hi;
+    }
+    __device__ __forceinline__ void turn(const fv2& cs) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const float a = lo[p], b = hi[p], c = cs[2 * p], s = cs[2 * p + 1];
+            lo[p] = a * c - b * s;
+            hi[p] = b * c + a * s;
+        }
+    }
+};
+
+template <typename T, int HD>
+__device__ __forceinline__ void load_gain(const void* gain, int l16, typename HeadRow<HD>::fv& lo,
+                                          typename HeadRow<HD>::fv& hi) {
+    constexpr int NP = HD / 32;
+    typedef T __attribute__((ext_vector_type(NP))) tv;
+    const tv a = *(const tv*)((const T*)gain + NP * l16), b = *(const tv*)((const T*)gain + HD / 2 + NP * l16);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        lo[p] = to_f32(a[p]);
+        hi[p] = to_f32(b[p]);
+    }
+}
+
+// K of one slot into its block.
+template <typename T, int HD>
+__device__ __forceinline__ void store_key(T* blk, int key, int l16, const HeadRow<HD>& x) {
     constexpr int NP = HD / 32, HALF = HD / 2;
     typedef T __attribute__((ext_vector_type(NP))) tv;
+    tv lo, hi;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        lo[p] = from_f32<T>(x.lo[p]);
+        hi[p] = from_f32<T>(x.hi[p]);
+    }
+    *(tv*)(blk + kblock_elem<T>(key, NP * l16)) = lo;
+    *(tv*)(blk + kblock_elem<T>(key, HALF + NP * l16)) = hi;
+}
+
+constexpr int KV_HEADS = 2, Q_HEADS = 4;         // heads of a work-group of k_paged_append_rows
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_paged_append_rows(PagedAppendArgs a) {
+    typedef HeadRow<HD> Row;
+    constexpr int NP = Row::NP, HALF = HD / 2, LDV = HD + 8;
+    __shared__ T s_v[KV_HEADS][16 * LDV];
     const int b = blockIdx.z, l16 = threadIdx.x & 15, grp = threadIdx.x >> 4;
     const int len = a.lens[b], n = a.n_new ? a.n_new[b] : a.max_new, pos = a.pos[b];
     const bool first = blockIdx.x == 0 && blockIdx.y == 0;
     if (!append_ok(a, b, len, n, pos, first)) return;
     if (first && threadIdx.x == 0 && a.lens_out) a.lens_out[b] = len + n;
-    // this lane group's row and head (heads: KV first, then queries)
-    int row, head;
-    if (MANY) {
-        row = (int)((len >> 4) + blockIdx.x) * 16 + grp - len;
-        head = blockIdx.y;
-    } else {
-        row = blockIdx.x;
-        head = blockIdx.y * 16 + grp;
+    const int s0 = ((len >> 4) + (int)blockIdx.x) * 16;      // the block's first slot
+    if (s0 >= len + n) return;
+    const int slot = s0 + grp, row = slot - len;
+    const bool live = row >= 0 && row < n;
+    const int safe = live ? row : max(0, min(row, n - 1));   // (n > 0 here or nothing is live)
+    const size_t r = ((size_t)b * a.max_new + (n > 0 ? safe : 0)) * a.row_stride;
+    const int kv_groups = (a.n_kv + KV_HEADS - 1) / KV_HEADS;
+    typename Row::fv2 cs;
+    if (live) cs = *(const typename Row::fv2*)(a.rope + (size_t)(pos + row) * HALF + NP * l16);
+    typename Row::fv g_lo, g_hi;
+    if ((int)blockIdx.y >= kv_groups) {
+        const int h0 = ((int)blockIdx.y - kv_groups) * Q_HEADS;
+        Row x[Q_HEADS];
+        if (!live) return;
+#pragma unroll
+        for (int i = 0; i < Q_HEADS; ++i) x[i].load(a.q + r + (size_t)min(h0 + i, a.n_q - 1) * HD, l16);
+        if (a.q_norm) load_gain<T, HD>(a.q_norm, l16, g_lo, g_hi);
+#pragma unroll
+        for (int i = 0; i < Q_HEADS; ++i) {
+            if (a.q_norm) x[i].norm(g_lo, g_hi, a.eps);
+            x[i].turn(cs);
+            if (h0 + i < a.n_q) x[i].store(a.q_out + (((size_t)b * a.max_new + row) * a.n_q + h0 + i) * HD, l16);
+        }
+        return;
     }
-    const int heads = a.n_kv + (a.q ? a.n_q : 0);
-    const bool live = row >= 0 && row < n && head < heads;
-    const int slot = len + row;
-    const bool kv = head < a.n_kv;
-    const size_t r = ((size_t)b * a.max_new + (live ? row : 0)) * a.row_stride;
-    const float2* rope = a.rope + (size_t)(pos + (live ? row : 0)) * HALF;
-    T* vblk = nullptr;
-    __shared__ T s_v[MANY ? 16 * (HD + 8) : 1];
-    if (live && !kv) {
-        const int h = head - a.n_kv;
-        RowPrep<float, HD> rp;
-        Gains<T, HD> gn;
-        float gl[NP], gh[NP], lo[NP], hi[NP];
-        rp.load(a.q + r + (size_t)h * HD, rope, l16);
-        if (a.q_norm) gn.load(a.q_norm, l16);
-        gn.get(a.q_norm != nullptr, gl, gh);
-        rp.values(true, gl, gh, a.q_norm != nullptr, a.eps, lo, hi);
-        typedef float __attribute__((ext_vector_type(NP))) fv;
-        float* dst = a.q_out + (((size_t)b * a.max_new + row) * a.n_q + h) * HD + NP * l16;
-        fv x, y;
+    const int h0 = blockIdx.y * KV_HEADS, blk = s0 >> 4;
+    const int id = a.pg.table[(size_t)b * a.pg.table_width + (blk >> a.pg.page_shift)];
+    if (live) {
+        Row x[KV_HEADS], v[KV_HEADS];
 #pragma unroll
-        for (int p = 0; p < NP; ++p) { x[p] = lo[p]; y[p] = hi[p]; }
-        *(fv*)dst = x;
-        *(fv*)(dst + HALF) = y;
-    }
-    if (live && kv) {
-        const int blk = slot >> 4, key = slot & 15;
-        const int id = a.pg.table[(size_t)b * a.pg.table_width + (blk >> a.pg.page_shift)];
-        const long long off = block_offset(a.pg, id, blk, head, 16 * HD);
-        T* kblk = (T*)a.pg.k + off;
-        vblk = (T*)a.pg.v + off;
-        RowPrep<float, HD> rp;
-        Gains<T, HD> gn;
-        float gl[NP], gh[NP], lo[NP], hi[NP];
-        rp.load(a.k + r + (size_t)head * HD, rope, l16);
-        if (a.k_norm) gn.load(a.k_norm, l16);
-        typedef float __attribute__((ext_vector_type(NP))) fv;
-        const float* vs = a.v + r + (size_t)head * HD + NP * l16;
-        const fv v0 = *(const fv*)vs, v1 = *(const fv*)(vs + HALF);
-        gn.get(a.k_norm != nullptr, gl, gh);
-        rp.values(true, gl, gh, a.k_norm != nullptr, a.eps, lo, hi);
-        tv x, y;
+        for (int i = 0; i < KV_HEADS; ++i) {
+            const size_t at = r + (size_t)min(h0 + i, a.n_kv - 1) * HD;
+            x[i].load(a.k + at, l16);
+            v[i].load(a.v + at, l16);
+        }
+        if (a.k_norm) load_gain<T, HD>(a.k_norm, l16, g_lo, g_hi);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) { x[p] = from_f32<T>(lo[p]); y[p] = from_f32<T>(hi[p]); }
-        *(tv*)(kblk + kblock_elem<T>(key, NP * l16)) = x;
-        *(tv*)(kblk + kblock_elem<T>(key, HALF + NP * l16)) = y;
+        for (int i = 0; i < KV_HEADS; ++i) {
+            if (h0 + i >= a.n_kv) break;
+            if (a.k_norm) x[i].norm(g_lo, g_hi, a.eps);
+            x[i].turn(cs);
+            store_key<T, HD>((T*)a.pg.k + block_offset(a.pg, id, blk, h0 + i, 16 * HD), grp, l16, x[i]);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            const T e0 = from_f32<T>(v0[p]), e1 = from_f32<T>(v1[p]);
-            if (MANY) {
-                s_v[key * (HD + 8) + NP * l16 + p] = e0;
-                s_v[key * (HD + 8) + HALF + NP * l16 + p] = e1;
-            } else {
-                vblk[vblock_elem(key, NP * l16 + p)] = e0;
-                vblk[vblock_elem(key, HALF + NP * l16 + p)] = e1;
+            for (int p = 0; p < NP; ++p) {
+                s_v[i][grp * LDV + NP * l16 + p] = from_f32<T>(v[i].lo[p]);
+                s_v[i][grp * LDV + HALF + NP * l16 + p] = from_f32<T>(v[i].hi[p]);
             }
         }
-        if (l16 == 0) {
-            const size_t at = ((size_t)b * a.n_kv + head) * a.pg.slot_stride + slot;
+    }
+    if (threadIdx.x < 16 * KV_HEADS) {
+        // the slots' state, 16 to a head
+        const int i = threadIdx.x >> 4, s = s0 + (threadIdx.x & 15);
+        if (h0 + i < a.n_kv && s >= len && s < len + n) {
+            const size_t at = ((size_t)b * a.n_kv + h0 + i) * a.pg.slot_stride + s;
             if (a.pg.score) a.pg.score[at] = 0.f;
-            if (a.pg.slot_pos) a.pg.slot_pos[at] = pos + row;
+            if (a.pg.slot_pos) a.pg.slot_pos[at] = pos + s - len;
         }
     }
-    if (MANY && kv) {
-        // one head and block per work-group: every group's page is the same
-        __syncthreads();
-        const int s0 = ((len >> 4) + (int)blockIdx.x) * 16;      // the block's first slot
-        if (s0 >= len + n) return;
-        const int blk = s0 >> 4;
-        const int id = a.pg.table[(size_t)b * a.pg.table_width + (blk >> a.pg.page_shift)];
-        T* dst = (T*)a.pg.v + block_offset(a.pg, id, blk, head, 16 * HD);
-        for (int i = threadIdx.x; i < HD * 4; i += 256) {
-            // run i of the block: dims i / 64 * 16 + i % 16, slots 4 g .. 4 g + 3
-            const int dim = i / 64 * 16 + i % 16, g = i / 16 % 4;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < KV_HEADS; ++i) {
+        if (h0 + i >= a.n_kv) break;
+        T* dst = (T*)a.pg.v + block_offset(a.pg, id, blk, h0 + i, 16 * HD);
+#pragma unroll
+        for (int u = threadIdx.x; u < HD * 4; u += 256) {
+            // run u of the block: dim u / 64 * 16 + u % 16, slots 4 g .. 4 g + 3
+            const int dim = u / 64 * 16 + u % 16, g = u / 16 % 4;
             typedef T __attribute__((ext_vector_type(4))) t4;
             t4 x;
             bool in[4];
@@ -151,17 +200,62 @@ __global__ __launch_bounds__(256) void k_paged_append(PagedAppendArgs a) {
             for (int e = 0; e < 4; ++e) {
                 const int s = s0 + 4 * g + e;
                 in[e] = s >= len && s < len + n;
-                if (in[e]) x[e] = s_v[(4 * g + e) * (HD + 8) + dim];
-                else x[e] = from_f32<T>(0.f);
+                x[e] = in[e] ? s_v[i][(4 * g + e) * LDV + dim] : from_f32<T>(0.f);
             }
             if (in[0] && in[3]) {                    // the live slots are one run
-                *(t4*)(dst + (size_t)i * 4) = x;
+                *(t4*)(dst + (size_t)u * 4) = x;
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (in[e]) dst[(size_t)i * 4 + e] = x[e];
+                    if (in[e]) dst[(size_t)u * 4 + e] = x[e];
             }
         }
+    }
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_paged_append_few(PagedAppendArgs a) {
+    typedef HeadRow<HD> Row;
+    constexpr int NP = Row::NP, HALF = HD / 2;
+    const int b = blockIdx.z, l16 = threadIdx.x & 15, row = blockIdx.x;
+    const int len = a.lens[b], n = a.n_new ? a.n_new[b] : a.max_new, pos = a.pos[b];
+    const bool first = blockIdx.x == 0 && blockIdx.y == 0;
+    if (!append_ok(a, b, len, n, pos, first)) return;
+    if (first && threadIdx.x == 0 && a.lens_out) a.lens_out[b] = len + n;
+    const int head = blockIdx.y * 16 + (threadIdx.x >> 4);   // KV heads first, then queries
+    const bool kv = head < a.n_kv;
+    if (row >= n || head >= a.n_kv + (a.q ? a.n_q : 0)) return;
+    const size_t r = ((size_t)b * a.max_new + row) * a.row_stride;
+    const typename Row::fv2 cs = *(const typename Row::fv2*)(a.rope + (size_t)(pos + row) * HALF + NP * l16);
+    const void* gain = kv ? a.k_norm : a.q_norm;
+    const int h = kv ? head : head - a.n_kv;
+    Row x, v;
+    x.load((kv ? a.k : a.q) + r + (size_t)h * HD, l16);
+    if (kv) v.load(a.v + r + (size_t)h * HD, l16);
+    if (gain) {
+        typename Row::fv g_lo, g_hi;
+        load_gain<T, HD>(gain, l16, g_lo, g_hi);
+        x.norm(g_lo, g_hi, a.eps);
+    }
+    x.turn(cs);
+    if (!kv) {
+        x.store(a.q_out + (((size_t)b * a.max_new + row) * a.n_q + h) * HD, l16);
+        return;
+    }
+    const int slot = len + row, blk = slot >> 4, key = slot & 15;
+    const int id = a.pg.table[(size_t)b * a.pg.table_width + (blk >> a.pg.page_shift)];
+    const long long off = block_offset(a.pg, id, blk, h, 16 * HD);
+    store_key<T, HD>((T*)a.pg.k + off, key, l16, x);
+    T* dst = (T*)a.pg.v + off;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        dst[vblock_elem(key, NP * l16 + p)] = from_f32<T>(v.lo[p]);
+        dst[vblock_elem(key, HALF + NP * l16 + p)] = from_f32<T>(v.hi[p]);
+    }
+    if (l16 == 0) {
+        const size_t at = ((size_t)b * a.n_kv + h) * a.pg.slot_stride + slot;
+        if (a.pg.score) a.pg.score[at] = 0.f;
+        if (a.pg.slot_pos) a.pg.slot_pos[at] = pos + row;
     }
 }
 
@@ -605,21 +699,21 @@ PageView page_view(const pbd_pages& p) {
 
 constexpr int FEW_ROWS = 8;       // rows per sequence below which a work-group takes heads instead of slots
 
+#define PBD_BY_TYPE(KERNEL, GRID)                                                                           \
+    do {                                                                                                    \
+        if (dtype == PBD_DTYPE_BF16 && head_dim == 128) PBD_LAUNCH((KERNEL<bf16, 128>), GRID, dim3(256), 0, st, a); \
+        else if (dtype == PBD_DTYPE_BF16) PBD_LAUNCH((KERNEL<bf16, 64>), GRID, dim3(256), 0, st, a);        \
+        else if (head_dim == 128) PBD_LAUNCH((KERNEL<float, 128>), GRID, dim3(256), 0, st, a);              \
+        else PBD_LAUNCH((KERNEL<float, 64>), GRID, dim3(256), 0, st, a);                                    \
+        return hipGetLastError();                                                                           \
+    } while (0)
+
 hipError_t launch_paged_append(int dtype, int head_dim, const PagedAppendArgs& a, int batch, hipStream_t st) {
     const int heads = a.n_kv + (a.q ? a.n_q : 0);
-    const bool many = a.max_new >= FEW_ROWS;
-    const dim3 grid = many ? dim3((a.max_new + 14) / 16 + 1, heads, batch) : dim3(std::max(1, a.max_new), (heads + 15) / 16, batch);
-#define PBD_APPEND(T, HD)                                                                     \
-    do {                                                                                      \
-        if (many) PBD_LAUNCH((k_paged_append<T, HD, true>), grid, dim3(256), 0, st, a);       \
-        else PBD_LAUNCH((k_paged_append<T, HD, false>), grid, dim3(256), 0, st, a);           \
-        return hipGetLastError();                                                             \
-    } while (0)
-    if (dtype == PBD_DTYPE_BF16 && head_dim == 128) PBD_APPEND(bf16, 128);
-    if (dtype == PBD_DTYPE_BF16) PBD_APPEND(bf16, 64);
-    if (head_dim == 128) PBD_APPEND(float, 128);
-    PBD_APPEND(float, 64);
-#undef PBD_APPEND
+    if (a.max_new < FEW_ROWS)
+        PBD_BY_TYPE(k_paged_append_few, dim3(std::max(1, a.max_new), (heads + 15) / 16, batch));
+    const int groups = (a.n_kv + KV_HEADS - 1) / KV_HEADS + (a.q ? (a.n_q + Q_HEADS - 1) / Q_HEADS : 0);
+    PBD_BY_TYPE(k_paged_append_rows, dim3((a.max_new + 14) / 16 + 1, groups, batch));
 }
 
 constexpr int KPS_MAX = 4096;     // a wave's lanes hold the addresses of 64 blocks: 4 waves, 16 slots each
@@ -649,15 +743,6 @@ PagedAttnPlan paged_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int ba
     if (p.bytes == 0) p.bytes = 256;                               // (a size of 0 says invalid)
     return p;
 }
-
-#define PBD_BY_TYPE(KERNEL, GRID)                                                                           \
-    do {                                                                                                    \
-        if (dtype == PBD_DTYPE_BF16 && head_dim == 128) PBD_LAUNCH((KERNEL<bf16, 128>), GRID, dim3(256), 0, st, a); \
-        else if (dtype == PBD_DTYPE_BF16) PBD_LAUNCH((KERNEL<bf16, 64>), GRID, dim3(256), 0, st, a);        \
-        else if (head_dim == 128) PBD_LAUNCH((KERNEL<float, 128>), GRID, dim3(256), 0, st, a);              \
-        else PBD_LAUNCH((KERNEL<float, 64>), GRID, dim3(256), 0, st, a);                                    \
-        return hipGetLastError();                                                                           \
-    } while (0)
 
 hipError_t launch_paged_attn_splits(int dtype, int head_dim, const PagedAttnArgs& a, int batch, hipStream_t st) {
     PBD_BY_TYPE(k_paged_attn, dim3(a.plan.splits, a.n_kv * a.plan.tiles, batch));
