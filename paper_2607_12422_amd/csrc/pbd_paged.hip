@@ -592,9 +592,23 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a) {
         const int G = a.n_q / a.n_kv, beg = c * SCORE_SLOTS, end = min(len, beg + SCORE_SLOTS);
         if (beg >= end) return;
         float* dst = a.pg.score + ((size_t)b * a.n_kv + kvh) * a.pg.slot_stride;
-        float sum[SCORE_SLOTS / 256];
+        // this thread's slots, 256 apart (past the end: the last, not stored)
+        constexpr int N = SCORE_SLOTS / 256, AHEAD = 2;
+        int at[N];
+        float old[N], sum[N], next[AHEAD][N];
+        const float* raw = a.raw + ((size_t)b * a.n_q + kvh * G) * a.plan.len_pad;
 #pragma unroll
-        for (int i = 0; i < SCORE_SLOTS / 256; ++i) sum[i] = 0.f;
+        for (int i = 0; i < N; ++i) at[i] = min(beg + i * 256 + (int)threadIdx.x, end - 1);
+        // the first heads' scores on their way while the sums over the splits are taken
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+            for (int i = 0; i < N; ++i) next[q][i] = load_once<float>(raw + (size_t)min(q, G - 1) * a.plan.len_pad + at[i]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            old[i] = dst[at[i]];
+            sum[i] = 0.f;
+        }
         bool bad = false;
         for (int q0 = 0; q0 < G; q0 += 16) {
             const int nq = min(16, G - q0);
@@ -609,22 +623,21 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a) {
                 bad |= x;
             }
             __syncthreads();
+#pragma unroll 1
             for (int q = 0; q < nq; ++q) {
-                const float* raw = a.raw + ((size_t)b * a.n_q + kvh * G + q0 + q) * a.plan.len_pad;
                 const float ref = s_max[q], inv = s_inv[q];
 #pragma unroll
-                for (int i = 0; i < SCORE_SLOTS / 256; ++i) {
-                    const int s = beg + i * 256 + threadIdx.x;
-                    if (s < end) sum[i] += __builtin_amdgcn_exp2f(raw[s] - ref) * inv;
+                for (int i = 0; i < N; ++i) {
+                    sum[i] += __builtin_amdgcn_exp2f(next[0][i] - ref) * inv;
+                    next[0][i] = next[1][i];
+                    next[1][i] = load_once<float>(raw + (size_t)min(q0 + q + AHEAD, G - 1) * a.plan.len_pad + at[i]);
                 }
             }
         }
         if (__syncthreads_or(bad)) return;
 #pragma unroll
-        for (int i = 0; i < SCORE_SLOTS / 256; ++i) {
-            const int s = beg + i * 256 + threadIdx.x;
-            if (s < end) dst[s] += sum[i];
-        }
+        for (int i = 0; i < N; ++i)
+            if (beg + i * 256 + (int)threadIdx.x < end) dst[at[i]] = old[i] + sum[i];
         return;
     }
     const int h = blockIdx.x;
