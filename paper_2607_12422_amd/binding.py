@@ -358,25 +358,30 @@ def pbd_paged_attention(pages: PbdPages, q, lens, max_len: int, out, ws, lse=Non
           D ** -0.5 if scale is None else scale, _f32(out, B * HQ * D, "out", dev), _f32(lse, B * HQ, "lse", dev), w, wb)
 
 
+def _rows_at(t, strides) -> bool:
+    """Whether the dimensions of more than one element have these strides."""
+    return all(n == 1 or a == b for n, a, b in zip(t.shape, t.stride(), strides))
+
+
 def pbd_paged_append(pages: PbdPages, k, v, lens, pos, rope, q=None, q_out=None, n_new=None, q_norm=None, k_norm=None,
                      eps: float = 1e-6, len_out=None, stream=None):
     """k, v float32 [batch][rows][n_kv_heads * head_dim] and q [batch][rows][n_q_heads * head_dim], all with the same
     stride from a row to the next (columns of one projection); lens, pos, n_new, len_out int32 [batch]; rope float32
     [positions][head_dim / 2][2]; q_norm, k_norm [head_dim] in the cache's type; q_out float32 like q, contiguous."""
     dev, H, HQ, D = pages.device, pages.n_kv_heads, pages.n_q_heads, pages.head_dim
-    B, R = k.shape[0], k.shape[1]
+    B, R, _ = k.shape
     # rows lie at one stride: that of the rows, or of the sequences where each has one
     stride = k.stride(1) if R > 1 else k.stride(0) if B > 1 else max(HQ, H) * D
+    whole = (R * stride, stride, 1)
     for t, width, what in ((k, H * D, "k"), (v, H * D, "v"), (q, HQ * D, "q")):
-        if t is not None and (t.dtype is not _torch.float32 or t.shape != (B, R, width) or t.stride(2) != 1 or
-                              (R > 1 and t.stride(1) != stride) or (B > 1 and t.stride(0) != R * stride) or
-                              t.get_device() != dev):
+        if t is not None and (t.dtype is not _torch.float32 or t.shape != (B, R, width) or t.get_device() != dev or
+                              (t.stride() != whole and not _rows_at(t, whole))):
             raise PbdError(PBD_ERR_INVALID_ARG,
                            f"{what} must be float32 [batch][rows][{width}] with the row stride of k")
     if B > pages.rows:
         raise PbdError(PBD_ERR_INVALID_ARG, "the table has fewer rows than k")
     if (rope.dtype is not _torch.float32 or not rope.is_contiguous() or rope.get_device() != dev or
-            rope.shape[1:] != (D // 2, 2)):
+            rope.shape != (rope.size(0), D // 2, 2)):
         raise PbdError(PBD_ERR_INVALID_ARG, "rope must be contiguous float32 [positions][head_dim / 2][2]")
     for t, what in ((q_norm, "q_norm"), (k_norm, "k_norm")):
         if t is not None and (t.numel() != D or not t.is_contiguous() or t.get_device() != dev or
@@ -384,7 +389,7 @@ def pbd_paged_append(pages: PbdPages, k, v, lens, pos, rope, q=None, q_out=None,
             raise PbdError(PBD_ERR_INVALID_ARG, f"{what} must be a contiguous [head_dim] tensor of the cache's type")
     _call(dev, stream, load_library().pbd_paged_append, pages.ref, B, R, _ptr(q), k.data_ptr(), v.data_ptr(),
           stride, _i32(lens, B, "lens", dev), _i32(n_new, B, "n_new", dev), _i32(pos, B, "pos", dev), _ptr(q_norm),
-          _ptr(k_norm), eps, rope.data_ptr(), rope.shape[0], _f32(q_out, B * R * HQ * D, "q_out", dev),
+          _ptr(k_norm), eps, rope.data_ptr(), rope.size(0), _f32(q_out, B * R * HQ * D, "q_out", dev),
           _i32(len_out, B, "len_out", dev))
 
 
