@@ -252,29 +252,29 @@ __global__ __launch_bounds__(256) void k_evict_move(PagedEvictArgs a) {
     const int h = blockIdx.y, b = blockIdx.z, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int l16 = lane & 15, g = lane >> 4;
     const int blk = blockIdx.x * MOVE_WAVES + wave;
+    const int* moves = a.moves + ((size_t)b * a.n_kv + h) * a.list * 2;
+    const int* block_first = a.block_first + ((size_t)b * a.n_kv + h) * a.blocks + min(blk, a.blocks - 2);
+    const int* tab = a.pg.table + (size_t)b * a.pg.table_width;
+    // all of these at once: the pairs' places mean something where there are pairs, the
+    // page where the sequence has the block
     const int K = a.count[(size_t)gridDim.z * a.n_kv + b];
     const int moved = a.count[(size_t)b * a.n_kv + h];
+    const int r0 = block_first[0], r1 = block_first[1];
+    const int id = tab[min(blk >> a.pg.page_shift, a.pg.table_width - 1)];
     if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0 && K >= 0) a.new_lens[b] = K;
     if (blk * 16 >= K) return;
-    const int* moves = a.moves + ((size_t)b * a.n_kv + h) * a.list * 2;
-    const int* block_first = a.block_first + ((size_t)b * a.n_kv + h) * a.blocks + blk;
-    const int* tab = a.pg.table + (size_t)b * a.pg.table_width;
+    const int n = moved > 0 ? r1 - r0 : 0;
     const long long at = ((long long)b * a.n_kv + h) * a.pg.slot_stride;
-    auto block = [&](int i) -> long long {
-        return (long long)tab[i >> a.pg.page_shift] * a.pg.page_stride + (long long)h * a.pg.head_stride +
+    auto place = [&](int page, int i) -> long long {
+        return (long long)page * a.pg.page_stride + (long long)h * a.pg.head_stride +
                (long long)(i & ((1 << a.pg.page_shift) - 1)) * (16 * HD);
     };
-    const long long d = block(blk);
-    int n = 0, r0 = 0;
-    if (moved > 0) {
-        r0 = block_first[0];
-        n = block_first[1] - r0;
-    }
+    const long long d = place(id, blk);
     if (lane < 16) s_slot[wave][lane] = -1;
     wave_sync();
     if (lane < n) {
         const int2 mv = *(const int2*)(moves + 2 * (r0 + lane));
-        s_from[wave][mv.x & 15] = block(mv.y >> 4);
+        s_from[wave][mv.x & 15] = place(tab[(mv.y >> 4) >> a.pg.page_shift], mv.y >> 4);
         s_slot[wave][mv.x & 15] = mv.y & 15;
         a.score_out[at + mv.x] = a.pg.score[at + mv.y];
         if (a.slot_pos_out) a.slot_pos_out[at + mv.x] = a.pg.slot_pos[at + mv.y];
