@@ -63,6 +63,7 @@ __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
     __shared__ __align__(16) unsigned s_hist[BINS * COPIES];
     __shared__ int s_w[3][SEL_W];
     __shared__ unsigned s_bin[3], s_above[3];
+    __shared__ int s_ties;
     __shared__ int4 s_run[SEL_W];
     const int h = blockIdx.x, b = blockIdx.y;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -179,28 +180,44 @@ __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
         if (before < need && before + c[0] >= need) {
             s_bin[pass] = b0;
             s_above[pass] = before;
+            s_ties = c[0];
         } else if (before + c[0] < need && before + c[0] + c[1] >= need) {
             s_bin[pass] = b0 - 1;
             s_above[pass] = before + c[0];
+            s_ties = c[1];
         }
         __syncthreads();
         T |= s_bin[pass] << shift;
         need -= s_above[pass];
     }
+    // what the last pass counted in its bin are the keys equal to T; mostly all stay
+    const bool all_ties = s_ties == need;
     // of each wave's run: the slots that stay for certain, below the new length and
     // past it, and those with the key T, of which the first `need` of all stay
     int4 run{0, 0, 0, 0};
-    walk([&](int i, unsigned u, bool in) {
-        const int i0 = i - lane;                    // the group's first slot: most groups lie on one side
-        if (i0 < K) {
-            run.x += __popcll(__ballot(i < K && u > T));
-            run.y += __popcll(__ballot(i < K && u == T));
-        }
-        if (i0 + 64 > K) {
-            run.z += __popcll(__ballot(in && i >= K && u > T));
-            run.w += __popcll(__ballot(in && i >= K && u == T));
-        }
-    });
+    if (all_ties) {
+        walk([&](int i, unsigned u, bool in) {
+            const int i0 = i - lane;                    // the group's first slot: most groups lie on one side
+            if (i0 + 64 <= K) {
+                run.x += __popcll(__ballot(u >= T));
+            } else {
+                run.x += __popcll(__ballot(i < K && u >= T));
+                run.z += __popcll(__ballot(in && i >= K && u >= T));
+            }
+        });
+    } else {
+        walk([&](int i, unsigned u, bool in) {
+            const int i0 = i - lane;
+            if (i0 < K) {
+                run.x += __popcll(__ballot(i < K && u > T));
+                run.y += __popcll(__ballot(i < K && u == T));
+            }
+            if (i0 + 64 > K) {
+                run.z += __popcll(__ballot(in && i >= K && u > T));
+                run.w += __popcll(__ballot(in && i >= K && u == T));
+            }
+        });
+    }
     if (lane == 0) s_run[wave] = run;
     __syncthreads();
     int tie = 0, hole = 0, mover = 0;
@@ -211,10 +228,7 @@ __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
         hole += min(max(K - w * per * 64, 0), per * 64) - r.x - low;
         mover += r.z + high;
     }
-    walk([&](int i, unsigned u, bool in) {
-        const unsigned long long eq = __ballot(in && u == T);
-        const bool stays = in && (u > T || (u == T && tie + bits_below(eq) < need));
-        tie += __popcll(eq);
+    auto place = [&](int i, bool in, bool stays) {
         const int i0 = i - lane;
         if (i0 < K) {
             const unsigned long long m = __ballot(i < K && !stays);
@@ -224,11 +238,21 @@ __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
             hole += __popcll(m);
         }
         if (i0 + 64 > K) {
-            const unsigned long long m = __ballot(i >= K && stays);
-            if (i >= K && stays) moves[2 * (mover + bits_below(m)) + 1] = i;
+            const unsigned long long m = __ballot(in && i >= K && stays);
+            if (in && i >= K && stays) moves[2 * (mover + bits_below(m)) + 1] = i;
             mover += __popcll(m);
         }
-    });
+    };
+    if (all_ties) {
+        walk([&](int i, unsigned u, bool in) { place(i, in, u >= T); });
+    } else {
+        walk([&](int i, unsigned u, bool in) {
+            const unsigned long long eq = __ballot(in && u == T);
+            const bool stays = u > T || (u == T && tie + bits_below(eq) < need);
+            tie += __popcll(eq);
+            place(i, in, stays);
+        });
+    }
     if (tid == SEL_T - 1) {                     // the last wave ends at the total
         *count = hole;
         block_first[(K + 15) >> 4] = hole;
