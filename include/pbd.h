@@ -352,7 +352,8 @@ int pbd_sync_status(pbd_ctx* ctx, pbd_stream_t stream, int32_t* status);
  * (slot within the block).  Page p of KV head h starts at element
  * p * page_stride + h * head_stride of k and of v; both strides are multiples of
  * 16 * head_dim, k and v are 16-byte aligned.  Pages may be shared by sequences
- * that only read them.  Table entries past the pages a call uses are not read.
+ * that only read them.  Table entries past the pages a sequence uses may hold
+ * anything.
  * score and slot_pos (both optional) hold, per sequence, KV head and slot, the
  * attention weight accumulated so far and the position of the token in the
  * slot; [batch][n_kv_heads][slot_stride].

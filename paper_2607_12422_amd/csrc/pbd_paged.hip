@@ -341,7 +341,11 @@ __global__ __launch_bounds__(256, 3) void k_paged_attn(PagedAttnArgs a) {
     const int G = a.n_q / a.n_kv, nq = min(16, G - tile * 16), hq0 = kvh * G + tile * 16;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
     const int len = a.lens[b];
-    const int beg = split * a.plan.kps;
+    const int beg = split * a.plan.kps, blk0 = beg >> 4;
+    // lane i: block i % NB of this wave's step i / NB, and its page, both looked up
+    // before the length is known (pages past it are not followed)
+    const int my_blk = min(blk0 + (wave + ATT_WAVES * (lane / NB)) * NB + lane % NB, (a.max_len - 1) >> 4);
+    const int id = a.pg.table[(size_t)b * a.pg.table_width + (my_blk >> a.pg.page_shift)];
     if (a.plan.direct) {
         // no join follows: invalid and empty sequences end here
         if (len < 0 || len > a.max_len) {
@@ -357,16 +361,13 @@ __global__ __launch_bounds__(256, 3) void k_paged_attn(PagedAttnArgs a) {
     // (otherwise the join reports a length out of range)
     if (len > a.max_len || beg >= len) return;
     const int end = min(len, beg + a.plan.kps);
-    const int blk0 = beg >> 4, blk_last = (end - 1) >> 4;
+    const int blk_last = (end - 1) >> 4;
     const int steps = (blk_last - blk0 + NB) / NB;
     const int mine = wave < steps ? (steps - wave + ATT_WAVES - 1) / ATT_WAVES : 0;
     if (threadIdx.x == 0) s_bad = 0;
-    // lane i: the address of block i % NB of this wave's step i / NB (past the
-    // last one: the last, whose slots are masked)
-    const int my_blk = min(blk0 + (wave + ATT_WAVES * (lane / NB)) * NB + lane % NB, blk_last);
-    const int id = a.pg.table[(size_t)b * a.pg.table_width + (my_blk >> a.pg.page_shift)];
-    const bool bad = id < 0 || id >= a.pg.n_pages;
-    const long long off = block_offset(a.pg, bad ? 0 : id, my_blk, kvh, 16 * HD) * (long long)sizeof(T);
+    // (past the last block: page 0's, whose slots are masked)
+    const bool valid = id >= 0 && id < a.pg.n_pages, bad = !valid && my_blk <= blk_last;
+    const long long off = block_offset(a.pg, valid && my_blk <= blk_last ? id : 0, my_blk, kvh, 16 * HD) * (long long)sizeof(T);
     const int off_lo = (int)(off & 0xffffffffll), off_hi = (int)(off >> 32);
     auto at = [&](int i) -> size_t {
         return (size_t)(unsigned)__builtin_amdgcn_readlane(off_lo, i) |
@@ -559,29 +560,37 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a) {
     constexpr int LANES = HD / 4, GROUPS = 256 / LANES;
     __shared__ f32x4 s_o[GROUPS][LANES];
     __shared__ float s_max[16], s_inv[16];
-    const int b = blockIdx.y;
-    const int len = a.lens[b];
-    if (len < 0 || len > a.max_len) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) raise(a.pg.status, PBD_STATUS_CAPACITY);
-        return;
-    }
-    const int n = (len + a.plan.kps - 1) / a.plan.kps;
+    const int b = blockIdx.y, splits = a.plan.splits;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    // the maximum and the sum over all splits of head h; whether a page was bad
-    auto total = [&](int h, float& M, float& L) -> bool {
-        const float* ml = a.part_ml + ((size_t)b * a.n_q + h) * a.plan.splits * 2;
-        float mx = -INFINITY;
-        bool bad = false;
-        for (int s = lane; s < n; s += 64) {
-            const float x = ml[2 * s];
-            bad |= x != x;
-            mx = fmaxf(mx, x);
+    // every load that the length does not place is requested before the length is
+    // used: entries of splits or slots past it are in bounds and dropped
+    const int len = a.lens[b];
+    auto invalid = [&]() -> bool {
+        if (len >= 0 && len <= a.max_len) return false;
+        if (blockIdx.x == 0 && threadIdx.x == 0) raise(a.pg.status, PBD_STATUS_CAPACITY);
+        return true;
+    };
+    // maximum and sum of a split
+    typedef float __attribute__((ext_vector_type(2))) ml2;
+    auto split_ml = [&](int h, int s) -> ml2 {
+        return *(const ml2*)(a.part_ml + (((size_t)b * a.n_q + h) * splits + min(s, splits - 1)) * 2);
+    };
+    auto scaled = [](ml2 x, float M) -> float { return x[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x[0] - M); };
+    // the maximum and the sum over all n splits of head h, of which the lane has one of
+    // the first 64; whether a page was bad
+    auto total = [&](int h, int n, ml2 mine, float& M, float& L) -> bool {
+        bool bad = lane < n && mine[0] != mine[0];
+        float mx = lane < n ? mine[0] : -INFINITY;
+        for (int s = lane + 64; s < n; s += 64) {
+            const ml2 x = split_ml(h, s);
+            bad |= x[0] != x[0];
+            mx = fmaxf(mx, x[0]);
         }
         M = wave_max(mx);
-        float sum = 0.f;
-        for (int s = lane; s < n; s += 64) {
-            const float x = ml[2 * s];
-            sum += ml[2 * s + 1] * (x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x - M));
+        float sum = lane < n ? mine[1] * scaled(mine, M) : 0.f;
+        for (int s = lane + 64; s < n; s += 64) {
+            const ml2 x = split_ml(h, s);
+            sum += x[1] * scaled(x, M);
         }
         L = wave_sum(sum);
         return __any(bad);
@@ -589,17 +598,16 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a) {
     if ((int)blockIdx.x >= a.n_q) {
         const int chunks = (a.max_len + SCORE_SLOTS - 1) / SCORE_SLOTS;
         const int kvh = ((int)blockIdx.x - a.n_q) / chunks, c = ((int)blockIdx.x - a.n_q) % chunks;
-        const int G = a.n_q / a.n_kv, beg = c * SCORE_SLOTS, end = min(len, beg + SCORE_SLOTS);
-        if (beg >= end) return;
+        const int G = a.n_q / a.n_kv, beg = c * SCORE_SLOTS;
         float* dst = a.pg.score + ((size_t)b * a.n_kv + kvh) * a.pg.slot_stride;
-        // this thread's slots, 256 apart (past the end: the last, not stored)
+        // this thread's slots, 256 apart (past the longest sequence: its last)
         constexpr int N = SCORE_SLOTS / 256, AHEAD = 2;
         int at[N];
         float old[N], sum[N], next[AHEAD][N];
         const float* raw = a.raw + ((size_t)b * a.n_q + kvh * G) * a.plan.len_pad;
 #pragma unroll
-        for (int i = 0; i < N; ++i) at[i] = min(beg + i * 256 + (int)threadIdx.x, end - 1);
-        // the first heads' scores on their way while the sums over the splits are taken
+        for (int i = 0; i < N; ++i) at[i] = min(beg + i * 256 + (int)threadIdx.x, a.max_len - 1);
+        ml2 first = split_ml(kvh * G + min(wave, G - 1), lane);
 #pragma unroll
         for (int q = 0; q < AHEAD; ++q)
 #pragma unroll
@@ -609,13 +617,16 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a) {
             old[i] = dst[at[i]];
             sum[i] = 0.f;
         }
+        if (invalid() || beg >= len) return;
+        const int end = min(len, beg + SCORE_SLOTS), n = (len + a.plan.kps - 1) / a.plan.kps;
         bool bad = false;
         for (int q0 = 0; q0 < G; q0 += 16) {
             const int nq = min(16, G - q0);
             __syncthreads();
             for (int q = wave; q < nq; q += 4) {
                 float M, L;
-                const bool x = total(kvh * G + q0 + q, M, L);
+                const int h = kvh * G + q0 + q;
+                const bool x = total(h, n, q0 + q == wave ? first : split_ml(h, lane), M, L);
                 if (lane == 0) {
                     s_max[q] = M;
                     s_inv[q] = 1.f / L;
@@ -640,17 +651,27 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a) {
             if (beg + i * 256 + (int)threadIdx.x < end) dst[at[i]] = old[i] + sum[i];
         return;
     }
-    const int h = blockIdx.x;
-    float M, L;
-    if (total(h, M, L)) return;
-    const int grp = threadIdx.x / LANES, d = threadIdx.x % LANES;
-    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-    const size_t row = ((size_t)b * a.n_q + h) * a.plan.splits;
-    for (int s = grp; s < n; s += GROUPS) {
-        const float x = a.part_ml[(row + s) * 2];
-        acc += *(const f32x4*)(a.part_o + (row + s) * HD + 4 * d) *
-               (x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x - M));
+    const int h = blockIdx.x, grp = threadIdx.x / LANES, d = threadIdx.x % LANES;
+    const float* part = a.part_o + ((size_t)b * a.n_q + h) * splits * HD + 4 * d;
+    constexpr int AHEAD = 4;                         // splits of a lane group whose loads go first
+    const ml2 mine = split_ml(h, lane);
+    ml2 x[AHEAD];
+    f32x4 o[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        x[i] = split_ml(h, grp + i * GROUPS);
+        o[i] = *(const f32x4*)(part + (size_t)min(grp + i * GROUPS, splits - 1) * HD);
     }
+    if (invalid()) return;
+    const int n = (len + a.plan.kps - 1) / a.plan.kps;
+    float M, L;
+    if (total(h, n, mine, M, L)) return;
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (grp + i * GROUPS < n) acc += o[i] * scaled(x[i], M);
+    for (int s = grp + AHEAD * GROUPS; s < n; s += GROUPS)
+        acc += *(const f32x4*)(part + (size_t)s * HD) * scaled(split_ml(h, s), M);
     s_o[grp][d] = acc;
     __syncthreads();
     if (grp != 0) return;
