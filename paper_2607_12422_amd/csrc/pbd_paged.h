@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include "../../include/pbd.h"
+#include "pbd_device.h"
 
 namespace pbd {
 
@@ -30,6 +31,19 @@ __device__ __forceinline__ void store_once(void* p, const V& v) {
     __builtin_memcpy(&w, &v, sizeof v);
     __builtin_nontemporal_store(w, (words*)p);
 }
+
+// Maximum over the wave, in every lane (DPP inside the 16-lane rows, then permlane swaps).
+__device__ __forceinline__ float wave_max_dpp(float v) {
+#define PBD_STEP(CTRL) v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false)))
+    PBD_STEP(0xB1);      // lane ^ 1
+    PBD_STEP(0x4E);      // lane ^ 2
+    PBD_STEP(0x141);     // half-row mirror
+    PBD_STEP(0x140);     // row mirror
+#undef PBD_STEP
+    return xrow_max(v);
+}
+
+__device__ __forceinline__ float wave_sum_dpp(float v) { return xrow_sum(row16_sum(v)); }
 
 // One layer's paged cache as the kernels address it.
 struct PageView {
