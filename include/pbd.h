@@ -391,7 +391,7 @@ typedef struct pbd_pages {
  * it is.  K and V go to slots lens[b] + i, rounded once to pages->dtype; those
  * slots' score becomes 0 and their slot_pos the position, where the cache has
  * them.  q (NULL: none) goes to q_out [batch][max_new][n_q_heads * head_dim].
- * lens_out (NULL: not wanted; not lens itself) receives lens[b] + n_new[b].
+ * lens_out (NULL: not wanted; overlaps no input) receives lens[b] + n_new[b].
  * Rows past n_new are not read and their q_out rows stay as they were.
  * PBD_STATUS_CAPACITY: lens, n_new or pos out of range, or no room in the table
  * or in rope.  q, k, v, q_out and rope are 16-byte aligned, row_stride is a

@@ -249,8 +249,10 @@ def _space(ws, device: int):
     return ws.data_ptr(), ws.nbytes
 
 
-def _call(device: int, stream, fn, *args):
+def _call(device: int, stream, fn, *args, ctx=None):
     """fn(*args, stream) with the device current."""
+    if device < 0:
+        raise PbdError(PBD_ERR_INVALID_ARG, "the tensors must be on a GPU")
     if stream is None:
         st = _raw_stream(device)
     else:
@@ -261,7 +263,7 @@ def _call(device: int, stream, fn, *args):
         with _torch.cuda.device(device):
             rc = fn(*args, st)
     if rc != PBD_OK:
-        _check(rc, None)
+        _check(rc, ctx)
 
 
 def _raw_stream(device: int) -> int:
@@ -319,12 +321,13 @@ def _attach(p: PbdPages, device: int, layers, table, score, slot_pos, status, ke
     if status is not None:
         p.status = _i32(status, 1, "status", device)
     p.keep = keep + (table, score, slot_pos, status)
-    p.device, p.rows, p.ref = device, B, ctypes.byref(p)
+    p.device, p.rows, p.layers, p.ref = device, B, layers, ctypes.byref(p)
     return p
 
 
 def layer_pages(pages: PbdPages, layer: int) -> PbdPages:
     """One layer of a cache of several."""
+    _need(pages.layers is not None and 0 <= layer < pages.layers, f"the cache has no layer {layer}")
     esz = 2 if pages.dtype == PBD_DTYPE_BF16 else 4
     p = PbdPages.from_buffer_copy(pages)
     p.k = pages.k + layer * pages.layer_stride * esz
@@ -332,7 +335,7 @@ def layer_pages(pages: PbdPages, layer: int) -> PbdPages:
     for name in ("score", "slot_pos"):
         if getattr(pages, name):
             setattr(p, name, getattr(pages, name) + layer * pages.state_layer_stride * 4)
-    p.keep, p.device, p.rows, p.ref = pages.keep, pages.device, pages.rows, ctypes.byref(p)
+    p.keep, p.device, p.rows, p.layers, p.ref = pages.keep, pages.device, pages.rows, None, ctypes.byref(p)
     return p
 
 
@@ -559,13 +562,14 @@ class Engine:
 
     def pbd_decode_paged(self, pages: PbdPages, token, pos, cache_len, max_len: int, ws, logits=None,
                          flags: int = PBD_PASS_DEFAULT, stream=None):
-        B, dev = int(token.shape[0]), pages.device
+        """token, pos, cache_len int32 [batch], advanced by the call; logits float32 [batch, vocab]."""
+        B, dev = token.numel(), pages.device
         _need(B <= pages.rows, "the table has fewer rows than token")
+        _need(pages.layers in (None, self.cfg.n_layers), "the cache has not the model's layers")
         w, wb = _space(ws, dev)
-        rc = self.lib.pbd_decode_paged(self.ctx, ctypes.byref(pages), B, _i32(token, B, "token", dev),
-                                       _i32(pos, B, "pos", dev), _i32(cache_len, B, "cache_len", dev), int(max_len),
-                                       flags, _f32(logits, B * self.cfg.vocab, "logits", dev), w, wb, _stream(stream))
-        _check(rc, self.ctx)
+        _call(dev, stream, self.lib.pbd_decode_paged, self.ctx, pages.ref, B, _i32(token, B, "token", dev),
+              _i32(pos, B, "pos", dev), _i32(cache_len, B, "cache_len", dev), int(max_len), flags,
+              _f32(logits, B * self.cfg.vocab, "logits", dev), w, wb, ctx=self.ctx)
 
     def pbd_sync_status(self, stream=None) -> int:
         st = ctypes.c_int32(0)

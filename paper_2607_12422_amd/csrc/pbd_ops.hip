@@ -100,7 +100,8 @@ int pbd_paged_append(const pbd_pages* pages, int32_t batch, int32_t max_new, con
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(rope, 16) || !aligned(q_out, 16) ||
         !aligned(q_norm, 16) || !aligned(k_norm, 16))
         return op_fail(PBD_ERR_INVALID_ARG, "q, k, v, rope, q_out and the gains must be 16-byte aligned");
-    if (lens_out == lens) return op_fail(PBD_ERR_INVALID_ARG, "lens_out must not be lens");
+    if (lens_out && (lens_out == lens || lens_out == n_new || lens_out == pos))
+        return op_fail(PBD_ERR_INVALID_ARG, "lens_out must be none of lens, n_new and pos");
     PagedAppendArgs a{};
     a.pg = page_view(*pages);
     a.n_q = pages->n_q_heads; a.n_kv = pages->n_kv_heads; a.max_new = max_new; a.rope_len = rope_len;
