@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256) void k_evict_move(PagedEvictArgs a) {
     constexpr int EPL = Elt<T>::EPL, NK = HD / EPL / 4, NT = HD / 16;
     typedef T __attribute__((ext_vector_type(4))) t4;
     __shared__ long long s_from[MOVE_WAVES][16];    // element of the block that slot i's new content comes from
-    __shared__ int s_slot[MOVE_WAVES][16];          // its slot there; -1: slot i keeps its own
+    __shared__ int s_slot[MOVE_WAVES][16];          // that slot; -1: slot i keeps its own
     const int h = blockIdx.y, b = blockIdx.z, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int l16 = lane & 15, g = lane >> 4;
     const int blk = blockIdx.x * MOVE_WAVES + wave;
@@ -299,23 +299,24 @@ __global__ __launch_bounds__(256) void k_evict_move(PagedEvictArgs a) {
     if (lane < n) {
         const int2 mv = *(const int2*)(moves + 2 * (r0 + lane));
         s_from[wave][mv.x & 15] = place(tab[(mv.y >> 4) >> a.pg.page_shift], mv.y >> 4);
-        s_slot[wave][mv.x & 15] = mv.y & 15;
-        a.score_out[at + mv.x] = a.pg.score[at + mv.y];
-        if (a.slot_pos_out) a.slot_pos_out[at + mv.x] = a.pg.slot_pos[at + mv.y];
+        s_slot[wave][mv.x & 15] = mv.y;
     }
     wave_sync();
-    if (lane < 16 && blk * 16 + lane < K && s_slot[wave][lane] < 0) {
-        const long long i = at + blk * 16 + lane;
-        if (a.score_out != a.pg.score) a.score_out[i] = a.pg.score[i];
-        if (a.slot_pos_out && a.slot_pos_out != a.pg.slot_pos) a.slot_pos_out[i] = a.pg.slot_pos[i];
-    }
-    if (n == 0) return;
+    // the slots' state, by lanes 0 .. 15: requested here, stored after the data
+    const int own = blk * 16 + l16, moved_in = s_slot[wave][l16];
+    const bool keeps = lane < 16 && own < K;
+    const bool new_score = keeps && (moved_in >= 0 || a.score_out != a.pg.score);
+    const bool new_pos = keeps && a.slot_pos_out && (moved_in >= 0 || a.slot_pos_out != a.pg.slot_pos);
+    const long long state = at + (moved_in >= 0 ? moved_in : own);
+    float score = 0.f;
+    int pos = 0;
+    if (new_score) score = a.pg.score[state];
+    if (new_pos) pos = a.pg.slot_pos[state];
     const bool whole = n >= WHOLE;
-    {
-        const int from = s_slot[wave][l16];
-        const T* src = (const T*)a.pg.k + (from < 0 ? d + l16 * EPL : s_from[wave][l16] + from * EPL);
+    if (n > 0) {
+        const T* src = (const T*)a.pg.k + (moved_in < 0 ? d + l16 * EPL : s_from[wave][l16] + (moved_in & 15) * EPL);
         T* dst = (T*)a.pg.k + d + l16 * EPL;
-        if (whole || from >= 0) {
+        if (whole || moved_in >= 0) {
             constexpr int STEP = NK > 4 ? 4 : NK;
 #pragma unroll
             for (int i0 = 0; i0 < NK; i0 += STEP) {
@@ -327,7 +328,7 @@ __global__ __launch_bounds__(256) void k_evict_move(PagedEvictArgs a) {
             }
         }
     }
-    {
+    if (n > 0) {
         int from[4];
         const T* src[4];
         bool some = false;
@@ -356,6 +357,8 @@ __global__ __launch_bounds__(256) void k_evict_move(PagedEvictArgs a) {
             }
         }
     }
+    if (new_score) a.score_out[at + own] = score;
+    if (new_pos) a.slot_pos_out[at + own] = pos;
 }
 
 }  // namespace
