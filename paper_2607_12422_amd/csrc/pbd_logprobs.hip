@@ -31,13 +31,28 @@ constexpr int TILE = LP_T * GROUP;
 constexpr int TILES_MAX = 20;                   // tiles of a part: their group maxima fit 20 KiB of LDS
 constexpr int GROUPS_CAP = 256, CAND_CAP = 512;
 constexpr int TOP_MAX = 32;
-constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr float LEAST = -1e30f;                 // bounds x - m where it is a factor: a masked token adds 0, not 0 * -inf
 
 typedef unsigned long long u64;
 
 struct Stat {
     float m, s, t;
+};
+
+// What a wave's sums are relative to: exp2(x log2 e - r) is one fused product and
+// one exponential an element.  r is the maximum's x log2 e rounded; what the
+// rounding left is known exactly (at_max) and taken out of the sums at the end.
+// Maxima whose product could overflow are subtracted first (shift), and none or
+// an infinite one stand for 0.
+struct Ref {
+    float r, at_max, shift;
+    __device__ __forceinline__ explicit Ref(float m) {
+        const bool plain = fabsf(m) < -LEAST;
+        r = plain ? m * LOG2E : 0.f;
+        at_max = plain ? __builtin_fmaf(m, LOG2E, -r) : 0.f;
+        shift = plain || isinf(m) ? 0.f : m;
+    }
 };
 
 // exp(x), x <= 0 or NaN
@@ -170,6 +185,7 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
     const Row<T> row(a.logits, a.row_stride, r, a.vocab);
     const int t0 = ONE ? part : part * pt.per, t1 = ONE ? t0 + 1 : min(pt.tiles, t0 + pt.per);
     float m = -INFINITY, s = 0.f, t = 0.f, mine = -INFINITY;
+    Ref ref(m);
     uint4 next[PER];
     auto fetch = [&](int tile) {
         if (row.inner(tile)) {
@@ -198,14 +214,17 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
         // (the same in every lane: a scalar, so that the branch is one)
         top = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(wave_max_dpp(top))));
         if (top > m) {
+            const Ref old = ref;
+            ref = Ref(top);
             if (m > -INFINITY) {
-                // lane 0 has the instance of the old maximum that the sum leaves out
-                const float d = fmaxf(m - top, LEAST), f = exp_neg(d), all = lane == 0 ? s + 1.f : s;
-                t = f * (t + d * all);
-                s = f * all;
+                // lane 0 has the instance of the old maximum that the sums leave out
+                const float d = old.shift == 0.f && ref.shift == 0.f ? old.r - ref.r : fmaxf(m - top, LEAST) * LOG2E;
+                const float f = __builtin_amdgcn_exp2f(d), e = lane == 0 ? __builtin_amdgcn_exp2f(old.at_max) : 0.f;
+                t = f * (t + e * old.at_max + d * (s + e));
+                s = f * (s + e);
             }
             m = top;
-            // the new one's instances add 1 each, but for one: out of the sums below
+            // the new one's instances, but for one, are summed here and not below
             int at_max = 0;
 #pragma unroll
             for (int i = 0; i < GROUP; ++i) {
@@ -213,15 +232,25 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
                 at_max += __popcll(__ballot(is));
                 x[i] = is ? -INFINITY : x[i];
             }
-            if (lane == 0) s += (float)(at_max - 1);
+            const float e = lane == 0 ? (float)(at_max - 1) * __builtin_amdgcn_exp2f(ref.at_max) : 0.f;
+            s += e;
+            t += e * ref.at_max;
         }
-        const float ref = m == -INFINITY ? 0.f : m;
+        if (ref.shift != 0.f)
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) x[i] -= ref.shift;
 #pragma unroll
         for (int i = 0; i < GROUP; ++i) {
-            const float d = x[i] - ref, e = exp_neg(d);
+            const float u = __builtin_fmaf(x[i], LOG2E, -ref.r), e = __builtin_amdgcn_exp2f(u);
             s += e;
-            t += e * fmaxf(d, LEAST);
+            t += e * fmaxf(u, LEAST);
         }
+    }
+    {
+        // relative to the maximum itself, in natural units
+        const float c = __builtin_amdgcn_exp2f(-ref.at_max);
+        t = (t - ref.at_max * s) * c * LN2;
+        s *= c;
     }
     s = wave_sum_dpp(s);
     t = wave_sum_dpp(t);
