@@ -265,12 +265,17 @@ __global__ __launch_bounds__(256) void k_paged_append_few(PagedAppendArgs a) {
 // A work-group takes kps slots of one KV head for up to 16 of its query heads;
 // its four waves take the 16 NB-slot steps of the split in turn, each with its
 // own running maximum and sum, and are joined in LDS.  K and V go from the cache
-// to registers once (non-temporal loads: 32 sequences of 8192 slots take 200 us a
+// to registers once (non-temporal loads: 32 sequences of 8192 slots took 200 us a
 // call, 225 through the caches' usual policy) and straight into the matrix
-// products: the next step's K is requested while this step's softmax runs, the next V while the next scores do,
-// and the blocks' addresses are looked up once per split, 64 in the wave's lanes.
+// products: the next step's K is requested while this step's softmax runs, the
+// next V while the next scores do, and the blocks' addresses are looked up once
+// per split, 64 in the wave's lanes.
 // The products do 4 * 16 * head_dim flops a slot on matrix cores whatever the
-// number of heads that share a KV head, so that the cache's bytes are the bound.
+// number of heads that share a KV head, so that the cache's bytes are the bound:
+// 32 sequences of 8192 slots, 8 heads of 128 in bf16 (1.07 GB, weights kept) take
+// 174 to 186 us, 5.8 to 6.2 TB/s; 24 of 256 to 4096 slots (107 MB) 22 us, where the
+// last work-groups run alone; one of 4096 (17 MB) 7 us, most of it the waits of one
+// split for its pages, its K and its V.
 //
 // A bf16 cache: K and V are exact operands, and the query and the weights go in
 // as three bf16 terms each, which hold all 24 bits of their fp32 values, so that
@@ -556,7 +561,8 @@ __global__ __launch_bounds__(256, 3) void k_paged_attn(PagedAttnArgs a) {
 // Joins the splits of one query head (work-groups x < n_q), in split order: the
 // same sums whatever ran first.  Work-groups past them (weights accumulated):
 // SCORE_SLOTS slots of one KV head each, whose kept scores become weights under
-// the head's whole sum.
+// the head's whole sum.  3.5 us for one sequence, 10 with 32 times 8192 slots'
+// weights (kept scores of two query heads a KV head: 33 MB in, 17 in and out).
 constexpr int SCORE_SLOTS = 1024;
 
 template <typename T, int HD>
@@ -735,7 +741,14 @@ PageView page_view(const pbd_pages& p) {
     return v;
 }
 
-constexpr int FEW_ROWS = 8;       // rows per sequence below which a work-group takes heads instead of slots
+// A work-group takes 16 heads of one row, not the 16 slots of a block, where most of
+// a block's slots would have no row, and up to as many work-groups as run at once,
+// two a CU: it has one wait less (captured, us, heads of a row against slots of a
+// block; 16 / 8 heads of 128 in bf16: one sequence of 16 rows 3.3 and 4.3, of 256 4.4
+// and 4.5, of 512 5.4 and 4.6; 32 sequences of one row 3.2 and 4.3, of 8 4.7 and 5.0,
+// of 16 7.2 and 5.4; 64 of 6 5.2 and 6.2, of 8 7.0 and 6.4).
+constexpr int FEW_ROWS = 8;
+constexpr int FEW_GROUPS = 512;
 
 #define PBD_BY_TYPE(KERNEL, GRID)                                                                           \
     do {                                                                                                    \
@@ -748,14 +761,17 @@ constexpr int FEW_ROWS = 8;       // rows per sequence below which a work-group 
 
 hipError_t launch_paged_append(int dtype, int head_dim, const PagedAppendArgs& a, int batch, hipStream_t st) {
     const int heads = a.n_kv + (a.q ? a.n_q : 0);
-    if (a.max_new < FEW_ROWS)
-        PBD_BY_TYPE(k_paged_append_few, dim3(std::max(1, a.max_new), (heads + 15) / 16, batch));
+    const int parts = (heads + 15) / 16;
+    if (a.max_new < FEW_ROWS || (long long)a.max_new * parts * batch <= FEW_GROUPS)
+        PBD_BY_TYPE(k_paged_append_few, dim3(std::max(1, a.max_new), parts, batch));
     const int groups = (a.n_kv + KV_HEADS - 1) / KV_HEADS + (a.q ? (a.n_q + Q_HEADS - 1) / Q_HEADS : 0);
     PBD_BY_TYPE(k_paged_append_rows, dim3((a.max_new + 14) / 16 + 1, groups, batch));
 }
 
 constexpr int KPS_MAX = 4096;     // a wave's lanes hold the addresses of 64 blocks of 16 slots, the four waves of 256
-constexpr int ATT_GROUPS = 1024;  // work-groups wanted
+// Work-groups wanted; 768 run at once, and an uneven batch leaves some with nothing to
+// do (24 sequences of 256 to 4096 slots: 26 us; 30 to 31 with 512, 768, 1536 or 2048).
+constexpr int ATT_GROUPS = 1024;
 // Slots up to which one work-group takes a whole sequence and no join follows
 // (captured: 16 / 8 heads of 128 in bf16, 384 slots 7.0 us against 8.0 split, 512
 // slots 8.0 and 8.0, 768 9.9 and 8.1; 4 / 2 heads of 64 in fp32, 128 slots 4.6 and

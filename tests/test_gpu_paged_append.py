@@ -127,7 +127,7 @@ class Call:
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("rows", [1, 2, 7, 8, 16, 33, 100])
+@pytest.mark.parametrize("rows", [1, 2, 7, 8, 16, 33, 100, 333])
 def test_rows(rows, dtype, D):
     """Few rows and many, from every place of a block, each sequence with its own count (none, too)."""
     lens = [0, 1, 3, 15, 16, 30]
@@ -137,8 +137,26 @@ def test_rows(rows, dtype, D):
     assert int(c.status) == 0
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows", [1, 7, 9])
+def test_many_sequences(rows, D):
+    """Few rows of many sequences, inside one block and over its end."""
+    lens = [(7 * i) % 50 for i in range(560)]
+    c = Call(lens, [(rows, rows - 1, rows)[i % 3] for i in range(560)], rows, 2, 2, D, BF, seed=rows)
+    c.run()
+    c.check()
+    assert int(c.status) == 0
+
+
+@pytest.mark.parametrize("rows", [4, 300])
+def test_no_rows(rows):
+    c = Call([3, 17], [0, 0], rows, 2, 2, 64, BF)
+    c.run()
+    c.check()
+
+
 @pytest.mark.parametrize("H,G", [(1, 1), (3, 5), (8, 2), (1, 33)])
-@pytest.mark.parametrize("rows", [1, 20])
+@pytest.mark.parametrize("rows", [1, 20, 300])
 def test_heads(H, G, rows):
     c = Call([4, 13], None, rows, H, G, 128, BF, seed=G)
     c.run()
@@ -148,13 +166,13 @@ def test_heads(H, G, rows):
 @pytest.mark.parametrize("major", ["page", "head"])
 @pytest.mark.parametrize("page", [16, 64, 512])
 def test_pages(page, major):
-    for rows in (3, 70):
+    for rows in (3, 70, 210):
         c = Call([5, 700, 48], [rows, rows, 1], rows, 2, 1, 64, BF, page=page, major=major)
         c.run()
         c.check()
 
 
-@pytest.mark.parametrize("rows", [1, 9])
+@pytest.mark.parametrize("rows", [1, 9, 290])
 def test_without_norm_queries_or_state(rows):
     for kw in (dict(norm=False), dict(with_q=False), dict(state=False), dict(joined=False)):
         c = Call([4, 40], None, rows, 2, 1, 64, F32, **kw)
@@ -168,7 +186,7 @@ def test_far_positions():
     c.check()
 
 
-@pytest.mark.parametrize("rows", [2, 20])
+@pytest.mark.parametrize("rows", [2, 20, 120])
 def test_sequences_that_do_not_fit_are_skipped(rows):
     """No room in the table, a negative length or count, positions outside the rope table."""
     c = Call([0, 10, 4, 20, 8], None, rows, 2, 2, 64, BF)
@@ -182,7 +200,7 @@ def test_sequences_that_do_not_fit_are_skipped(rows):
     c.check(skipped=(1, 2, 3, 4))
 
 
-@pytest.mark.parametrize("rows", [2, 40])
+@pytest.mark.parametrize("rows", [2, 40, 290])
 def test_bad_pages_are_not_followed(rows):
     c = Call([3, 14], None, rows, 2, 1, 64, BF)
     k, v, table = c.pages.keep[:3]
@@ -203,3 +221,45 @@ def test_slots_past_the_state_do_not_fit():
     c.run()
     assert int(c.status) == pbd.PBD_STATUS_CAPACITY
     c.check(skipped=(0,))
+
+
+@pytest.mark.parametrize("rows", [2, 300])
+def test_captured_and_replayed(rows):
+    """A replay appends what the buffers hold by then, at the lengths of then."""
+    c = Call([8, 35], None, rows, 2, 2, 64, BF)                  # (its table has pages for these)
+    first = c.i(c.lens)
+    pos, rope, gains = c.i(c.pos), rope_table(1000, 64).to(DEV), [g.to(DEV) for g in c.gains]
+    c.rope = rope.cpu()
+
+    def call():
+        pbd.pbd_paged_append(c.pages, c.dk, c.dv, first, pos, rope, q=c.dq, q_out=c.q_out, q_norm=gains[0],
+                             k_norm=gains[1], eps=1e-6, len_out=c.len_out)
+    call()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for c.lens in ([3, 30], [8, 35], [3, 30]):
+        first.copy_(c.i(c.lens))
+        c.pool[0].copy_(c.k0)
+        c.pool[1].copy_(c.v0)
+        c.score.fill_(3.0)
+        c.slot_pos.fill_(-9)
+        g.replay()
+        torch.cuda.synchronize()
+        c.check()
+
+
+def test_two_streams():
+    """Calls on two streams, each on its own cache and tensors."""
+    calls = [Call([4, 13], None, rows, 2, 2, 64, BF, seed=rows) for rows in (5, 290)]
+    streams = [torch.cuda.Stream() for _ in calls]
+    args = [(c.i(c.lens), c.i(c.pos), c.rope.to(DEV), [g.to(DEV) for g in c.gains]) for c in calls]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, s, (lens, pos, rope, gains) in zip(calls, streams, args):
+            with torch.cuda.stream(s):
+                pbd.pbd_paged_append(c.pages, c.dk, c.dv, lens, pos, rope, q=c.dq, q_out=c.q_out, q_norm=gains[0],
+                                     k_norm=gains[1], eps=1e-6, len_out=c.len_out)
+    torch.cuda.synchronize()
+    for c in calls:
+        c.check()
