@@ -58,7 +58,15 @@ __device__ __forceinline__ int bits_below(unsigned long long m) {
 // (KEYS 0: longer caches, whose keys every walk reads again).  Accumulated
 // weights crowd a few exponents, so that a wave's lanes would queue at one bin:
 // each bin has COPIES counters, a lane's by its number.
-template <int KEYS, int COPIES>
+// Latency bounds it, one CU a head through barriers between dependent passes: 7 us
+// at 640 slots, 19 at 8192, 42 at 40001 (68 at 65536, and twice that past it).  A
+// call with its moves (captured, us, fp32 640 / bf16 8192 / 40001 slots): keys in
+// as few groups as hold them 11.6 / 25.3 / 57.6, in the next larger ones 15.9 /
+// 27.5 / 106, read again by every walk 12.2 / 35.8 / 106; one, two and four
+// counters a bin 11.6, 11.6, 12.4 / 24.7, 24.7, 25.3 / 58.2, 57.7, 57.6.
+constexpr int COPIES = 2;
+
+template <int KEYS>
 __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
     __shared__ __align__(16) unsigned s_hist[BINS * COPIES];
     __shared__ int s_w[3][SEL_W];
@@ -264,7 +272,12 @@ __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
 // slot's own place or from the slot that moves in; a V run (4 slots of one dim)
 // is put together from up to four.  The block is read and written whole where
 // WHOLE slots or more of it are replaced (its lines are touched anyway, and a
-// line written whole need not be read back for the bytes between).
+// line written whole need not be read back for the bytes between): 32 sequences of
+// 8192 slots halved take 363 us with 3 and 405, 410 and 413 with 6, 9 and never.
+// What bounds it is the lines it touches, not the bytes it needs: a K piece is 16
+// bytes of a 128-byte line and a V element 2, so that a block with a few leavers
+// is read and written whole, and so nearly is the block each filler comes from: 1.6
+// GB there in 308 to 332 us, 4.9 to 5.2 TB/s, the rate of a copy.
 constexpr int MOVE_WAVES = 4, WHOLE = 3;
 
 template <typename T, int HD>
@@ -368,11 +381,11 @@ size_t paged_evict_blocks(int max_len) { return ((size_t)max_len + 15) / 16 + 1;
 
 hipError_t launch_paged_evict(int dtype, int head_dim, const PagedEvictArgs& a, int batch, hipStream_t st) {
     const dim3 sel(a.n_kv, batch);
-    if (a.max_len <= 2 * SEL_T) PBD_LAUNCH((k_evict_select<2, 1>), sel, dim3(SEL_T), 0, st, a);
-    else if (a.max_len <= 8 * SEL_T) PBD_LAUNCH((k_evict_select<8, 4>), sel, dim3(SEL_T), 0, st, a);
-    else if (a.max_len <= 24 * SEL_T) PBD_LAUNCH((k_evict_select<24, 4>), sel, dim3(SEL_T), 0, st, a);
-    else if (a.max_len <= 64 * SEL_T) PBD_LAUNCH((k_evict_select<64, 4>), sel, dim3(SEL_T), 0, st, a);
-    else PBD_LAUNCH((k_evict_select<0, 4>), sel, dim3(SEL_T), 0, st, a);
+    if (a.max_len <= 2 * SEL_T) PBD_LAUNCH((k_evict_select<2>), sel, dim3(SEL_T), 0, st, a);
+    else if (a.max_len <= 8 * SEL_T) PBD_LAUNCH((k_evict_select<8>), sel, dim3(SEL_T), 0, st, a);
+    else if (a.max_len <= 24 * SEL_T) PBD_LAUNCH((k_evict_select<24>), sel, dim3(SEL_T), 0, st, a);
+    else if (a.max_len <= 64 * SEL_T) PBD_LAUNCH((k_evict_select<64>), sel, dim3(SEL_T), 0, st, a);
+    else PBD_LAUNCH((k_evict_select<0>), sel, dim3(SEL_T), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const dim3 grid((a.blocks - 1 + MOVE_WAVES - 1) / MOVE_WAVES, a.n_kv, batch);
