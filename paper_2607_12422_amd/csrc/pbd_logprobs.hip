@@ -14,6 +14,12 @@
 // the groups that reach the bound (about 1.2 n of some thousands) are read again,
 // the elements that reach it ranked by (value, lower id).  Where too many reach it
 // (masses of equal logits) the row is scanned n times instead.
+//
+// An element's vector instructions (conversion, maxima, an exponential, two sums) and
+// its load bound a pass about equally: 1024 rows of 151936 bf16 logits, as many as run
+// at once, take 69 us (4.5 TB/s), 2048 take 124 (5.0 TB/s); 1056 take 84, the last 32
+// rows alone.  Few rows take a part's latency and a join's: 17 rows of fp32 10 and 7
+// us.
 #include "pbd_device.h"
 #include "pbd_launch.h"
 #include "pbd_paged.h"
@@ -28,7 +34,7 @@ namespace {
 constexpr int LP_T = 256;
 constexpr int GROUP = 32;                       // elements per thread and tile
 constexpr int TILE = LP_T * GROUP;
-constexpr int TILES_MAX = 20;                   // tiles of a part: their group maxima fit 20 KiB of LDS
+constexpr int TILES_MAX = 20;                   // tiles of a part: their group maxima fit 20 KiB of LDS, so that LDS limits no CU's work-groups
 constexpr int GROUPS_CAP = 256, CAND_CAP = 512;
 constexpr int TOP_MAX = 32;
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
@@ -449,7 +455,10 @@ __global__ __launch_bounds__(LP_T) void k_logprobs_join(LogprobArgs a, Part pt) 
     write_row(a, r, st, chosen, s_top);
 }
 
-constexpr int LP_GROUPS = 512;      // work-groups wanted
+// Work-groups wanted: parts of one tile for a few rows, fewer to join for more
+// (captured, us, for 128 / 256 / 512 / 1024; 17 rows of 151936 in fp32 17.2 / 15.3 /
+// 14.6 / 14.3, 64 rows 26.0 / 20.6 / 20.3 / 21.7, 128 rows 32.2 / 27.6 / 24.0 / 27.7).
+constexpr int LP_GROUPS = 512;
 
 Part plan(int rows, int vocab, int top_n, char* ws) {
     Part p{};
