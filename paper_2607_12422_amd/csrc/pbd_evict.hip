@@ -59,11 +59,11 @@ __device__ __forceinline__ int bits_below(unsigned long long m) {
 // weights crowd a few exponents, so that a wave's lanes would queue at one bin:
 // each bin has COPIES counters, a lane's by its number.
 // Latency bounds it, one CU a head through barriers between dependent passes: 7 us
-// at 640 slots, 19 at 8192, 42 at 40001 (68 at 65536, and twice that past it).  A
-// call with its moves (captured, us, fp32 640 / bf16 8192 / 40001 slots): keys in
-// as few groups as hold them 11.6 / 25.3 / 57.6, in the next larger ones 15.9 /
-// 27.5 / 106, read again by every walk 12.2 / 35.8 / 106; one, two and four
-// counters a bin 11.6, 11.6, 12.4 / 24.7, 24.7, 25.3 / 58.2, 57.7, 57.6.
+// at 640 slots, 18 at 8192, 42 at 40001 (a whole call that evicts one slot takes 68 at
+// 65530 and 136 at 65540).  A call with its moves (captured, us, fp32 640 / bf16 8192
+// / 40001 slots): keys in as few groups as hold them 11.6 / 25.3 / 57.6, in the next
+// larger ones 15.9 / 27.5 / 106, read again by every walk 12.2 / 35.8 / 106; one, two
+// and four counters a bin 11.6, 11.6, 12.4 / 24.7, 24.7, 25.3 / 58.2, 57.7, 57.6.
 constexpr int COPIES = 2;
 
 template <int KEYS>

