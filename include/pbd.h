@@ -432,7 +432,8 @@ int pbd_paged_attention(const pbd_pages* pages, int32_t batch, const float* q, i
  * Eviction by accumulated attention weight.  Each KV head of each sequence
  * keeps min(keep[b], lens[b]) of its lens[b] slots: first those that always
  * stay (slot_pos >= pos[b] - recent or slot_pos < sink; pos is the position of
- * the next token; without slot_pos, recent and sink must be 0), then by
+ * the next token, NULL only where recent is 0, and then no slot stays for being
+ * recent; without slot_pos, recent and sink must be 0), then by
  * descending score (NaN last); equal ones by ascending slot.  The kept slots at
  * or past the new length move, K, V, score and position, into the evicted
  * slots below it, the i-th (ascending) into the i-th; every other slot stays

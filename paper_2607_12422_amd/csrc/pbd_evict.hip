@@ -83,7 +83,7 @@ __global__ __launch_bounds__(SEL_T) void k_evict_select(PagedEvictArgs a) {
     if (len < 0 || len > a.max_len || want < 0) bad = PBD_STATUS_CAPACITY;
     const float* score = a.pg.score + at;
     const int* slot_pos = a.pg.slot_pos ? a.pg.slot_pos + at : nullptr;
-    const long long last = a.pos ? (long long)a.pos[b] - a.recent : 0;
+    const long long last = a.pos ? (long long)a.pos[b] - a.recent : 1ll << 32;   // (no pos: no position stays for being recent)
     // each wave's run of 64-slot groups: lane's slot of group j, its key
     const int groups = bad ? 0 : (len + 63) / 64, per = (groups + SEL_W - 1) / SEL_W;
     const int first = wave * per * 64 + lane;

@@ -119,7 +119,7 @@ struct PagedEvictArgs {
     int n_kv, max_len, recent, sink;
     const int* lens;
     const int* keep;
-    const int* pos;             // null: recent and sink are 0
+    const int* pos;             // null: recent is 0
     float* score_out;
     int* slot_pos_out;
     int* new_lens;

@@ -108,6 +108,16 @@ def test_lengths_and_weights(weights, dtype, D):
         assert int(c.status) == 0
 
 
+@pytest.mark.parametrize("sink", [0, 30])
+def test_positions_without_the_next_one(sink):
+    """Positions kept, nothing recent protected: pos may be None, and then only the score and sink decide."""
+    c = Call([200, 77, 2100], [100, 30, 500], 3, 64, BF, sink=sink, seed=sink + 3)
+    c.dpos, c.pos = None, [math.inf] * 3
+    c.run()
+    c.check()
+    assert int(c.status) == 0
+
+
 @pytest.mark.parametrize("recent,sink", [(40, 0), (0, 30), (100, 20), (5000, 0), (0, 5000)])
 def test_protected_slots(recent, sink):
     """Also more of them than stay."""
