@@ -1,5 +1,6 @@
 """Refusals of the paged-cache and log-probability operators that need no GPU:
 every argument the host can check is checked before anything is enqueued."""
+import contextlib
 import ctypes
 import os
 
@@ -124,6 +125,14 @@ def test_struct_layout_matches_header():
             b.PbdPages.score.offset, b.PbdPages.status.offset) == (24, 48, 72, 80, 112)
 
 
+@contextlib.contextmanager
+def refused():
+    """A refusal for the argument's sake (host tensors alone are one, too)."""
+    with pytest.raises(b.PbdError) as e:
+        yield
+    assert "must be on a GPU" not in str(e.value)
+
+
 def test_binding_checks_shapes_and_types():
     """make_pages and the calls refuse tensors that do not hold what the library would read."""
     c = ref.Cache([40, 10], 2, 64, torch.bfloat16)
@@ -137,14 +146,14 @@ def test_binding_checks_shapes_and_types():
                      ((c.k, c.v, c.table), dict(score=score.double())), ((c.k, c.v, c.table), dict(score=score[:1])),
                      ((c.k, c.v, c.table), dict(slot_pos=pos, score=score[..., :9])), ((c.k[:, :, :40], c.v[:, :, :40], c.table), {}),
                      ((c.k, c.v, c.table), dict(status=torch.zeros(2, dtype=torch.int32)))]:
-        with pytest.raises(b.PbdError):
+        with refused():
             b.make_pages(*args, **ok, **kw)
     lens, q, out = torch.zeros(2, dtype=torch.int32), torch.zeros(2, 4, 64), torch.zeros(2, 4, 64)
     ws = torch.zeros(1 << 16, dtype=torch.uint8)
     for a in [(q[:1], lens, out, ws), (q.double(), lens, out, ws), (q, lens.long(), out, ws), (q, lens, out[:1], ws),
               (q.transpose(1, 2).contiguous().transpose(1, 2), lens, out, ws), (q, lens, out.bfloat16(), ws),
               (torch.zeros(3, 4, 64), torch.zeros(3, dtype=torch.int32), torch.zeros(3, 4, 64), ws)]:
-        with pytest.raises(b.PbdError):
+        with refused():
             b.pbd_paged_attention(pg, a[0], a[1], 48, a[2], a[3])
     k, rope = torch.zeros(2, 3, 128), torch.zeros(9, 32, 2)
     for a, kw in [((k, k[:, :2], lens, lens, rope), {}), ((k, k, lens, lens, rope[:, :16]), {}),
@@ -152,11 +161,32 @@ def test_binding_checks_shapes_and_types():
                   ((k, k, lens, lens, rope), dict(q=torch.zeros(2, 3, 128), q_out=torch.zeros(2, 3, 256))),
                   ((k, torch.zeros(2, 3, 256)[..., :128], lens, lens, rope), {}),
                   ((k, k, lens, lens, rope), dict(k_norm=torch.zeros(64)))]:
-        with pytest.raises(b.PbdError):
+        with refused():
             b.pbd_paged_append(pg, *a, **kw)
     x, t, lp = torch.zeros(4, 100), torch.zeros(4, dtype=torch.int32), torch.zeros(4)
     for a, kw in [((x.half(), t, lp, ws), {}), ((x, t.long(), lp, ws), {}), ((x, t, lp[:2], ws), {}),
                   ((x.t(), torch.zeros(100, dtype=torch.int32), torch.zeros(100), ws), {}),
                   ((x, t, lp, ws), dict(top_ids=torch.zeros(4, 3, dtype=torch.int32), top_logprobs=torch.zeros(4, 2)))]:
-        with pytest.raises(b.PbdError):
+        with refused():
             b.pbd_token_logprobs(*a, **kw)
+
+
+def test_host_tensors_and_layers_out_of_range():
+    c = ref.Cache([40, 10], 2, 64, torch.bfloat16)
+    pg = b.make_pages(c.k, c.v, c.table, n_q_heads=4, head_dim=64, score=torch.zeros(2, 2, 48))
+    lens, ws = torch.zeros(2, dtype=torch.int32), torch.zeros(1 << 16, dtype=torch.uint8)
+    k, rope = torch.zeros(2, 3, 128), torch.zeros(9, 32, 2)
+    for call in (lambda: b.pbd_paged_attention(pg, torch.zeros(2, 4, 64), lens, 48, torch.zeros(2, 4, 64), ws),
+                 lambda: b.pbd_paged_append(pg, k, k, lens, lens, rope),
+                 lambda: b.pbd_paged_evict(pg, lens, 48, lens, lens.clone(), ws),
+                 lambda: b.pbd_token_logprobs(torch.zeros(2, 100), lens, torch.zeros(2), ws)):
+        with pytest.raises(b.PbdError, match="must be on a GPU"):
+            call()
+    with refused():
+        b.layer_pages(pg, 0)
+    k, v = (torch.stack((t, t)) for t in (c.k, c.v))
+    both = b.make_pages(k, v, c.table, n_q_heads=4, head_dim=64)
+    assert b.layer_pages(both, 1).k == k[1].data_ptr() and b.layer_pages(both, 1).v == v[1].data_ptr()
+    for layer in (-1, 2):
+        with refused():
+            b.layer_pages(both, layer)
