@@ -263,3 +263,22 @@ def test_two_streams():
     torch.cuda.synchronize()
     for c in calls:
         c.check()
+
+
+@pytest.mark.parametrize("rows", [2, 300])
+def test_offsets_past_32_bits(rows):
+    """The last pages of pools of more than 2^31 elements take what a small pool's pages take."""
+    c = Call([3, 30], None, rows, 8, 1, 128, BF)
+    c.run()
+    small, n = c.pool, 2 ** 31 // (8 * 128 * 16) + 40
+    base = n - small[0].shape[0]
+    far = [torch.empty(n, 8, 16 * 128, dtype=BF, device=DEV) for _ in range(2)]
+    for f, first in zip(far, (c.k0, c.v0)):
+        f[base:] = first
+    table = c.pages.keep[2]
+    c.pages = pbd.make_pages(*far, torch.where(table < 0, table, table + base), n_q_heads=8, head_dim=128,
+                             status=c.status)
+    c.run()
+    assert int(c.status) == 0
+    for f, s in zip(far, small):
+        assert torch.equal(f[base:].view(torch.int16), s.view(torch.int16))

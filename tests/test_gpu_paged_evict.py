@@ -191,3 +191,23 @@ def test_captured_and_replayed():
         g.replay()
         torch.cuda.synchronize()
         c.check()
+
+
+def test_offsets_past_32_bits():
+    """The last pages of pools of more than 2^31 elements move as a small pool's pages do."""
+    c = Call([200, 90], [100, 41], 8, 128, BF, seed=4)
+    first = [t.clone() for t in c.pool]
+    c.run()
+    c.check()
+    n = 2 ** 31 // (8 * 128 * 16) + 40
+    base = n - first[0].shape[0]
+    far = [torch.empty(n, 8, 16 * 128, dtype=BF, device=DEV) for _ in range(2)]
+    for f, s in zip(far, first):
+        f[base:] = s
+    table = c.pages.keep[2]
+    c.pages = pbd.make_pages(*far, torch.where(table < 0, table, table + base), n_q_heads=8, head_dim=128,
+                             score=c.score, slot_pos=c.slot_pos, status=c.status)
+    c.run()
+    assert int(c.status) == 0
+    for f, s in zip(far, c.pool):
+        assert torch.equal(f[base:].view(torch.int16), s.view(torch.int16))

@@ -240,3 +240,11 @@ def test_captured_and_replayed():
         near(lp, want_lp, tl)
         near(best, want_best, tb)
         assert ids.tolist() == want_ids
+
+
+def test_rows_past_32_bits():
+    """Rows 2^29 elements apart, the last one 2^31 from the first."""
+    x, _ = logits(5, 1001, BF, seed=29)
+    far = torch.empty(4 * 2 ** 29 + 1001, dtype=BF, device=DEV).as_strided((5, 1001), (2 ** 29, 1))
+    far.copy_(x)
+    check(x, [3, 999, -1, 0, 1000], 7, dx=far, skip=(2,))
