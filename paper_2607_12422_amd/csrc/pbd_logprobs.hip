@@ -49,12 +49,15 @@ struct Stat {
 // What a wave's sums are relative to: exp2(x log2 e - r) is one fused product and
 // one exponential an element.  r is the maximum's x log2 e rounded; what the
 // rounding left is known exactly (at_max) and taken out of the sums at the end.
-// Maxima whose product could overflow are subtracted first (shift), and none or
-// an infinite one stand for 0.
+// It is at most half a step of r: below PLAIN in size the steps are 1/8 at most and
+// at_max 1/16.  It grows with the maximum (4e9, say a mask of minus that: 128), and
+// its exponential would overflow, so that larger maxima are subtracted from the
+// elements first (shift); none or an infinite one stand for 0.
+constexpr float PLAIN = 0x1p20f;
 struct Ref {
     float r, at_max, shift;
     __device__ __forceinline__ explicit Ref(float m) {
-        const bool plain = fabsf(m) < -LEAST;
+        const bool plain = fabsf(m) < PLAIN;
         r = plain ? m * LOG2E : 0.f;
         at_max = plain ? __builtin_fmaf(m, LOG2E, -r) : 0.f;
         shift = plain || isinf(m) ? 0.f : m;
@@ -224,7 +227,9 @@ __global__ __launch_bounds__(LP_T) void k_logprobs(LogprobArgs a, Part pt) {
             ref = Ref(top);
             if (m > -INFINITY) {
                 // lane 0 has the instance of the old maximum that the sums leave out
-                const float d = old.shift == 0.f && ref.shift == 0.f ? old.r - ref.r : fmaxf(m - top, LEAST) * LOG2E;
+                const float d = old.shift == 0.f && ref.shift == 0.f
+                                    ? old.r - ref.r
+                                    : fmaxf(m - top, LEAST) * LOG2E + (ref.at_max - old.at_max);
                 const float f = __builtin_amdgcn_exp2f(d), e = lane == 0 ? __builtin_amdgcn_exp2f(old.at_max) : 0.f;
                 t = f * (t + e * old.at_max + d * (s + e));
                 s = f * (s + e);

@@ -248,3 +248,91 @@ def test_rows_past_32_bits():
     far = torch.empty(4 * 2 ** 29 + 1001, dtype=BF, device=DEV).as_strided((5, 1001), (2 ** 29, 1))
     far.copy_(x)
     check(x, [3, 999, -1, 0, 1000], 7, dx=far, skip=(2,))
+
+
+MASKS = [-1e6, -1.2e6, -1e9, -4e9, -1e10, -1e12, -1e15, -1e20, -1e29, -2e30, -3e38]
+
+
+def masked_by(mask, R, V, dtype):
+    """Rows with a finite mask: a few tokens left, early, late, in the middle; half of them; none; the first tiles."""
+    x, t = logits(R, V, dtype, seed=7)
+    for r in range(R):
+        live = {0: [0, 1, 2], 1: [V - 3, V - 1], 2: [9000, 9001, 9007], 3: range(0, V, 2), 4: [], 5: range(9 * V // 10, V),
+                6: range(V // 100)}[r % 7]
+        live = torch.tensor(list(live), dtype=torch.long)
+        row = torch.full((V,), mask).to(dtype)
+        row[live] = x[r, live]
+        x[r] = row
+        if len(live) and r % 14 < 11:
+            t[r] = int(live[t[r] % len(live)])
+    return x, t
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("mask", MASKS)
+def test_finite_masks(mask, dtype):
+    """Masks that are numbers, as a constrained vocabulary has them, whole tiles and rows of them among the rest."""
+    x, t = masked_by(mask, 14, 40000, dtype)
+    check(x, t, 5)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("mask", MASKS)
+def test_finite_masks_of_many_rows(mask, dtype):
+    """The same where one work-group takes a whole row, tile after tile."""
+    x, t = masked_by(mask, 14, 40000, dtype)
+    many = x.to(DEV).repeat(40, 1)
+    a, _ = check(many[:14].cpu(), t, 5)
+    f = dict(device=DEV)
+    lp, H, best = torch.zeros(560, **f), torch.zeros(560, **f), torch.zeros(560, 5, **f)
+    ids = torch.zeros(560, 5, dtype=torch.int32, **f)
+    ws = torch.empty(pbd.pbd_token_logprobs_workspace_bytes(560, 40000, 5), dtype=torch.uint8, **f)
+    pbd.pbd_token_logprobs(many, torch.tensor(t * 40, dtype=torch.int32, **f), lp, ws, entropy=H, top_ids=ids,
+                           top_logprobs=best)
+    want_lp, want_H, want_ids, want_best, tl, th, tb = plain(x, t, 5)
+    for i in range(40):
+        at = slice(14 * i, 14 * i + 14)
+        near(lp[at], want_lp, tl)
+        near(H[at], want_H, th)
+        near(best[at], want_best, tb)
+        assert ids[at].tolist() == want_ids
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("size", [1e4, 2.0 ** 20, 1e9, 4e9, 1e20, 1e29, 3e38])
+def test_large_logits(size, dtype):
+    """Equal rows of a size, and rows that reach it once, in both signs."""
+    x = torch.full((6, 30000), size)
+    x[1] = -size
+    x[2] = 0.0
+    x[2, 20000] = size
+    x[3] = torch.linspace(-size, size, 30000, dtype=torch.float64).float()
+    x[4] = -x[3]
+    x[5, ::3] = -size
+    check(x.to(dtype), [5, 6, 20000, 29999, 0, 1], 8)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 16, 2.0 ** 18, 2.0 ** 20, 2.0 ** 22, 2.0 ** 30])
+def test_maxima_that_cross_a_size(size):
+    """Maxima that rise and fall from tile to tile past a power of two, in both signs, a row to a work-group."""
+    V, tile = 50000, 8192
+    g = torch.Generator().manual_seed(5)
+    step = max(2.0 ** -8, size * 2.0 ** -22)
+    base = (torch.arange(V) // tile).double()
+    rows = []
+    for sign in (1.0, -1.0):
+        for slope in (1.0, -1.0):
+            noise = torch.rand(2, V, generator=g, dtype=torch.float64) * -4.0
+            rows.append(sign * size + slope * (base - 3.0) + noise)
+    x = torch.cat(rows).div(step).round().mul(step).float()
+    x = x.repeat(65, 1)
+    check(x, torch.randint(0, V, (520,), generator=g).tolist(), 4)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("R", [1, 3])
+def test_ties_over_many_parts(R, dtype):
+    """A row of equal logits in more parts than the join has room to rank at once."""
+    x = torch.full((R, 151936), 0.5, dtype=dtype)
+    x[R - 1, :3] = -math.inf
+    check(x, [7] * R, 32)
