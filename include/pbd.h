@@ -418,8 +418,12 @@ int pbd_paged_append(const pbd_pages* pages, int32_t batch, int32_t max_new,
  * 16-byte aligned.  max_len: host bound on lens, in [1, table_width * page_size];
  * the work is laid out for it.  PBD_STATUS_CAPACITY: lens[b] outside [0, max_len].
  * Products and sums are held to fp32 rounding: a bf16 cache meets queries and
- * weights carried as three bf16 terms each.  Results are bitwise the same from run
- * to run, and do not depend on the other sequences of the batch but for its size.
+ * weights carried as three bf16 terms each.  Infinite and NaN elements of slots in
+ * use count as in fp32 arithmetic, in either type: a slot whose score is -inf has
+ * weight 0, an infinite value reaches its dim of every head that gives it a weight.
+ * Results are bitwise the same from run to run.  They depend on a sequence's own
+ * data, the batch's size, max_len and whether weights are accumulated, not on the
+ * other sequences.
  * ws: 16-byte aligned, of at least pbd_paged_attention_workspace_bytes (0 if
  * the arguments are invalid).
  */

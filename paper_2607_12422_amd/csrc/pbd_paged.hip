@@ -283,6 +283,9 @@ __global__ __launch_bounds__(256) void k_paged_append_few(PagedAppendArgs a) {
 // A bf16 cache: K and V are exact operands, and the query and the weights go in
 // as three bf16 terms each, which hold all 24 bits of their fp32 values, so that
 // the result has fp32 rounding only; the extra products hide behind the loads.
+// Where an element is infinite, the lower terms, which may be 0 or of the other
+// sign, make NaN of its products: a wave whose output has a NaN goes over its slots
+// again, with such scores and values from the first terms alone.
 // ---------------------------------------------------------------------------
 template <typename T, int HD> struct AttnShape;
 template <int HD> struct AttnShape<bf16, HD> {
@@ -295,14 +298,21 @@ template <int HD> struct AttnShape<float, HD> {
 };
 
 __device__ __forceinline__ void clear_past(uint2& v, int n) {      // keep the first n of four slots
-    if (n < 4) v.y &= n == 3 ? 0x0000ffffu : 0u;
-    if (n < 2) v.x &= n == 1 ? 0x0000ffffu : 0u;
+    v.y &= n >= 4 ? 0xffffffffu : n == 3 ? 0x0000ffffu : 0u;
+    v.x &= n >= 2 ? 0xffffffffu : n == 1 ? 0x0000ffffu : 0u;
 }
 __device__ __forceinline__ void clear_past(uint4& v, int n) {
     if (n < 4) v.w = 0u;
     if (n < 3) v.z = 0u;
     if (n < 2) v.y = 0u;
     if (n < 1) v.x = 0u;
+}
+
+// Two bf16 values, those that are not finite as 0.
+__device__ __forceinline__ unsigned finite_only(unsigned v) {
+    if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
+    if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
+    return v;
 }
 
 // Two floats cut to bf16 (toward zero): three such terms hold all 24 bits.
@@ -435,94 +445,130 @@ __global__ __launch_bounds__(256, 3) void k_paged_attn(PagedAttnArgs a) {
     f32x4 o[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < mine; ++j) {
-        const int slot0 = (blk0 + (wave + ATT_WAVES * j) * NB) * 16;
-        f32x4 sc[NB], lo[NB];
+    // again: scores and values that are not finite from the query's and the weights' first terms alone
+    for (bool again = false;;) {
+        for (int j = 0; j < mine; ++j) {
+            const int slot0 = (blk0 + (wave + ATT_WAVES * j) * NB) * 16;
+            f32x4 sc[NB], lo[NB];
 #pragma unroll
-        for (int c = 0; c < NB; ++c) sc[c] = lo[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int c = 0; c < NB; ++c) sc[c] = lo[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int c = 0; c < NB; ++c) {
-                mma_frag<T>(sc[c], kf[c][d], s_q[0][d][lane]);
-                if constexpr (TERMS == 3) {
-                    mma_frag<T>(lo[c], kf[c][d], s_q[1][d][lane]);
-                    mma_frag<T>(lo[c], kf[c][d], s_q[2][d][lane]);
+                for (int c = 0; c < NB; ++c) {
+                    mma_frag<T>(sc[c], kf[c][d], s_q[0][d][lane]);
+                    if constexpr (TERMS == 3) {
+                        mma_frag<T>(lo[c], kf[c][d], s_q[1][d][lane]);
+                        mma_frag<T>(lo[c], kf[c][d], s_q[2][d][lane]);
+                    }
+                }
+            mfma_settle();
+            if constexpr (TERMS == 3) {
+                if (__builtin_expect(again, false))
+#pragma unroll
+                    for (int c = 0; c < NB; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (isnan(sc[c][i] + lo[c][i])) lo[c][i] = 0.f;
+#pragma unroll
+                for (int c = 0; c < NB; ++c) sc[c] += lo[c];
+            }
+            if (j + 1 < mine) load_k(j + 1);
+            if (slot0 + 16 * NB > end) {
+#pragma unroll
+                for (int c = 0; c < NB; ++c) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (slot0 + 16 * c + 4 * g + i >= end) sc[c][i] = -INFINITY;
+                    // a masked slot may hold anything: its weight is 0, its value must be finite
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) clear_past(vf[c][t], end - (slot0 + 16 * c + 4 * g));
                 }
             }
-        mfma_settle();
-        if constexpr (TERMS == 3)
+            if (a.raw && col < nq) {
 #pragma unroll
-            for (int c = 0; c < NB; ++c) sc[c] += lo[c];
-        if (j + 1 < mine) load_k(j + 1);
-        if (slot0 + 16 * NB > end) {
-#pragma unroll
-            for (int c = 0; c < NB; ++c) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (slot0 + 16 * c + 4 * g + i >= end) sc[c][i] = -INFINITY;
-                // a masked slot may hold anything: its weight is 0, its value must be finite
-#pragma unroll
-                for (int t = 0; t < NT; ++t) clear_past(vf[c][t], end - (slot0 + 16 * c + 4 * g));
+                for (int c = 0; c < NB; ++c)
+                    if (slot0 + 16 * c < end)
+                        *(f32x4*)(a.raw + ((size_t)b * a.n_q + hq0 + col) * a.plan.len_pad + slot0 + 16 * c + 4 * g) = sc[c];
             }
-        }
-        if (a.raw && col < nq) {
+            float top = -INFINITY;
 #pragma unroll
             for (int c = 0; c < NB; ++c)
-                if (slot0 + 16 * c < end)
-                    *(f32x4*)(a.raw + ((size_t)b * a.n_q + hq0 + col) * a.plan.len_pad + slot0 + 16 * c + 4 * g) = sc[c];
-        }
-        float top = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < NB; ++c)
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[c][i]);
+            top = fmaxf(m, xrow_max(top));
+            if (__any(top > m)) {
+                const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+                l *= f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[c][i]);
-        top = fmaxf(m, xrow_max(top));
-        if (__any(top > m)) {
-            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-            l *= f;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) o[t] *= f;
-            m = top;
-        }
-        const float ref = m == -INFINITY ? 0.f : m;      // every score so far is -inf: weights 0
-        f32x4 p[NB];
-#pragma unroll
-        for (int c = 0; c < NB; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                p[c][i] = __builtin_amdgcn_exp2f(sc[c][i] - ref);
-                l += p[c][i];
+                for (int t = 0; t < NT; ++t) o[t] *= f;
+                m = top;
             }
-        if constexpr (TERMS == 3) {
-            // two blocks share a product of 32 slots
+            const float ref = m == -INFINITY ? 0.f : m;      // every score so far is -inf: weights 0
+            f32x4 p[NB];
 #pragma unroll
-            for (int c = 0; c < NB; c += 2) {
-                uint4 pt[TERMS];
+            for (int c = 0; c < NB; ++c)
 #pragma unroll
-                for (int u = 0; u < TERMS; ++u) {
-                    pt[u] = uint4{high_halves(p[c][0], p[c][1]), high_halves(p[c][2], p[c][3]),
-                                  high_halves(p[c + 1][0], p[c + 1][1]), high_halves(p[c + 1][2], p[c + 1][3])};
-#pragma unroll
-                    for (int k = c; k < c + 2; ++k)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) p[k][i] -= __uint_as_float(__float_as_uint(p[k][i]) & 0xffff0000u);
+                for (int i = 0; i < 4; ++i) {
+                    p[c][i] = __builtin_amdgcn_exp2f(sc[c][i] - ref);
+                    l += p[c][i];
                 }
+            if constexpr (TERMS == 3) {
+                // two blocks share a product of 32 slots
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const uint4 v = uint4{vf[c][t].x, vf[c][t].y, vf[c + 1][t].x, vf[c + 1][t].y};
+                for (int c = 0; c < NB; c += 2) {
+                    uint4 pt[TERMS];
 #pragma unroll
-                    for (int u = 0; u < TERMS; ++u) mma_frag<T>(o[t], v, pt[u]);
+                    for (int u = 0; u < TERMS; ++u) {
+                        pt[u] = uint4{high_halves(p[c][0], p[c][1]), high_halves(p[c][2], p[c][3]),
+                                      high_halves(p[c + 1][0], p[c + 1][1]), high_halves(p[c + 1][2], p[c + 1][3])};
+#pragma unroll
+                        for (int k = c; k < c + 2; ++k)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) p[k][i] -= __uint_as_float(__float_as_uint(p[k][i]) & 0xffff0000u);
+                    }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const uint4 v = uint4{vf[c][t].x, vf[c][t].y, vf[c + 1][t].x, vf[c + 1][t].y};
+                        mma_frag<T>(o[t], v, pt[0]);
+                    }
+                    if (__builtin_expect(again, false)) {
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            vf[c][t] = uint2{finite_only(vf[c][t].x), finite_only(vf[c][t].y)};
+                            vf[c + 1][t] = uint2{finite_only(vf[c + 1][t].x), finite_only(vf[c + 1][t].y)};
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const uint4 v = uint4{vf[c][t].x, vf[c][t].y, vf[c + 1][t].x, vf[c + 1][t].y};
+#pragma unroll
+                        for (int u = 1; u < TERMS; ++u) mma_frag<T>(o[t], v, pt[u]);
+                    }
                 }
+            } else {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int c = 0; c < NB; ++c) mma_k4(o[t], vf[c][t], p[c]);
             }
-        } else {
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int c = 0; c < NB; ++c) mma_k4(o[t], vf[c][t], p[c]);
+            mfma_settle();
+            if (j + 1 < mine) load_v(j + 1);
         }
-        mfma_settle();
-        if (j + 1 < mine) load_v(j + 1);
+        if constexpr (TERMS == 1) break;
+        f32x4 all[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) all[t] = NT > 4 ? o[t] + o[t + NT - 4] : o[t];
+        const f32x4 sum = (all[0] + all[1]) + (all[2] + all[3]);
+        const float one = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        if (__builtin_expect(again || !__any(col < nq && one != one), true)) break;
+        again = true;
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        load_k(0);
+        load_v(0);
     }
     l = xrow_sum(l);
     if (g == 0) {

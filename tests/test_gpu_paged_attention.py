@@ -230,3 +230,57 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for c in calls:
             c.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("gain", [0.0, 1.0])
+@pytest.mark.parametrize("n", [1, 40, 300, 2000])
+def test_infinite_values(n, gain, dtype):
+    """An infinite or NaN value reaches its dim, with its sign, and no other; weights of exactly 1 among them."""
+    cache = ref.Cache([n, n, n], 2, 64, dtype, seed=n)
+    odd = ((n // 2, 5, math.inf), (n - 1, 60, -math.inf), (0, 33, math.nan))
+    held = cache.dv.clone()
+    for b, (slot, dim, x) in enumerate(odd):
+        cache.dv[b, 0, slot, dim] = x
+        cache.put(b, 0, cache.dk[b, :, :n], cache.dv[b, :, :n])
+    for scored in (False, True):
+        c = Call(cache, 3, scored=scored, gain=gain)
+        c.run()
+        out = c.out.double().cpu()
+        cache.dv, odd_v = held, cache.dv
+        want = ref.attention(cache, c.q, 64 ** -0.5)
+        cache.dv = odd_v
+        for b, (slot, dim, x) in enumerate(odd):
+            near = (out[b] - want[b]["out"]).abs() <= want[b]["out_tol"]
+            assert torch.equal(out[b, :3, dim], torch.full((3,), x, dtype=torch.float64)) or \
+                (math.isnan(x) and torch.isnan(out[b, :3, dim]).all()), (b, out[b, :3, dim])
+            near[:3, dim] = True
+            assert torch.all(near), b
+            assert torch.all((c.lse[b].double().cpu() - want[b]["lse"]).abs() <= want[b]["lse_tol"])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [2, 40, 300, 2000])
+def test_slots_whose_score_is_minus_infinity(n, dtype):
+    """An infinite key element against queries of the other sign: weight 0, the others as if the slot were not there."""
+    cache = ref.Cache([n], 1, 64, dtype, seed=n)
+    slot = n // 2
+    held = cache.dk.clone()
+    cache.dk[0, 0, slot, 5] = -math.inf
+    cache.put(0, 0, cache.dk[0, :, :n], cache.dv[0, :, :n])
+    rest = [i for i in range(n) if i != slot]
+    for scored in (False, True):
+        c = Call(cache, 4, scored=scored)
+        c.q[:, :, 5] = c.q[:, :, 5].abs() + 0.1
+        c.dq.copy_(c.q)
+        c.run()
+        less = ref.Cache([n - 1], 1, 64, dtype)
+        less.dk, less.dv = held[:, :, rest], cache.dv[:, :, rest]
+        want = ref.attention(less, c.q, 64 ** -0.5)[0]
+        assert torch.all((c.out[0].double().cpu() - want["out"]).abs() <= want["out_tol"])
+        assert torch.all((c.lse[0].double().cpu() - want["lse"]).abs() <= want["lse_tol"])
+        if scored:
+            got, s0 = c.score[0, 0].double().cpu(), c.score0[0, 0].double()
+            assert got[slot] == s0[slot]
+            assert torch.all((got[rest] - s0[rest] - want["w"][0]).abs() <=
+                             want["w_tol"][0] + (s0[rest] + want["w"][0]) * ref.U)
