@@ -284,3 +284,39 @@ def test_slots_whose_score_is_minus_infinity(n, dtype):
             assert got[slot] == s0[slot]
             assert torch.all((got[rest] - s0[rest] - want["w"][0]).abs() <=
                              want["w_tol"][0] + (s0[rest] + want["w"][0]) * ref.U)
+
+
+def direct(dtype, scored):
+    """Sequences of at most 384 slots: without weights kept, attention in one launch."""
+    return Call(ref.Cache([100, 60, 50, 384], 2, 64, dtype, seed=8), 2, scored=scored, seed=8)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("scored", [False, True])
+def test_lengths_out_of_range_of_short_sequences(scored, dtype):
+    c = direct(dtype, scored)
+    assert c.max_len == 384
+    c.lens = torch.tensor([100, 385, -1, 384], dtype=torch.int32, device=DEV)
+    c.cache.lens = [100, 0, 0, 384]
+    c.run()
+    c.check(skip=(1, 2))
+    assert int(c.status) == pbd.PBD_STATUS_CAPACITY
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("scored", [False, True])
+def test_bad_pages_of_short_sequences(scored, dtype):
+    for at, bad in ((0, -1), (2, 10 ** 6), (3, 2 ** 31 - 1)):
+        c = direct(dtype, scored)
+        k, v, table = c.pages.keep[:3]
+        t = table.clone()
+        t[1, at] = bad
+        c.pages = pbd.make_pages(k, v, t, n_q_heads=4, head_dim=64, score=c.score, status=c.status)
+        c.run()
+        want = ref.attention(c.cache, c.q, 64 ** -0.5)
+        for b in (0, 2, 3):
+            assert torch.all((c.out[b].double().cpu() - want[b]["out"]).abs() <= want[b]["out_tol"])
+        assert torch.all(c.out[1] == 77.0) and torch.all(c.lse[1] == 77.0)
+        if scored:
+            assert torch.equal(c.score[1].cpu(), c.score0[1])
+        assert int(c.status) == pbd.PBD_STATUS_PAGE
