@@ -416,7 +416,7 @@ int pbd_paged_append(const pbd_pages* pages, int32_t batch, int32_t max_new,
  * q: float, heads contiguous, q_stride floats from a sequence to the next
  * (16-byte aligned, a multiple of 4).  out: float [batch][n_q_heads][head_dim],
  * 16-byte aligned.  max_len: host bound on lens, in [1, table_width * page_size];
- * the work is laid out for it.  PBD_STATUS_CAPACITY: lens[b] outside [0, max_len].
+ * the work is laid out for it (with scores, n_kv_heads * max_len below 2^34 - 2^24).  PBD_STATUS_CAPACITY: lens[b] outside [0, max_len].
  * Products and sums are held to fp32 rounding: a bf16 cache meets queries and
  * weights carried as three bf16 terms each.  Infinite and NaN elements of slots in
  * use count as in fp32 arithmetic, in either type: a slot whose score is -inf has
@@ -445,7 +445,7 @@ int pbd_paged_attention(const pbd_pages* pages, int32_t batch, const float* q, i
  * receive the first new-length entries, in the layout of score; each may be
  * the cache's own array or must not overlap it.  new_lens[b] receives the new
  * length; it may be lens.  max_len: host bound on lens, in [1, table_width *
- * page_size].  PBD_STATUS_CAPACITY: lens[b] outside [0, max_len] or keep[b] < 0.
+ * page_size], at most 2^30 - 4096.  PBD_STATUS_CAPACITY: lens[b] outside [0, max_len] or keep[b] < 0.
  * The pages of the sequences must not be shared.
  */
 size_t pbd_paged_evict_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t max_len);
@@ -469,7 +469,8 @@ int pbd_paged_evict(const pbd_pages* pages, int32_t batch, const int32_t* lens, 
  * NaN or +inf has NaN logprob, entropy and top log probabilities.  The sums are
  * taken relative to the row's maximum and without it, so that values near zero
  * keep their precision.  Bitwise the same from run to run.
- * ws: 16-byte aligned.
+ * rows and vocab are at most 2^22 each; rows * ceil((vocab + 7) / 163840) is below
+ * 2^24.  ws: 16-byte aligned.
  */
 size_t pbd_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top_n);
 int pbd_token_logprobs(int32_t rows, int32_t vocab, int32_t dtype, const void* logits, int64_t row_stride,

@@ -1309,6 +1309,7 @@ size_t pbd_decode_paged_workspace_bytes(const pbd_ctx* c, const pbd_pages* pages
     if (!c || batch < 1 || batch > c->cfg.max_batch || max_len < 1 || check_pages(pages, batch, max_len, msg)) return 0;
     const PagedAttnPlan plan = paged_attn_plan(pages->dtype, pages->n_q_heads, pages->n_kv_heads, pages->head_dim,
                                                batch, max_len, pages->score != nullptr);
+    if (plan.join_groups > GROUPS_MAX) return 0;
     return align_up(plan.bytes, 256) + align_up((size_t)batch * 3 * sizeof(int), 256);
 }
 
@@ -1336,8 +1337,9 @@ int pbd_decode_paged(pbd_ctx* c, const pbd_pages* pages, int32_t batch, int32_t*
         return fail(c, PBD_ERR_INVALID_ARG, "a single token takes no mask flag");
     bool adapter, causal;
     if ((rc = resolve_flags(c, flags, false, true, adapter, causal))) return rc;
-    if (ws_bytes < pbd_decode_paged_workspace_bytes(c, pages, batch, max_len))
-        return fail(c, PBD_ERR_CAPACITY, "workspace smaller than pbd_decode_paged_workspace_bytes");
+    const size_t need = pbd_decode_paged_workspace_bytes(c, pages, batch, max_len);
+    if (need == 0) return fail(c, PBD_ERR_CAPACITY, "max_len times n_kv_heads is too much for a cache with scores");
+    if (ws_bytes < need) return fail(c, PBD_ERR_CAPACITY, "workspace smaller than pbd_decode_paged_workspace_bytes");
     PagedPass pp{};
     pp.pages = pages;
     pp.max_len = max_len;

@@ -483,6 +483,10 @@ size_t logprob_ws_bytes(int rows, int vocab, int top_n) {
     return p.parts == 1 ? 16 : (size_t)rows * p.parts * (top_n * sizeof(u64) + sizeof(Stat));
 }
 
+long long logprob_groups(int rows, int vocab, int top_n) {
+    return (long long)rows * plan(rows, vocab, top_n, nullptr).parts;
+}
+
 hipError_t launch_logprobs(int dtype, const LogprobArgs& a, hipStream_t st) {
     const Part p = plan(a.rows, a.vocab, a.top_n, a.ws);
     const dim3 grid((unsigned)a.rows * p.parts);

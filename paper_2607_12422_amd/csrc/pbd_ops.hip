@@ -14,6 +14,7 @@ namespace {
 
 constexpr int BATCH_MAX = 65535;             // the grids' third dimension
 constexpr long long SLOTS_MAX = 1ll << 30;
+constexpr int EVICT_SLOTS_MAX = (int)SLOTS_MAX - 4096;   // a work-group moves 64 slots: fewer than GROUPS_MAX of them
 
 bool aligned(const void* p, size_t n) { return ((size_t)p & (n - 1)) == 0; }
 
@@ -113,8 +114,9 @@ int pbd_paged_append(const pbd_pages* pages, int32_t batch, int32_t max_new, con
 
 size_t pbd_paged_attention_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t max_len) {
     if (pages_ok(pages, batch, max_len) || max_len < 1) return 0;
-    return paged_attn_plan(pages->dtype, pages->n_q_heads, pages->n_kv_heads, pages->head_dim, batch, max_len,
-                           pages->score != nullptr).bytes;
+    const PagedAttnPlan plan = paged_attn_plan(pages->dtype, pages->n_q_heads, pages->n_kv_heads, pages->head_dim, batch,
+                                               max_len, pages->score != nullptr);
+    return plan.join_groups > GROUPS_MAX ? 0 : plan.bytes;
 }
 
 int pbd_paged_attention(const pbd_pages* pages, int32_t batch, const float* q, int64_t q_stride, const int32_t* lens,
@@ -132,6 +134,7 @@ int pbd_paged_attention(const pbd_pages* pages, int32_t batch, const float* q, i
     PagedAttnArgs a{};
     a.plan = paged_attn_plan(pages->dtype, pages->n_q_heads, pages->n_kv_heads, pages->head_dim, batch, max_len,
                              pages->score != nullptr);
+    if (a.plan.join_groups > GROUPS_MAX) return op_fail(PBD_ERR_CAPACITY, "max_len times n_kv_heads is too much for a cache with scores");
     if (ws_bytes < a.plan.bytes) return op_fail(PBD_ERR_CAPACITY, "workspace smaller than pbd_paged_attention_workspace_bytes");
     a.pg = page_view(*pages);
     a.n_q = pages->n_q_heads; a.n_kv = pages->n_kv_heads; a.max_len = max_len;
@@ -148,7 +151,7 @@ int pbd_paged_attention(const pbd_pages* pages, int32_t batch, const float* q, i
 }
 
 size_t pbd_paged_evict_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t max_len) {
-    if (pages_ok(pages, batch, max_len) || max_len < 1) return 0;
+    if (pages_ok(pages, batch, max_len) || max_len < 1 || max_len > EVICT_SLOTS_MAX) return 0;
     return evict_count_offset(*pages, batch, max_len) + up256((size_t)batch * (pages->n_kv_heads + 1) * sizeof(int));
 }
 
@@ -158,6 +161,7 @@ int pbd_paged_evict(const pbd_pages* pages, int32_t batch, const int32_t* lens, 
     int rc = pages_ok(pages, batch, max_len);
     if (rc) return rc;
     if (max_len < 1) return op_fail(PBD_ERR_INVALID_ARG, "max_len must be >= 1");
+    if (max_len > EVICT_SLOTS_MAX) return op_fail(PBD_ERR_CAPACITY, "max_len is too much for an eviction");
     if (!lens || !keep || !score_out || !new_lens || !ws) return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
     if (!pages->score) return op_fail(PBD_ERR_INVALID_ARG, "the cache has no score");
     if (recent < 0 || sink < 0) return op_fail(PBD_ERR_INVALID_ARG, "recent and sink must be >= 0");
@@ -184,6 +188,7 @@ static int logprob_sizes_ok(int32_t rows, int32_t vocab, int32_t top_n) {
     if (rows < 1 || rows > (1 << 22)) return op_fail(PBD_ERR_INVALID_ARG, "rows outside [1, 2^22]");
     if (vocab < 1 || vocab > (1 << 22)) return op_fail(PBD_ERR_INVALID_ARG, "vocab outside [1, 2^22]");
     if (top_n < 0 || top_n > 32) return op_fail(PBD_ERR_INVALID_ARG, "top_n outside [0, 32]");
+    if (logprob_groups(rows, vocab, top_n) > GROUPS_MAX) return op_fail(PBD_ERR_CAPACITY, "rows times vocab is too much for one call");
     return PBD_OK;
 }
 

@@ -62,6 +62,9 @@ struct PageView {
 
 PageView page_view(const pbd_pages& p);
 
+// Work-groups of 256 threads that a launch may have along a dimension: fewer than 2^32 threads.
+constexpr long long GROUPS_MAX = (1ll << 24) - 1;
+
 struct PagedAppendArgs {
     PageView pg;
     int n_q, n_kv, max_new, rope_len;
@@ -88,6 +91,7 @@ struct PagedAttnPlan {
     int splits;                 // splits of max_len slots
     bool direct;                // one split and no weights kept: it writes the output, no join
     int len_pad;                // slots per row of the kept raw scores
+    long long join_groups;      // work-groups of the join for a sequence
     size_t off_ml, off_raw, bytes;   // workspace: partial outputs first
 };
 PagedAttnPlan paged_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int max_len, bool scored);
@@ -146,6 +150,7 @@ struct LogprobArgs {
     char* ws;
 };
 size_t logprob_ws_bytes(int rows, int vocab, int top_n);
+long long logprob_groups(int rows, int vocab, int top_n);    // work-groups of its largest launch
 hipError_t launch_logprobs(int dtype, const LogprobArgs& a, hipStream_t st);
 
 // The decode pass: which sequences take part, and their advance afterwards.

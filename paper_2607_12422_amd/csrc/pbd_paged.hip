@@ -839,6 +839,7 @@ PagedAttnPlan paged_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int ba
     p.splits = (max_len + p.kps - 1) / p.kps;
     p.direct = p.splits == 1 && !scored;
     p.len_pad = (max_len + 15) / 16 * 16;
+    p.join_groups = n_q + (scored ? ((long long)max_len + SCORE_SLOTS - 1) / SCORE_SLOTS * n_kv : 0);
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     const size_t rows = p.direct ? 0 : (size_t)batch * n_q * p.splits;
     p.off_ml = up(rows * head_dim * 4);
@@ -853,9 +854,8 @@ hipError_t launch_paged_attn_splits(int dtype, int head_dim, const PagedAttnArgs
 }
 
 hipError_t launch_paged_attn_join(int dtype, int head_dim, const PagedAttnArgs& a, int batch, hipStream_t st) {
-    const int chunks = a.raw ? (a.max_len + SCORE_SLOTS - 1) / SCORE_SLOTS : 0;
     if (a.plan.direct) return hipSuccess;
-    PBD_BY_TYPE(k_paged_join, dim3(a.n_q + chunks * a.n_kv, batch));
+    PBD_BY_TYPE(k_paged_join, dim3((unsigned)a.plan.join_groups, batch));
 }
 #undef PBD_BY_TYPE
 

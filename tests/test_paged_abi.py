@@ -190,3 +190,21 @@ def test_host_tensors_and_layers_out_of_range():
     for layer in (-1, 2):
         with refused():
             b.layer_pages(both, layer)
+
+
+def test_launches_past_the_largest_grid(lib):
+    """Sizes within the other limits whose launches would have 2^32 threads or more: refused before anything runs."""
+    far = dict(page_size=4096, table_width=1 << 18, slot_stride=1 << 30, page_stride=4096 * 64 * 16, head_stride=4096 * 64)
+    big = dict(far, n_kv_heads=16, n_q_heads=16)
+    n = 1 << 30
+    assert attention(lib, pages(**big), batch=1, q_stride=1024, max_len=n) == CAP
+    assert b.pbd_last_error()
+    assert b.pbd_paged_attention_workspace_bytes(pages(**big), 1, n) == 0
+    assert b.pbd_paged_attention_workspace_bytes(pages(**big), 1, n - 2048) > 0
+    assert b.pbd_paged_attention_workspace_bytes(pages(**dict(big, score=0)), 1, n) > 0
+    assert evict(lib, pages(**far), batch=1, max_len=n) == CAP
+    assert b.pbd_paged_evict_workspace_bytes(pages(**far), 1, n) == 0
+    assert b.pbd_paged_evict_workspace_bytes(pages(**far), 1, n - 4096) > 0
+    assert logprobs(lib, rows=1 << 22, vocab=1 << 20, stride=1 << 20) == CAP
+    assert b.pbd_token_logprobs_workspace_bytes(1 << 22, 1 << 20, 1) == 0
+    assert b.pbd_token_logprobs_workspace_bytes(1 << 22, 152000, 1) > 0
