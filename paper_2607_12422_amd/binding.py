@@ -564,6 +564,7 @@ class Engine:
                          flags: int = PBD_PASS_DEFAULT, stream=None):
         """token, pos, cache_len int32 [batch], advanced by the call; logits float32 [batch, vocab]."""
         B, dev = token.numel(), pages.device
+        _need(dev == self.kv.get_device(), "the cache must be on the context's device")
         _need(B <= pages.rows, "the table has fewer rows than token")
         _need(pages.layers in (None, self.cfg.n_layers), "the cache has not the model's layers")
         w, wb = _space(ws, dev)

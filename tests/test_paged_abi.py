@@ -208,3 +208,37 @@ def test_launches_past_the_largest_grid(lib):
     assert logprobs(lib, rows=1 << 22, vocab=1 << 20, stride=1 << 20) == CAP
     assert b.pbd_token_logprobs_workspace_bytes(1 << 22, 1 << 20, 1) == 0
     assert b.pbd_token_logprobs_workspace_bytes(1 << 22, 152000, 1) > 0
+
+
+def test_decoding_over_a_cache_on_another_device():
+    """The context's buffers lie on its own device: a cache on another one is refused."""
+    class On:
+        """Stands for an int32 tensor on a device."""
+        dtype, nbytes = torch.int32, 1 << 20
+
+        def __init__(self, device):
+            self.device = device
+
+        def numel(self):
+            return 2
+
+        def get_device(self):
+            return self.device
+
+        def is_contiguous(self):
+            return True
+
+        def data_ptr(self):
+            return P
+
+    class Tiny:
+        n_layers, vocab = 1, 100
+
+    c = ref.Cache([40, 10], 2, 64, torch.bfloat16)
+    pg = b.make_pages(c.k, c.v, c.table, n_q_heads=4, head_dim=64)
+    pg.device = 1
+    eng = object.__new__(b.Engine)
+    eng.lib, eng.ctx, eng.cfg, eng.kv = b.load_library(), None, Tiny, On(0)
+    t = [On(1) for _ in range(3)]
+    with pytest.raises(b.PbdError, match="context's device"):
+        eng.pbd_decode_paged(pg, *t, 48, On(1))
