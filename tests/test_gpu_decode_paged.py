@@ -279,3 +279,53 @@ def test_invalid_sequences_are_skipped():
     was = kv.view(s.dtype).view_as(s.dense)
     assert torch.equal(s.dense[:, :, 1:], was[:, :, 1:]) and not torch.equal(s.dense[:, :, 0], was[:, :, 0])
     s.g.close()
+
+
+def test_refusals_on_a_live_context():
+    """What the host can see is refused before anything runs: tokens, lengths, caches and the status stay."""
+    import ctypes
+    s = Server(TINY, [40, 30], own_pool=32)
+    lib, ctx = s.eng.lib, s.eng.ctx
+    INV, SHAPE, CAP = pbd.PBD_ERR_INVALID_ARG, pbd.PBD_ERR_SHAPE, pbd.PBD_ERR_CAPACITY
+    n, most = s.ws.numel(), s.pages.table_width * s.page
+    before = [t.clone() for t in (s.token, s.pos, s.len, s.pool, s.eng.kv, s.score, s.slot_pos, s.logits)]
+
+    def call(batch=2, token=s.token.data_ptr(), pos=s.pos.data_ptr(), length=s.len.data_ptr(), max_len=s.cap, flags=0,
+             logits=s.logits.data_ptr(), ws=s.ws.data_ptr(), size=n, **kw):
+        p = pbd.PbdPages.from_buffer_copy(s.pages)
+        for k, x in kw.items():
+            setattr(p, k, x)
+        return lib.pbd_decode_paged(ctx, ctypes.byref(p), batch, token, pos, length, max_len, flags, logits, ws, size, None)
+
+    other = s.pages.state_layer_stride
+    for kw, code in [(dict(batch=0), INV), (dict(batch=3), CAP), (dict(token=None), INV), (dict(pos=None), INV),
+                     (dict(length=None), INV), (dict(ws=None), INV), (dict(token=s.pos.data_ptr()), INV),
+                     (dict(length=s.pos.data_ptr()), INV), (dict(length=s.token.data_ptr()), INV), (dict(max_len=0), INV),
+                     (dict(max_len=most + 1), CAP), (dict(max_len=-1), CAP), (dict(ws=s.ws.data_ptr() + 8), INV),
+                     (dict(size=n - 1), CAP), (dict(flags=pbd.PBD_PASS_MASK_BLOCK), INV),
+                     (dict(flags=pbd.PBD_PASS_MASK_CAUSAL), INV),
+                     (dict(flags=pbd.PBD_PASS_ADAPTER_ON | pbd.PBD_PASS_ADAPTER_OFF), INV), (dict(flags=1 << 30), INV),
+                     (dict(dtype=pbd.PBD_DTYPE_BF16), SHAPE), (dict(n_q_heads=2 * TINY.n_q_heads), SHAPE),
+                     (dict(n_kv_heads=1, n_q_heads=TINY.n_q_heads), SHAPE), (dict(head_dim=128), SHAPE),
+                     (dict(layer_stride=0), INV), (dict(layer_stride=-1024), INV), (dict(layer_stride=1000), INV),
+                     (dict(state_layer_stride=0), INV), (dict(state_layer_stride=-other), INV),
+                     (dict(k=None), INV), (dict(table=None), INV), (dict(page_size=24), SHAPE), (dict(n_pages=0), INV),
+                     (dict(slot_stride=s.cap - 1), CAP)]:
+        assert call(**kw) == code, kw
+        assert pbd.pbd_last_error(ctx)
+    # the binding's own: a table of fewer sequences, another number of layers, types
+    for args, kw in [((torch.cat((s.token, s.token)), s.pos, s.len), {}), ((s.token, s.pos.long(), s.len), {}),
+                     ((s.token, s.pos, s.len[:1]), {}), ((s.token, s.pos, s.len), dict(logits=s.logits[:1])),
+                     ((s.token, s.pos, s.len), dict(logits=s.logits.double()))]:
+        with pytest.raises(pbd.PbdError):
+            s.eng.pbd_decode_paged(s.pages, *args, s.cap, s.ws, **kw)
+    few = pbd.make_pages(s.pool[0][:1], s.pool[1][:1], s.table, n_q_heads=TINY.n_q_heads, head_dim=s.D)
+    with pytest.raises(pbd.PbdError):
+        s.eng.pbd_decode_paged(few, s.token, s.pos, s.len, s.cap, s.ws)
+    torch.cuda.synchronize()
+    bits = lambda t: t.contiguous().view(torch.uint8)
+    for t, t0 in zip((s.token, s.pos, s.len, s.pool, s.eng.kv, s.score, s.slot_pos, s.logits), before):
+        assert torch.equal(bits(t), bits(t0))
+    assert s.g.status() == 0
+    s.step()
+    s.g.close()
