@@ -17,8 +17,8 @@
 //
 // An element's vector instructions (conversion, maxima, an exponential, two sums) and
 // its load bound a pass about equally: 1024 rows of 151936 bf16 logits, as many as run
-// at once, take 69 us (4.5 TB/s), 2048 take 124 (5.0 TB/s); 1056 take 84, the last 32
-// rows alone.  Few rows take a part's latency and a join's: 17 rows of fp32 10 and 7
+// at once, take 69 us (4.5 TB/s), 2048 take 124 (5.0 TB/s); 1056 take 83 to 84 (90 in
+// the first hundred calls of a program), the last 32 rows alone.  Few rows take a part's latency and a join's: 17 rows of fp32 10 and 7
 // us.
 #include "pbd_device.h"
 #include "pbd_launch.h"

@@ -276,7 +276,7 @@ __global__ __launch_bounds__(256) void k_paged_append_few(PagedAppendArgs a) {
 // The products do 4 * 16 * head_dim flops a slot on matrix cores whatever the
 // number of heads that share a KV head, so that the cache's bytes are the bound:
 // 32 sequences of 8192 slots, 8 heads of 128 in bf16 (1.07 GB, weights kept) take
-// 174 to 186 us, 5.8 to 6.2 TB/s; 24 of 256 to 4096 slots (107 MB) 22 us, where the
+// 174 to 187 us, 5.7 to 6.2 TB/s; 24 of 256 to 4096 slots (107 MB) 22 us, where the
 // last work-groups run alone; one of 4096 (17 MB) 7 us, most of it the waits of one
 // split for its pages, its K and its V.
 //
@@ -611,7 +611,8 @@ __global__ __launch_bounds__(256, 3) void k_paged_attn(PagedAttnArgs a) {
 // same sums whatever ran first.  Work-groups past them (weights accumulated):
 // SCORE_SLOTS slots of one KV head each, whose kept scores become weights under
 // the head's whole sum.  3.5 us for one sequence, 10 with 32 times 8192 slots'
-// weights (kept scores of two query heads a KV head: 33 MB in, 17 in and out).
+// weights (two query heads a KV head: 17 MB of kept scores in, 8 MB of weights in and
+// out).
 constexpr int SCORE_SLOTS = 1024;
 
 template <typename T, int HD>
@@ -819,12 +820,15 @@ hipError_t launch_paged_append(int dtype, int head_dim, const PagedAppendArgs& a
 
 constexpr int KPS_MAX = 4096;     // a wave's lanes hold the addresses of 64 blocks of 16 slots, the four waves of 256
 // Work-groups wanted; 768 run at once, and an uneven batch leaves some with nothing to
-// do (24 sequences of 256 to 4096 slots: 26 us; 30 to 31 with 512, 768, 1536 or 2048).
+// do (24 sequences of 256 to 4096 slots: 26 us; 30 to 31 with 512, 768, 1536 or 2048;
+// of uneven batches only this one was measured).
 constexpr int ATT_GROUPS = 1024;
 // Slots up to which one work-group takes a whole sequence and no join follows
 // (captured: 16 / 8 heads of 128 in bf16, 384 slots 7.0 us against 8.0 split, 512
 // slots 8.0 and 8.0, 768 9.9 and 8.1; 4 / 2 heads of 64 in fp32, 128 slots 4.6 and
-// 6.5, 384 8.2 and 6.8, but called one by one 7.0 and 9.0: a launch less).
+// 6.5, 384 8.2 and 6.8, but called one by one 7.0 and 9.0: a launch less).  One bound
+// for both types, the better one for calls; a captured pass over an fp32 cache pays for
+// it, up to 1.4 us a layer, from about 280 slots on (by those times).
 constexpr int DIRECT_LEN = 384;
 
 PagedAttnPlan paged_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int max_len, bool scored) {
