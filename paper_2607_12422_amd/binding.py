@@ -288,7 +288,8 @@ _torch = _LazyTorch()
 def make_pages(k, v, table, n_q_heads: int, head_dim: int, score=None, slot_pos=None, status=None) -> PbdPages:
     """pbd_pages of a cache of one layer, k and v [n_pages][n_kv_heads][page_size * head_dim], or of several,
     [layers][n_pages][...]; table int32 [batch][pages]; score float32 and slot_pos int32 [batch][n_kv_heads][slots]
-    (layers first where k has them).  Pages and heads may have any strides, a page of a head is contiguous."""
+    (layers first where k has them).  Pages and heads may have any strides, a page of a head is contiguous.  status
+    int32 [1]: without it a sequence with a bad length or page is skipped silently."""
     _need(k.dim() in (3, 4) and v.shape == k.shape and v.dtype == k.dtype and v.stride() == k.stride(),
           "k and v must be alike, [n_pages][n_kv_heads][page_size * head_dim], layers first")
     _need(k.stride(-1) == 1, "a page of a head must be contiguous")
@@ -424,7 +425,8 @@ def pbd_token_logprobs_workspace_bytes(rows: int, vocab: int, top_n: int) -> int
 def pbd_token_logprobs(logits, tokens, logprob, ws, entropy=None, top_ids=None, top_logprobs=None, status=None,
                        stream=None):
     """logits float32 or bfloat16 [..., vocab] (rows at one stride), tokens int32 [rows] (-1: padding) and logprob
-    float32 [rows], or both None; entropy float32 [rows]; top_ids int32 and top_logprobs float32 [rows, n]."""
+    float32 [rows], or both None; entropy float32 [rows]; top_ids int32 and top_logprobs float32 [rows, n]; status
+    int32 [1]: without it a row with a bad token is skipped silently."""
     dev = logits.get_device()
     x = logits if logits.dim() == 2 else logits.view(-1, logits.shape[-1])
     R, V = x.shape
