@@ -86,6 +86,7 @@ typedef void* pbd_stream_t;            /* hipStream_t */
 #define PBD_STATUS_TIMEOUT   8         /* a bounded wait of the persistent batch-1 pass gave up:
                                           that pass's outputs are invalid */
 #define PBD_STATUS_PAGE     16         /* a page id outside [0, n_pages) among the pages a sequence uses */
+#define PBD_STATUS_TREE     32         /* a tree node whose parent is neither -1 nor a node before it */
 
 /*
  * Model and capacity description.  The backbone is a Qwen3-style decoder
@@ -367,7 +368,7 @@ typedef struct pbd_pages {
     int32_t n_pages;            /* page ids lie in [0, n_pages) */
     int64_t page_stride;        /* elements */
     int64_t head_stride;        /* elements */
-    int64_t layer_stride;       /* elements from a layer's cache to the next (pbd_decode_paged only) */
+    int64_t layer_stride;       /* elements from a layer's cache to the next (pbd_decode_paged, pbd_tree_commit) */
     void* k;
     void* v;
     const int32_t* table;       /* [batch][table_width] */
@@ -510,6 +511,145 @@ size_t pbd_decode_paged_workspace_bytes(const pbd_ctx* ctx, const pbd_pages* pag
 int pbd_decode_paged(pbd_ctx* ctx, const pbd_pages* pages, int32_t batch, int32_t* token, int32_t* pos,
                      int32_t* cache_len, int32_t max_len, uint32_t flags, float* logits,
                      void* ws, size_t ws_bytes, pbd_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Packed rows over a paged cache: new rows of many sequences in one call, each
+ * sequence's behind those of the one before, without padding.  Whole prompts,
+ * chunks of prompts behind a cached part, and trees of drafted tokens are all
+ * such rows: a plan gives them pages and slots, an append brings them into the
+ * cache, one of the two attentions reads it, and a tree's accepted path is kept.
+ * Rows of sequence b are row_start[b] .. row_start[b + 1] - 1 (row_start: device
+ * int32 [batch + 1], ascending from 0); `rows` is a host bound on row_start[batch]
+ * that the work is laid out for, at most 2^22.  After their append they are the last
+ * slots of the lens[b] that the sequence then has.  Conventions, errors and
+ * workspaces are those of the operators above.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Pages for new rows, and their slots.  table (device int32 [batch][table_width])
+ * holds seq_pages[b] pages of sequence b; free_pages (device int32 [n_pages]) is a
+ * stack of free ones, the first *n_free of it.  Sequence b has lens[b] slots in use,
+ * all of them in its pages, and gets n_new[b] more: pages that it lacks for
+ * lens[b] + n_new[b] are taken from the top of the stack, the sequences in order, the
+ * lower pages of a sequence first.  A sequence is served if its and the earlier ones'
+ * demand is met together, or if it needs no page.
+ * Results: table, seq_pages and *n_free, in place; row_start; for every packed row r
+ * below max_rows slot_map[r] = page id * page_size + place in the page, and, where they
+ * are wanted, row_seq[r] = its sequence and row_pos[r] = pos[b] + its number among the
+ * sequence's rows (NULL: not wanted; pos and row_pos go together); new_lens[b] =
+ * lens[b] + n_new[b].  Rows behind the last sequence have slot and sequence -1,
+ * position 0.  A sequence that is not served, whose lens, n_new or seq_pages is out of
+ * range, or whose rows do not end within max_rows, raises PBD_STATUS_CAPACITY: it keeps
+ * its pages, its rows (there for n_new > 0, within max_rows) have slot -1 and
+ * new_lens[b] is lens[b].  A page id outside [0, n_pages) among those to be taken raises
+ * PBD_STATUS_PAGE and nobody who needs a page is served.
+ * page_size: as in pbd_pages; n_pages * page_size below 2^31; max_rows in [0, 2^22].
+ * row_start, new_lens and the other outputs overlap no input but the three in place.
+ * A table, its stack and counts belong to one call at a time.
+ */
+int pbd_page_plan(int32_t batch, int32_t page_size, int32_t n_pages, int32_t* table, int32_t table_width,
+                  int32_t* seq_pages, const int32_t* free_pages, int32_t* n_free,
+                  const int32_t* lens, const int32_t* n_new, const int32_t* pos, int32_t max_rows,
+                  int32_t* row_start, int32_t* row_seq, int32_t* row_pos, int32_t* slot_map, int32_t* new_lens,
+                  int32_t* status, pbd_stream_t stream);
+
+/*
+ * Pages given back: sequence b keeps those of its first keep[b] slots (0: none), and the
+ * others return to the stack, in the order that undoes a plan's taking.  Their table
+ * entries become -1, seq_pages[b] what is left.  keep[b] < 0 or seq_pages[b] out of range
+ * (PBD_STATUS_CAPACITY) or a page id out of range among those to go (PBD_STATUS_PAGE):
+ * the sequence keeps all.  More pages than the stack has room for: PBD_STATUS_CAPACITY,
+ * and nothing is given back.  A page goes back once: one that sequences share is the
+ * caller's to count.
+ */
+int pbd_page_release(int32_t batch, int32_t page_size, int32_t n_pages, int32_t* table, int32_t table_width,
+                     int32_t* seq_pages, int32_t* free_pages, int32_t* n_free, const int32_t* keep,
+                     int32_t* status, pbd_stream_t stream);
+
+/*
+ * Append of packed rows: row r's k and v go to slot slot_map[r] (a plan's: page id *
+ * page_size + place), its heads normalised and rotated as pbd_paged_append does, by row
+ * row_pos[r] of rope; its q (NULL: none) goes to q_out [rows][n_q_heads * head_dim], in
+ * elements of pages->dtype, rounded once.  Rows may stand at any positions: a tree's
+ * nodes stand at their depths.  A row whose slot is negative is skipped: it is not read
+ * and its q_out row stays as it was.  So is one whose slot lies in no page
+ * (PBD_STATUS_PAGE) or whose position is outside rope (PBD_STATUS_CAPACITY).  Two rows
+ * with one slot: either's values, also mixed.  A cache that keeps score or slot_pos is
+ * refused (PBD_ERR_UNSUPPORTED): a slot does not say whose state it has.  Alignment as
+ * pbd_paged_append; rows in [0, 2^22]; n_pages * page_size below 2^31; pages->table is
+ * not read.
+ */
+int pbd_paged_append_rows(const pbd_pages* pages, int32_t rows, const float* q, const float* k, const float* v,
+                          int64_t row_stride, const int32_t* slot_map, const int32_t* row_pos,
+                          const void* q_norm, const void* k_norm, float eps, const float* rope, int32_t rope_len,
+                          void* q_out, pbd_stream_t stream);
+
+/*
+ * Causal attention of packed rows: with n = row_start[b + 1] - row_start[b], row i of
+ * sequence b attends to the slots j <= lens[b] - n + i of its cache.  Whole prompts have
+ * lens[b] = n; smaller n are the last chunk of a longer one.  q and out: elements of
+ * pages->dtype; q [rows], n_q_heads * head_dim contiguous, q_stride elements from a row to the
+ * next (16-byte aligned, a multiple of 16 bytes); out [rows][n_q_heads][head_dim], 16-byte
+ * aligned; lse (NULL: not wanted) float [rows][n_q_heads], natural.  Heads, scale and
+ * lse as pbd_paged_attention; score and slot_pos are neither read nor written.
+ * Scores and sums are fp32; the weights of a bf16 cache are rounded to bf16 for their
+ * product with the values, as in the passes of the step, the outputs once to pages->dtype.
+ * Slots that a row does not see never reach it, whatever they hold; infinite and NaN
+ * elements of slots that it sees count as in fp32 arithmetic.  Rows behind the last
+ * sequence stay as they were.  Results are bitwise the same from run to run; they depend
+ * on a sequence's own data and on batch, rows and max_len.
+ * max_len: host bound on lens, in [1, table_width * page_size].  PBD_STATUS_CAPACITY:
+ * lens[b] outside [0, max_len] or less than n, row_start out of [0, rows] or
+ * descending (then others may be skipped with it).  PBD_STATUS_PAGE: a bad page among
+ * those of the lens[b] slots.  Such a sequence's outputs stay as they were.
+ */
+size_t pbd_packed_attention_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t rows, int32_t max_len);
+int pbd_packed_attention(const pbd_pages* pages, int32_t batch, int32_t rows, const void* q, int64_t q_stride,
+                         const int32_t* row_start, const int32_t* lens, int32_t max_len, float scale,
+                         void* out, float* lse, void* ws, size_t ws_bytes, pbd_stream_t stream);
+
+/*
+ * What the nodes of trees see and where they stand.  The rows of a sequence are its
+ * tree's nodes, at most 64; parent[r] (device int32 [rows]) is the number of a node before
+ * it in the same tree, or -1.  mask[r] (device uint64 [rows]) gets a bit for each ancestor
+ * and for the node itself, row_pos[r] = pos[b] + the number of ancestors (pos and row_pos
+ * go together; NULL: not wanted).  More nodes or bad rows: PBD_STATUS_CAPACITY; a parent
+ * that is neither: PBD_STATUS_TREE; such a sequence's outputs stay as they were.
+ */
+int pbd_tree_layout(int32_t batch, int32_t rows, const int32_t* row_start, const int32_t* parent, const int32_t* pos,
+                    uint64_t* mask, int32_t* row_pos, int32_t* status, pbd_stream_t stream);
+
+/*
+ * Attention of the nodes of trees: with n <= 64 rows of a sequence, its row attends to the
+ * slots before lens[b] - n, and to slot lens[b] - n + j where bit j of mask[row] is set
+ * (bits from n on count for nothing).  Any masks will do: pbd_tree_layout's, or
+ * those of a block that sees itself whole.  A row that sees no slot has out = 0, lse = -inf.
+ * Everything else as pbd_packed_attention; n > 64 raises PBD_STATUS_CAPACITY.
+ */
+size_t pbd_tree_attention_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t rows, int32_t max_len);
+int pbd_tree_attention(const pbd_pages* pages, int32_t batch, int32_t rows, const void* q, int64_t q_stride,
+                       const int32_t* row_start, const int32_t* lens, const uint64_t* mask, int32_t max_len,
+                       float scale, void* out, float* lse, void* ws, size_t ws_bytes, pbd_stream_t stream);
+
+/*
+ * Acceptance and commit of trees.  Node 0 of a tree is the anchor, the last committed
+ * token, and tokens[r] the nodes' tokens; verify[r] is the verifier's token after each.
+ * The path starts at node 0 and goes on to the lowest-numbered child whose token is the
+ * verifier's, while there is one.  path[b][0..k] receives its nodes (0 first),
+ * n_accepted[b] = k, out_tokens[b] the k accepted tokens and then the verifier's after
+ * the last of them, anchor[b] (NULL: not wanted) that one; entries past them are -1 (both
+ * [batch][width]).  In each of n_layers layers of the cache (layer_stride apart) the K
+ * and V of the path's nodes move to the slots lens[b] - n + 0..k, and new_lens[b] = lens[b]
+ * - n + k + 1; what lies behind is given up.  A sequence without rows is left as it is.
+ * n above width or 64, or lens[b] < n: PBD_STATUS_CAPACITY; PBD_STATUS_TREE as
+ * pbd_tree_layout; PBD_STATUS_PAGE for the nodes' pages: the sequence is skipped.
+ * Outputs overlap no input (new_lens is not lens); the nodes' pages belong to one sequence.  A cache that keeps score or slot_pos
+ * is refused (PBD_ERR_UNSUPPORTED).  n_layers >= 1, n_layers * n_kv_heads < 2^24; width in [1, 2^20].
+ */
+int pbd_tree_commit(const pbd_pages* pages, int32_t n_layers, int32_t batch, int32_t rows, const int32_t* row_start,
+                    const int32_t* lens, const int32_t* parent, const int32_t* tokens, const int32_t* verify,
+                    int32_t width, int32_t* path, int32_t* n_accepted, int32_t* out_tokens, int32_t* new_lens,
+                    int32_t* anchor, pbd_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Implementation controls.  The calls below are not part of the step's

@@ -41,6 +41,7 @@ PBD_STATUS_TOKEN = 2
 PBD_STATUS_FORCED_N = 4
 PBD_STATUS_TIMEOUT = 8
 PBD_STATUS_PAGE = 16
+PBD_STATUS_TREE = 32
 
 EXPORTED = (
     "pbd_packed_weight_bytes", "pbd_kv_bytes", "pbd_workspace_bytes", "pbd_init_weights",
@@ -51,6 +52,9 @@ EXPORTED = (
     "pbd_paged_append", "pbd_paged_attention", "pbd_paged_attention_workspace_bytes", "pbd_paged_evict",
     "pbd_paged_evict_workspace_bytes", "pbd_token_logprobs", "pbd_token_logprobs_workspace_bytes",
     "pbd_context_pages", "pbd_decode_paged", "pbd_decode_paged_workspace_bytes",
+    "pbd_page_plan", "pbd_page_release", "pbd_paged_append_rows", "pbd_packed_attention",
+    "pbd_packed_attention_workspace_bytes", "pbd_tree_layout", "pbd_tree_attention",
+    "pbd_tree_attention_workspace_bytes", "pbd_tree_commit",
 )
 
 
@@ -140,6 +144,15 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         "pbd_context_pages": (ctypes.c_int, [vp, vp]),
         "pbd_decode_paged_workspace_bytes": (sz, [vp, vp, i32, i32]),
         "pbd_decode_paged": (ctypes.c_int, [vp, vp, i32, vp, vp, vp, i32, u32, vp, vp, sz, vp]),
+        "pbd_page_plan": (ctypes.c_int, [i32, i32, i32, vp, i32] + [vp] * 6 + [i32] + [vp] * 7),
+        "pbd_page_release": (ctypes.c_int, [i32, i32, i32, vp, i32] + [vp] * 6),
+        "pbd_paged_append_rows": (ctypes.c_int, [vp, i32, vp, vp, vp, i64, vp, vp, vp, vp, f32, vp, i32, vp, vp]),
+        "pbd_packed_attention_workspace_bytes": (sz, [vp, i32, i32, i32]),
+        "pbd_packed_attention": (ctypes.c_int, [vp, i32, i32, vp, i64, vp, vp, i32, f32, vp, vp, vp, sz, vp]),
+        "pbd_tree_layout": (ctypes.c_int, [i32, i32] + [vp] * 7),
+        "pbd_tree_attention_workspace_bytes": (sz, [vp, i32, i32, i32]),
+        "pbd_tree_attention": (ctypes.c_int, [vp, i32, i32, vp, i64, vp, vp, vp, i32, f32, vp, vp, vp, sz, vp]),
+        "pbd_tree_commit": (ctypes.c_int, [vp, i32, i32, i32] + [vp] * 5 + [i32] + [vp] * 6),
         "pbd_last_error": (ctypes.c_char_p, [vp]),
         "pbd_destroy": (None, [vp]),
     }
@@ -439,6 +452,149 @@ def pbd_token_logprobs(logits, tokens, logprob, ws, entropy=None, top_ids=None, 
           x.stride(0) if R > 1 else V, _i32(tokens, R, "tokens", dev), n, _f32(logprob, R, "logprob", dev),
           _f32(entropy, R, "entropy", dev), _i32(top_ids, R * n, "top_ids", dev),
           _f32(top_logprobs, R * n, "top_logprobs", dev), _i32(status, 1, "status", dev), w, wb)
+
+
+# -- packed rows over a paged cache ------------------------------------------------------
+# A call's batch is lens' (or row_start's), its rows those of its row tensors.
+
+
+def _table(table, device: int):
+    if table.dtype is not _torch.int32 or table.dim() != 2 or not table.is_contiguous() or table.get_device() != device:
+        raise PbdError(PBD_ERR_INVALID_ARG, "table must be a contiguous int32 tensor [batch][pages], with the others")
+    return table.data_ptr()
+
+
+def pbd_page_plan(table, seq_pages, free_pages, n_free, lens, n_new, page_size: int, row_start, row_seq, slot_map,
+                  new_lens, pos=None, row_pos=None, status=None, stream=None):
+    """Pages for lens + n_new slots of each sequence, from the stack free_pages[:n_free].  int32: table [batch][pages],
+    free_pages [n_pages] (the pool's pages), n_free and status [1], row_start [batch + 1], seq_pages, lens, n_new, pos and
+    new_lens [batch], slot_map [max_rows] and row_seq and row_pos (either None: not wanted) like it.  status: without it
+    a sequence that is not served is told by new_lens alone."""
+    dev, B = lens.get_device(), lens.numel()
+    if B != table.shape[0]:
+        raise PbdError(PBD_ERR_INVALID_ARG, "table must have a row for each of lens")
+    N, R = free_pages.numel(), slot_map.numel()
+    _call(dev, stream, load_library().pbd_page_plan, B, page_size, N, _table(table, dev), table.shape[1],
+          _i32(seq_pages, B, "seq_pages", dev), _i32(free_pages, N, "free_pages", dev), _i32(n_free, 1, "n_free", dev),
+          _i32(lens, B, "lens", dev), _i32(n_new, B, "n_new", dev), _i32(pos, B, "pos", dev), R,
+          _i32(row_start, B + 1, "row_start", dev), _i32(row_seq, R, "row_seq", dev), _i32(row_pos, R, "row_pos", dev),
+          _i32(slot_map, R, "slot_map", dev), _i32(new_lens, B, "new_lens", dev), _i32(status, 1, "status", dev))
+
+
+def pbd_page_release(table, seq_pages, free_pages, n_free, keep, page_size: int, status=None, stream=None):
+    """Pages past each sequence's first keep slots back to the stack; tensors as pbd_page_plan's, keep int32 [batch]."""
+    dev, B, N = keep.get_device(), keep.numel(), free_pages.numel()
+    if B != table.shape[0]:
+        raise PbdError(PBD_ERR_INVALID_ARG, "table must have a row for each of keep")
+    _call(dev, stream, load_library().pbd_page_release, B, page_size, N, _table(table, dev), table.shape[1],
+          _i32(seq_pages, B, "seq_pages", dev), _i32(free_pages, N, "free_pages", dev), _i32(n_free, 1, "n_free", dev),
+          _i32(keep, B, "keep", dev), _i32(status, 1, "status", dev))
+
+
+def _cache_type(pages):
+    return _torch.bfloat16 if pages.dtype == PBD_DTYPE_BF16 else _torch.float32
+
+
+def _rope_len(rope, D: int, device: int) -> int:
+    if (rope.dtype is not _torch.float32 or not rope.is_contiguous() or rope.get_device() != device or
+            rope.shape != (rope.size(0), D // 2, 2)):
+        raise PbdError(PBD_ERR_INVALID_ARG, "rope must be contiguous float32 [positions][head_dim / 2][2]")
+    return rope.size(0)
+
+
+def _typed(t, dtype, n: int, what: str, device: int):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        raise PbdError(PBD_ERR_INVALID_ARG, f"{what} must be a contiguous tensor of {n} elements of the cache's type")
+    return t.data_ptr()
+
+
+def pbd_paged_append_rows(pages: PbdPages, k, v, slot_map, row_pos, rope, q=None, q_out=None, q_norm=None, k_norm=None,
+                          eps: float = 1e-6, stream=None):
+    """k, v float32 [rows][n_kv_heads * head_dim] and q [rows][n_q_heads * head_dim], all with the same stride from a row
+    to the next (columns of one projection); slot_map, row_pos int32 [rows]; rope float32 [positions][head_dim / 2][2];
+    q_norm, k_norm [head_dim] and q_out [rows][n_q_heads * head_dim] in the cache's type."""
+    dev, H, HQ, D, dt = pages.device, pages.n_kv_heads, pages.n_q_heads, pages.head_dim, _cache_type(pages)
+    R = k.shape[0]
+    stride = k.stride(0) if R > 1 else max(HQ, H) * D
+    for t, width, what in ((k, H * D, "k"), (v, H * D, "v"), (q, HQ * D, "q")):
+        if t is not None and (t.dtype is not _torch.float32 or t.shape != (R, width) or t.get_device() != dev or
+                              t.stride(1) != 1 or (R > 1 and t.stride(0) != stride)):
+            raise PbdError(PBD_ERR_INVALID_ARG, f"{what} must be float32 [rows][{width}] with the row stride of k")
+    n = _rope_len(rope, D, dev)
+    _call(dev, stream, load_library().pbd_paged_append_rows, pages.ref, R, _ptr(q), k.data_ptr(), v.data_ptr(), stride,
+          _i32(slot_map, R, "slot_map", dev), _i32(row_pos, R, "row_pos", dev), _typed(q_norm, dt, D, "q_norm", dev),
+          _typed(k_norm, dt, D, "k_norm", dev), eps, rope.data_ptr(), n, _typed(q_out, dt, R * HQ * D, "q_out", dev))
+
+
+def _rows_attention(name: str, pages, q, row_start, lens, mask, max_len: int, out, ws, lse, scale, stream):
+    dev, HQ, D, dt = pages.device, pages.n_q_heads, pages.head_dim, _cache_type(pages)
+    B, R = lens.numel(), q.shape[0]
+    if (q.dtype is not dt or q.shape != (R, HQ, D) or q.stride(2) != 1 or (q.stride(1) != D and HQ > 1) or
+            q.get_device() != dev):
+        raise PbdError(PBD_ERR_INVALID_ARG,
+                       "q must be [rows][n_q_heads][head_dim] of the cache's type, the heads of a row contiguous")
+    if B > pages.rows:
+        raise PbdError(PBD_ERR_INVALID_ARG, "the table has fewer rows than lens")
+    w, wb = _space(ws, dev)
+    args = (pages.ref, B, R, q.data_ptr(), q.stride(0) if R > 1 else HQ * D, _i32(row_start, B + 1, "row_start", dev),
+            _i32(lens, B, "lens", dev))
+    if mask is not None:
+        if mask.dtype is not _torch.int64 or mask.numel() != R or not mask.is_contiguous() or mask.get_device() != dev:
+            raise PbdError(PBD_ERR_INVALID_ARG, f"mask must be a contiguous int64 tensor of {R} elements, with the others")
+        args += (mask.data_ptr(),)
+    _call(dev, stream, getattr(load_library(), name), *args, max_len, D ** -0.5 if scale is None else scale,
+          _typed(out, dt, R * HQ * D, "out", dev), _f32(lse, R * HQ, "lse", dev), w, wb)
+
+
+def pbd_packed_attention_workspace_bytes(pages: PbdPages, batch: int, rows: int, max_len: int) -> int:
+    return load_library().pbd_packed_attention_workspace_bytes(ctypes.byref(pages), batch, rows, max_len)
+
+
+def pbd_packed_attention(pages: PbdPages, q, row_start, lens, max_len: int, out, ws, lse=None,
+                         scale: Optional[float] = None, stream=None):
+    """q [rows][n_q_heads][head_dim] of the cache's type (any stride from a row to the next), row_start int32 [batch + 1],
+    lens int32 [batch]; out like q, contiguous, lse float32 [rows][n_q_heads].  scale: 1 / sqrt(head_dim) if None."""
+    _rows_attention("pbd_packed_attention", pages, q, row_start, lens, None, max_len, out, ws, lse, scale, stream)
+
+
+def pbd_tree_layout(row_start, parent, mask, pos=None, row_pos=None, status=None, stream=None):
+    """row_start int32 [batch + 1], parent int32 [rows], mask int64 [rows] (bits of a node's ancestors and itself); pos
+    int32 [batch] and row_pos int32 [rows], or both None; status int32 [1]."""
+    dev, B, R = row_start.get_device(), row_start.numel() - 1, parent.numel()
+    if mask.dtype is not _torch.int64 or mask.numel() != R or not mask.is_contiguous() or mask.get_device() != dev:
+        raise PbdError(PBD_ERR_INVALID_ARG, f"mask must be a contiguous int64 tensor of {R} elements, with the others")
+    _call(dev, stream, load_library().pbd_tree_layout, B, R, _i32(row_start, B + 1, "row_start", dev),
+          _i32(parent, R, "parent", dev), _i32(pos, B, "pos", dev), mask.data_ptr(), _i32(row_pos, R, "row_pos", dev),
+          _i32(status, 1, "status", dev))
+
+
+def pbd_tree_attention_workspace_bytes(pages: PbdPages, batch: int, rows: int, max_len: int) -> int:
+    return load_library().pbd_tree_attention_workspace_bytes(ctypes.byref(pages), batch, rows, max_len)
+
+
+def pbd_tree_attention(pages: PbdPages, q, row_start, lens, mask, max_len: int, out, ws, lse=None,
+                       scale: Optional[float] = None, stream=None):
+    """As pbd_packed_attention, with mask int64 [rows]: bits of the sequence's own rows that a row sees."""
+    if mask is None:
+        raise PbdError(PBD_ERR_INVALID_ARG, "mask must be given")
+    _rows_attention("pbd_tree_attention", pages, q, row_start, lens, mask, max_len, out, ws, lse, scale, stream)
+
+
+def pbd_tree_commit(pages: PbdPages, row_start, lens, parent, tokens, verify, path, n_accepted, out_tokens, new_lens,
+                    anchor=None, stream=None):
+    """int32: row_start [batch + 1]; parent, tokens, verify [rows]; path, out_tokens [batch][width]; lens, n_accepted,
+    new_lens, anchor [batch].  All layers of the cache are moved."""
+    dev, B, R = pages.device, lens.numel(), parent.numel()
+    if B > pages.rows:
+        raise PbdError(PBD_ERR_INVALID_ARG, "the table has fewer rows than lens")
+    W = path.shape[-1]
+    _call(dev, stream, load_library().pbd_tree_commit, pages.ref, pages.layers or 1, B, R,
+          _i32(row_start, B + 1, "row_start", dev), _i32(lens, B, "lens", dev), _i32(parent, R, "parent", dev),
+          _i32(tokens, R, "tokens", dev), _i32(verify, R, "verify", dev), W, _i32(path, B * W, "path", dev),
+          _i32(n_accepted, B, "n_accepted", dev), _i32(out_tokens, B * W, "out_tokens", dev),
+          _i32(new_lens, B, "new_lens", dev), _i32(anchor, B, "anchor", dev))
 
 
 class Engine:

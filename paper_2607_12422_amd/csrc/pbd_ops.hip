@@ -1,4 +1,4 @@
-// C entry points of the paged-cache and log-probability operators: argument
+// C entry points of the paged-cache, packed-row and log-probability operators: argument
 // checks, workspace layout and launches.  See include/pbd.h.
 #include <math.h>
 #include <stdio.h>
@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "pbd_paged.h"
+#include "pbd_rows.h"
 
 namespace pbd {
 
@@ -41,6 +42,69 @@ int pages_ok(const pbd_pages* p, int batch, int max_len) {
     char msg[192];
     const int rc = check_pages(p, batch, max_len, msg);
     return rc == PBD_OK ? rc : op_fail(rc, msg);
+}
+
+constexpr int ROWS_MAX = 1 << 22;
+
+// A pool whose slots a map can number, in pages of a supported size.
+int pool_ok(int64_t page_size, int64_t n_pages) {
+    if (page_size < 16 || page_size > 4096 || (page_size & (page_size - 1)))
+        return op_fail(PBD_ERR_SHAPE, "page_size must be 16 times a power of two, at most 4096");
+    if (n_pages < 1) return op_fail(PBD_ERR_INVALID_ARG, "n_pages must be >= 1");
+    if (n_pages * page_size > INT32_MAX) return op_fail(PBD_ERR_CAPACITY, "n_pages times page_size exceeds 2^31 - 1");
+    return PBD_OK;
+}
+
+int tables_ok(int batch, int page_size, int n_pages, int table_width) {
+    const int rc = pool_ok(page_size, n_pages);
+    if (rc) return rc;
+    if (table_width < 1 || table_width > SLOTS_MAX / page_size) return op_fail(PBD_ERR_CAPACITY, "table_width out of range");
+    if (batch < 1) return op_fail(PBD_ERR_INVALID_ARG, "batch must be >= 1");
+    if (batch > BATCH_MAX) return op_fail(PBD_ERR_CAPACITY, "batch exceeds 65535");
+    return PBD_OK;
+}
+
+int log2_of(int x) {
+    int n = 0;
+    while (1 << n < x) ++n;
+    return n;
+}
+
+// Sizes of an attention of packed rows, and its layout.
+int rows_plan(const pbd_pages* pages, int batch, int rows, int max_len, RowsAttnPlan& plan) {
+    const int rc = pages_ok(pages, batch, max_len);
+    if (rc) return rc;
+    if (max_len < 1) return op_fail(PBD_ERR_INVALID_ARG, "max_len must be >= 1");
+    if (rows < 1 || rows > ROWS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "rows outside [1, 2^22]");
+    plan = rows_attn_plan(pages->dtype, pages->n_q_heads, pages->n_kv_heads, pages->head_dim, batch, rows, max_len);
+    if (plan.groups * pages->n_kv_heads > GROUPS_MAX / 2) return op_fail(PBD_ERR_CAPACITY, "rows times heads is too much for one call");
+    return PBD_OK;
+}
+
+int rows_attention(const pbd_pages* pages, int batch, int rows, const void* q, int64_t q_stride, const int32_t* row_start,
+                   const int32_t* lens, const uint64_t* mask, int max_len, float scale, void* out, float* lse, void* ws,
+                   size_t ws_bytes, pbd_stream_t stream) {
+    RowsAttnPlan plan;
+    const int rc = rows_plan(pages, batch, rows, max_len, plan);
+    if (rc) return rc;
+    if (!q || !row_start || !lens || !out || !ws) return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
+    const int esz = pages->dtype == PBD_DTYPE_BF16 ? 2 : 4;
+    if (q_stride < (int64_t)pages->n_q_heads * pages->head_dim || q_stride % (16 / esz))
+        return op_fail(PBD_ERR_INVALID_ARG, "q_stride must hold a row and be a multiple of 16 bytes");
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 16))
+        return op_fail(PBD_ERR_INVALID_ARG, "q, out and ws must be 16-byte aligned");
+    if (!(scale > 0.f) || isinf(scale)) return op_fail(PBD_ERR_INVALID_ARG, "scale must be positive and finite");
+    if (ws_bytes < plan.bytes) return op_fail(PBD_ERR_CAPACITY, "workspace smaller than the call's workspace_bytes");
+    RowsAttnArgs a{};
+    a.pg = page_view(*pages);
+    a.n_q = pages->n_q_heads; a.n_kv = pages->n_kv_heads; a.batch = batch; a.rows = rows; a.max_len = max_len;
+    a.q = q; a.q_stride = q_stride; a.row_start = row_start; a.lens = lens; a.mask = (const unsigned long long*)mask;
+    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    a.kps = plan.kps; a.splits = plan.splits; a.direct = plan.splits == 1;
+    a.part_o = (float*)ws;
+    a.part_ml = (float*)((char*)ws + plan.off_ml);
+    a.out = out; a.lse = lse;
+    return hip_result(launch_rows_attn(pages->dtype, pages->head_dim, a, plan, (hipStream_t)stream), "attention of rows");
 }
 
 }  // namespace
@@ -215,6 +279,130 @@ int pbd_token_logprobs(int32_t rows, int32_t vocab, int32_t dtype, const void* l
     a.tokens = tokens; a.logprob = logprob; a.entropy = entropy; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
     a.status = status; a.ws = (char*)ws;
     return hip_result(launch_logprobs(dtype, a, (hipStream_t)stream), "log probabilities");
+}
+
+int pbd_page_plan(int32_t batch, int32_t page_size, int32_t n_pages, int32_t* table, int32_t table_width, int32_t* seq_pages,
+                  const int32_t* free_pages, int32_t* n_free, const int32_t* lens, const int32_t* n_new, const int32_t* pos,
+                  int32_t max_rows, int32_t* row_start, int32_t* row_seq, int32_t* row_pos, int32_t* slot_map,
+                  int32_t* new_lens, int32_t* status, pbd_stream_t stream) {
+    const int rc = tables_ok(batch, page_size, n_pages, table_width);
+    if (rc) return rc;
+    if (max_rows < 0 || max_rows > ROWS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "max_rows outside [0, 2^22]");
+    if (!table || !seq_pages || !free_pages || !n_free || !lens || !n_new || !row_start || !new_lens || (max_rows > 0 && !slot_map))
+        return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
+    if (max_rows > 0 && (pos == nullptr) != (row_pos == nullptr)) return op_fail(PBD_ERR_INVALID_ARG, "pos and row_pos go together");
+    for (const int32_t* in : {lens, n_new, (const int32_t*)seq_pages})
+        if (new_lens == in || row_start == in) return op_fail(PBD_ERR_INVALID_ARG, "new_lens and row_start must be no input");
+    PagePlanArgs a{};
+    a.batch = batch; a.page_bits = log2_of(page_size); a.n_pages = n_pages; a.table_width = table_width; a.max_rows = max_rows;
+    a.table = table; a.seq_pages = seq_pages; a.free_pages = free_pages; a.n_free = n_free;
+    a.lens = lens; a.n_new = n_new; a.pos = pos; a.row_start = row_start; a.row_seq = row_seq; a.row_pos = row_pos;
+    a.slot_map = slot_map; a.new_lens = new_lens; a.status = status;
+    return hip_result(launch_page_plan(a, (hipStream_t)stream), "page plan");
+}
+
+int pbd_page_release(int32_t batch, int32_t page_size, int32_t n_pages, int32_t* table, int32_t table_width,
+                     int32_t* seq_pages, int32_t* free_pages, int32_t* n_free, const int32_t* keep, int32_t* status,
+                     pbd_stream_t stream) {
+    const int rc = tables_ok(batch, page_size, n_pages, table_width);
+    if (rc) return rc;
+    if (!table || !seq_pages || !free_pages || !n_free || !keep) return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
+    if (keep == seq_pages) return op_fail(PBD_ERR_INVALID_ARG, "keep must not be seq_pages");
+    PageReleaseArgs a{};
+    a.batch = batch; a.page_bits = log2_of(page_size); a.n_pages = n_pages; a.table_width = table_width;
+    a.table = table; a.seq_pages = seq_pages; a.free_pages = free_pages; a.n_free = n_free; a.keep = keep; a.status = status;
+    return hip_result(launch_page_release(a, (hipStream_t)stream), "page release");
+}
+
+int pbd_paged_append_rows(const pbd_pages* pages, int32_t rows, const float* q, const float* k, const float* v,
+                          int64_t row_stride, const int32_t* slot_map, const int32_t* row_pos, const void* q_norm,
+                          const void* k_norm, float eps, const float* rope, int32_t rope_len, void* q_out,
+                          pbd_stream_t stream) {
+    int rc = pages_ok(pages, 1, 0);
+    if (rc) return rc;
+    rc = pool_ok(pages->page_size, pages->n_pages);
+    if (rc) return rc;
+    if (pages->score || pages->slot_pos) return op_fail(PBD_ERR_UNSUPPORTED, "the cache keeps score or slot_pos");
+    if (rows < 0 || rows > ROWS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "rows outside [0, 2^22]");
+    if (rows == 0) return PBD_OK;
+    if (!k || !v || !slot_map || !row_pos || !rope) return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
+    if ((q == nullptr) != (q_out == nullptr)) return op_fail(PBD_ERR_INVALID_ARG, "q and q_out go together");
+    if (q_norm && !q) return op_fail(PBD_ERR_INVALID_ARG, "q_norm without q");
+    if (rope_len < 1) return op_fail(PBD_ERR_INVALID_ARG, "rope_len must be >= 1");
+    if (!(eps >= 0.f) || isinf(eps)) return op_fail(PBD_ERR_INVALID_ARG, "eps must be finite and >= 0");
+    const int width = (q ? pages->n_q_heads : pages->n_kv_heads) * pages->head_dim;
+    if (row_stride < width || row_stride % 4) return op_fail(PBD_ERR_INVALID_ARG, "row_stride must hold a row and be a multiple of 4");
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(rope, 16) || !aligned(q_out, 16) ||
+        !aligned(q_norm, 16) || !aligned(k_norm, 16))
+        return op_fail(PBD_ERR_INVALID_ARG, "q, k, v, rope, q_out and the gains must be 16-byte aligned");
+    PackedAppendArgs a{};
+    a.pg = page_view(*pages);
+    a.n_q = pages->n_q_heads; a.n_kv = pages->n_kv_heads; a.rows = rows; a.rope_len = rope_len;
+    a.q = q; a.k = k; a.v = v; a.row_stride = row_stride; a.slot_map = slot_map; a.row_pos = row_pos;
+    a.q_norm = q_norm; a.k_norm = k_norm; a.eps = eps; a.rope = (const float2*)rope; a.q_out = q_out;
+    return hip_result(launch_packed_append(pages->dtype, pages->head_dim, a, (hipStream_t)stream), "append of rows");
+}
+
+size_t pbd_packed_attention_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t rows, int32_t max_len) {
+    RowsAttnPlan plan;
+    return rows_plan(pages, batch, rows, max_len, plan) ? 0 : plan.bytes;
+}
+
+int pbd_packed_attention(const pbd_pages* pages, int32_t batch, int32_t rows, const void* q, int64_t q_stride,
+                         const int32_t* row_start, const int32_t* lens, int32_t max_len, float scale, void* out,
+                         float* lse, void* ws, size_t ws_bytes, pbd_stream_t stream) {
+    return rows_attention(pages, batch, rows, q, q_stride, row_start, lens, nullptr, max_len, scale, out, lse, ws, ws_bytes, stream);
+}
+
+int pbd_tree_layout(int32_t batch, int32_t rows, const int32_t* row_start, const int32_t* parent, const int32_t* pos,
+                    uint64_t* mask, int32_t* row_pos, int32_t* status, pbd_stream_t stream) {
+    if (batch < 1) return op_fail(PBD_ERR_INVALID_ARG, "batch must be >= 1");
+    if (batch > BATCH_MAX) return op_fail(PBD_ERR_CAPACITY, "batch exceeds 65535");
+    if (rows < 1 || rows > ROWS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "rows outside [1, 2^22]");
+    if (!row_start || !parent || !mask) return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
+    if (!aligned(mask, 8)) return op_fail(PBD_ERR_INVALID_ARG, "mask must be 8-byte aligned");
+    if ((pos == nullptr) != (row_pos == nullptr)) return op_fail(PBD_ERR_INVALID_ARG, "pos and row_pos go together");
+    TreeLayoutArgs a{};
+    a.batch = batch; a.rows = rows; a.row_start = row_start; a.parent = parent; a.pos = pos;
+    a.mask = (unsigned long long*)mask; a.row_pos = row_pos; a.status = status;
+    return hip_result(launch_tree_layout(a, (hipStream_t)stream), "tree layout");
+}
+
+size_t pbd_tree_attention_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t rows, int32_t max_len) {
+    return pbd_packed_attention_workspace_bytes(pages, batch, rows, max_len);
+}
+
+int pbd_tree_attention(const pbd_pages* pages, int32_t batch, int32_t rows, const void* q, int64_t q_stride,
+                       const int32_t* row_start, const int32_t* lens, const uint64_t* mask, int32_t max_len, float scale,
+                       void* out, float* lse, void* ws, size_t ws_bytes, pbd_stream_t stream) {
+    if (!mask) return op_fail(PBD_ERR_INVALID_ARG, "mask is NULL");
+    if (!aligned(mask, 8)) return op_fail(PBD_ERR_INVALID_ARG, "mask must be 8-byte aligned");
+    return rows_attention(pages, batch, rows, q, q_stride, row_start, lens, mask, max_len, scale, out, lse, ws, ws_bytes, stream);
+}
+
+int pbd_tree_commit(const pbd_pages* pages, int32_t n_layers, int32_t batch, int32_t rows, const int32_t* row_start,
+                    const int32_t* lens, const int32_t* parent, const int32_t* tokens, const int32_t* verify,
+                    int32_t width, int32_t* path, int32_t* n_accepted, int32_t* out_tokens, int32_t* new_lens,
+                    int32_t* anchor, pbd_stream_t stream) {
+    const int rc = pages_ok(pages, batch, 0);
+    if (rc) return rc;
+    if (pages->score || pages->slot_pos) return op_fail(PBD_ERR_UNSUPPORTED, "the cache keeps score or slot_pos");
+    if (n_layers < 1 || (long long)n_layers * pages->n_kv_heads > GROUPS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "n_layers out of range");
+    if (rows < 1 || rows > ROWS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "rows outside [1, 2^22]");
+    if (width < 1 || width > (1 << 20)) return op_fail(PBD_ERR_INVALID_ARG, "width outside [1, 2^20]");
+    if (!row_start || !lens || !parent || !tokens || !verify || !path || !n_accepted || !out_tokens || !new_lens)
+        return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
+    if (n_layers > 1 && (pages->layer_stride < 0 || pages->layer_stride % (16 * pages->head_dim)))
+        return op_fail(PBD_ERR_INVALID_ARG, "layer_stride must be a multiple of 16 head_dim");
+    if (new_lens == lens || path == out_tokens || anchor == new_lens || anchor == n_accepted || n_accepted == new_lens)
+        return op_fail(PBD_ERR_INVALID_ARG, "new_lens must not be lens, and outputs not each other");
+    TreeCommitArgs a{};
+    a.pg = page_view(*pages);
+    a.n_kv = pages->n_kv_heads; a.n_layers = n_layers; a.batch = batch; a.rows = rows; a.width = width;
+    a.layer_stride = n_layers > 1 ? pages->layer_stride : 0;
+    a.row_start = row_start; a.lens = lens; a.parent = parent; a.tokens = tokens; a.verify = verify;
+    a.path = path; a.n_accepted = n_accepted; a.out_tokens = out_tokens; a.new_lens = new_lens; a.anchor = anchor;
+    return hip_result(launch_tree_commit(pages->dtype, pages->head_dim, a, (hipStream_t)stream), "tree commit");
 }
 
 }  // extern "C"

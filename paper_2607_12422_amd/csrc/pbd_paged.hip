@@ -8,6 +8,7 @@
 #include "pbd_device.h"
 #include "pbd_launch.h"
 #include "pbd_paged.h"
+#include "pbd_rows.h"
 
 #include <algorithm>
 
@@ -259,6 +260,165 @@ __global__ __launch_bounds__(256) void k_paged_append_few(PagedAppendArgs a) {
         const size_t at = ((size_t)b * a.n_kv + h) * a.pg.slot_stride + slot;
         if (a.pg.score) a.pg.score[at] = 0.f;
         if (a.pg.slot_pos) a.pg.slot_pos[at] = pos + row;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Append of packed rows, each to the slot that a map gives it.  The same lanes hold a
+// row of a head; queries leave rounded to the cache's type.  k_packed_rows: 16 rows and
+// several heads a work-group; V is turned in LDS, and rows whose slots make up a 4-slot
+// group of the layout leave as one, the others element by element.  k_packed_few: the
+// 16 lane groups take 16 heads of one row.
+// ---------------------------------------------------------------------------
+// A row's slot, or -1 where it is none: not wanted, or out of range (reported once).
+__device__ __forceinline__ int packed_slot(const PackedAppendArgs& a, int row, bool report, int& pos) {
+    const int slot = a.slot_map[row];
+    pos = a.row_pos[row];
+    if (slot < 0) return -1;
+    const bool page = slot >> (a.pg.page_shift + 4) >= a.pg.n_pages;
+    if (!page && pos >= 0 && pos < a.rope_len) return slot;
+    if (report) raise(a.pg.status, page ? PBD_STATUS_PAGE : PBD_STATUS_CAPACITY);
+    return -1;
+}
+
+// Elements of a slot's block from the pool's start, for KV head h.
+template <int HD>
+__device__ __forceinline__ long long slot_block(const PageView& pg, int slot, int h) {
+    const int sh = pg.page_shift + 4;
+    return (long long)(slot >> sh) * pg.page_stride + (long long)h * pg.head_stride +
+           (long long)((slot & ((1 << sh) - 1)) >> 4) * (16 * HD);
+}
+
+template <typename T, int HD>
+__device__ __forceinline__ void store_query(T* dst, int l16, const HeadRow<HD>& x) {
+    constexpr int NP = HD / 32, HALF = HD / 2;
+    typedef T __attribute__((ext_vector_type(NP))) tv;
+    tv lo, hi;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        lo[p] = from_f32<T>(x.lo[p]);
+        hi[p] = from_f32<T>(x.hi[p]);
+    }
+    *(tv*)(dst + NP * l16) = lo;
+    *(tv*)(dst + HALF + NP * l16) = hi;
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_packed_rows(PackedAppendArgs a) {
+    typedef HeadRow<HD> Row;
+    constexpr int NP = Row::NP, HALF = HD / 2, LDV = HD + 8;
+    __shared__ T s_v[KV_HEADS][16 * LDV];
+    __shared__ int s_slot[16];
+    const int l16 = threadIdx.x & 15, grp = threadIdx.x >> 4, row = blockIdx.x * 16 + grp;
+    const int kv_groups = (a.n_kv + KV_HEADS - 1) / KV_HEADS;
+    int pos = 0;
+    const int slot = row < a.rows ? packed_slot(a, row, blockIdx.y == 0 && l16 == 0, pos) : -1;
+    const bool live = slot >= 0;
+    const size_t r = (size_t)row * a.row_stride;
+    typename Row::fv2 cs;
+    if (live) cs = *(const typename Row::fv2*)(a.rope + (size_t)pos * HALF + NP * l16);
+    typename Row::fv g_lo, g_hi;
+    if ((int)blockIdx.y >= kv_groups) {
+        const int h0 = ((int)blockIdx.y - kv_groups) * Q_HEADS;
+        Row x[Q_HEADS];
+        if (!live) return;
+#pragma unroll
+        for (int i = 0; i < Q_HEADS; ++i) x[i].load(a.q + r + (size_t)min(h0 + i, a.n_q - 1) * HD, l16);
+        if (a.q_norm) load_gain<T, HD>(a.q_norm, l16, g_lo, g_hi);
+#pragma unroll
+        for (int i = 0; i < Q_HEADS; ++i) {
+            if (a.q_norm) x[i].norm(g_lo, g_hi, a.eps);
+            x[i].turn(cs);
+            if (h0 + i < a.n_q) store_query<T, HD>((T*)a.q_out + ((size_t)row * a.n_q + h0 + i) * HD, l16, x[i]);
+        }
+        return;
+    }
+    const int h0 = blockIdx.y * KV_HEADS;
+    if (l16 == 0) s_slot[grp] = slot;
+    if (live) {
+        Row x[KV_HEADS], v[KV_HEADS];
+#pragma unroll
+        for (int i = 0; i < KV_HEADS; ++i) {
+            const size_t at = r + (size_t)min(h0 + i, a.n_kv - 1) * HD;
+            x[i].load(a.k + at, l16);
+            v[i].load(a.v + at, l16);
+        }
+        if (a.k_norm) load_gain<T, HD>(a.k_norm, l16, g_lo, g_hi);
+#pragma unroll
+        for (int i = 0; i < KV_HEADS; ++i) {
+            if (h0 + i >= a.n_kv) break;
+            if (a.k_norm) x[i].norm(g_lo, g_hi, a.eps);
+            x[i].turn(cs);
+            store_key<T, HD>((T*)a.pg.k + slot_block<HD>(a.pg, slot, h0 + i), slot & 15, l16, x[i]);
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                s_v[i][grp * LDV + NP * l16 + p] = from_f32<T>(v[i].lo[p]);
+                s_v[i][grp * LDV + HALF + NP * l16 + p] = from_f32<T>(v[i].hi[p]);
+            }
+        }
+    }
+    __syncthreads();
+    // whether the rows j .. j + 3 are the four slots of a group of the layout
+    auto whole = [&](int j) -> bool {
+        if (j < 0 || j > 12) return false;
+        const int s = s_slot[j];
+        return s >= 0 && (s & 3) == 0 && s_slot[j + 1] == s + 1 && s_slot[j + 2] == s + 2 && s_slot[j + 3] == s + 3;
+    };
+#pragma unroll
+    for (int it = 0; it < 16 * HD / 256; ++it) {
+        const int u = it * 256 + threadIdx.x, j = u / HD, dim = u % HD, s = s_slot[j];
+        if (s < 0) continue;
+        const bool head = (s & 3) == 0 && whole(j);
+        if (!head && whole(j - (s & 3))) continue;   // its group's first row takes it along
+#pragma unroll
+        for (int i = 0; i < KV_HEADS; ++i) {
+            if (h0 + i >= a.n_kv) break;
+            T* dst = (T*)a.pg.v + slot_block<HD>(a.pg, s, h0 + i) + vblock_elem(s & 15, dim);
+            if (head) {
+                typedef T __attribute__((ext_vector_type(4))) t4;
+                *(t4*)dst = t4{s_v[i][j * LDV + dim], s_v[i][(j + 1) * LDV + dim], s_v[i][(j + 2) * LDV + dim], s_v[i][(j + 3) * LDV + dim]};
+            } else {
+                *dst = s_v[i][j * LDV + dim];
+            }
+        }
+    }
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_packed_few(PackedAppendArgs a) {
+    typedef HeadRow<HD> Row;
+    constexpr int NP = Row::NP, HALF = HD / 2;
+    const int l16 = threadIdx.x & 15, row = blockIdx.x;
+    int pos;
+    const int slot = packed_slot(a, row, blockIdx.y == 0 && threadIdx.x == 0, pos);
+    const int head = blockIdx.y * 16 + (threadIdx.x >> 4);   // KV heads first, then queries
+    const bool kv = head < a.n_kv;
+    if (slot < 0 || head >= a.n_kv + (a.q ? a.n_q : 0)) return;
+    const size_t r = (size_t)row * a.row_stride;
+    const typename Row::fv2 cs = *(const typename Row::fv2*)(a.rope + (size_t)pos * HALF + NP * l16);
+    const void* gain = kv ? a.k_norm : a.q_norm;
+    const int h = kv ? head : head - a.n_kv;
+    Row x, v;
+    x.load((kv ? a.k : a.q) + r + (size_t)h * HD, l16);
+    if (kv) v.load(a.v + r + (size_t)h * HD, l16);
+    if (gain) {
+        typename Row::fv g_lo, g_hi;
+        load_gain<T, HD>(gain, l16, g_lo, g_hi);
+        x.norm(g_lo, g_hi, a.eps);
+    }
+    x.turn(cs);
+    if (!kv) {
+        store_query<T, HD>((T*)a.q_out + ((size_t)row * a.n_q + h) * HD, l16, x);
+        return;
+    }
+    const int key = slot & 15;
+    const long long off = slot_block<HD>(a.pg, slot, h);
+    store_key<T, HD>((T*)a.pg.k + off, key, l16, x);
+    T* dst = (T*)a.pg.v + off;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        dst[vblock_elem(key, NP * l16 + p)] = from_f32<T>(v.lo[p]);
+        dst[vblock_elem(key, HALF + NP * l16 + p)] = from_f32<T>(v.hi[p]);
     }
 }
 
@@ -816,6 +976,13 @@ hipError_t launch_paged_append(int dtype, int head_dim, const PagedAppendArgs& a
         PBD_BY_TYPE(k_paged_append_few, dim3(std::max(1, a.max_new), parts, batch));
     const int groups = (a.n_kv + KV_HEADS - 1) / KV_HEADS + (a.q ? (a.n_q + Q_HEADS - 1) / Q_HEADS : 0);
     PBD_BY_TYPE(k_paged_append_rows, dim3((a.max_new + 14) / 16 + 1, groups, batch));
+}
+
+hipError_t launch_packed_append(int dtype, int head_dim, const PackedAppendArgs& a, hipStream_t st) {
+    const int parts = (a.n_kv + (a.q ? a.n_q : 0) + 15) / 16;
+    if ((long long)a.rows * parts <= FEW_GROUPS) PBD_BY_TYPE(k_packed_few, dim3(a.rows, parts));
+    const int groups = (a.n_kv + KV_HEADS - 1) / KV_HEADS + (a.q ? (a.n_q + Q_HEADS - 1) / Q_HEADS : 0);
+    PBD_BY_TYPE(k_packed_rows, dim3((a.rows + 15) / 16, groups));
 }
 
 constexpr int KPS_MAX = 4096;     // a wave's lanes hold the addresses of 64 blocks of 16 slots, the four waves of 256

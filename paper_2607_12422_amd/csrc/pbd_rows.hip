@@ -1,0 +1,597 @@
+// Attention of several rows of each sequence over a paged KV cache: the causal rows
+// of a prompt (or of a chunk of one), and the nodes of a tree of drafted tokens.
+//
+// The rows of a sequence are packed behind those of the sequence before; for one KV
+// head they are the products row x query head of its G heads (head row r: row r / G).
+// A work-group takes RW tiles of 32 head rows, one to a wave, over one range of slots,
+// whose blocks a wave of its own streams from their pages into a ring in LDS.  Both
+// products run as 32 x 32 tiles (S^T = K Q^T, O^T = V^T P^T): K and V come from the
+// cache's blocks as A operands, 16 bytes a lane of K, 4 slots of one dim of V, and the
+// weights leave the score accumulators in the lanes that the value product wants them
+// in, so that nothing crosses lanes but a rare new maximum.  A tile of 32 columns
+// reads a block from LDS once for 32 rows, which is as fast as the matrix cores take
+// it; with 16 it was twice that.
+#include "pbd_launch.h"
+#include "pbd_rows.h"
+
+#include <algorithm>
+
+namespace pbd {
+namespace {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+__device__ __forceinline__ void raise(int* status, int bit) {
+    if (status) atomicOr(status, bit);
+}
+
+// How far a score may exceed the running maximum before it is raised (log2 units):
+// weights up to 2^8 in place of a rescaling of the output at most steps.
+constexpr float SLACK = 8.f;
+
+template <typename T> struct Stage;
+template <> struct Stage<bf16> { static constexpr int BLOCKS = 4; };     // 16-slot blocks of a stage
+template <> struct Stage<float> { static constexpr int BLOCKS = 2; };
+
+// acc += A B over the 16 bytes of a lane's row (column): halves of the wave hold the
+// two halves of the step's k values.
+template <typename T> __device__ __forceinline__ void mma32(f32x16& acc, const uint4& a, const uint4& b);
+template <> __device__ __forceinline__ void mma32<bf16>(f32x16& acc, const uint4& a, const uint4& b) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+}
+template <> __device__ __forceinline__ void mma32<float>(f32x16& acc, const uint4& a, const uint4& b) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+}
+
+// Wait states for the longest of these products (16 passes in fp32) before vector
+// instructions touch its registers, with nothing scheduled across.
+template <typename T> __device__ __forceinline__ void settle() {
+    mfma_settle();
+    if constexpr (sizeof(T) == 4) asm volatile("s_nop 7" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ float half_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Where a group of head rows lies: its sequence, by a search of the wave over the
+// groups' first numbers first(b) = row_start[b] G / ROWS + b, which leave room for
+// every sequence's groups wherever its rows begin.
+struct Place {
+    int b, row0, n, len;        // sequence, its first packed row, its rows and slots
+    int tile;                   // number of the group in the sequence
+    bool ok;                    // rows to do
+};
+template <int ROWS>
+__device__ __forceinline__ Place find_group(const RowsAttnArgs& a, int group) {
+    const int lane = threadIdx.x & 63, G = a.n_q / a.n_kv;
+    auto first = [&](int b) -> long long { return (long long)a.row_start[b] * G / ROWS + b; };
+    int lo = 0, hi = a.batch;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const bool below = at < hi && (lane == 0 || first(at) <= group);
+        const int cnt = __popcll(__ballot(below));
+        lo += (cnt - 1) * step;
+        hi = min(hi, lo + step);
+    }
+    Place p;
+    p.b = __builtin_amdgcn_readfirstlane(lo);
+    const int r0 = __builtin_amdgcn_readfirstlane(a.row_start[p.b]), r1 = __builtin_amdgcn_readfirstlane(a.row_start[p.b + 1]);
+    p.len = __builtin_amdgcn_readfirstlane(a.lens[p.b]);
+    p.row0 = r0;
+    p.n = r1 - r0;
+    const bool valid = r0 >= 0 && r1 >= r0 && r1 <= a.rows && p.len >= p.n && p.len <= a.max_len && (!a.mask || p.n <= TREE_MAX);
+    const long long t = valid ? group - first(p.b) : -1;
+    p.tile = (int)t;
+    p.ok = valid && t >= 0 && t * ROWS < (long long)p.n * G;
+    return p;
+}
+
+// Reports sequences whose rows or length are out of range (the first work-group).
+__device__ __forceinline__ void report_bad(const RowsAttnArgs& a) {
+    bool bad = false;
+    for (int b = threadIdx.x; b < a.batch; b += blockDim.x) {
+        const int r0 = a.row_start[b], r1 = a.row_start[b + 1], len = a.lens[b];
+        bad |= r0 < 0 || r1 < r0 || r1 > a.rows || len < 0 || len > a.max_len || len < r1 - r0 || (a.mask && r1 - r0 > TREE_MAX);
+    }
+    if (bad) raise(a.pg.status, PBD_STATUS_CAPACITY);
+}
+
+__device__ __forceinline__ void keep_first(uint2& v, int n) {      // the first n of four slots, the others 0
+    v.y &= n >= 4 ? 0xffffffffu : n == 3 ? 0x0000ffffu : 0u;
+    v.x &= n >= 2 ? 0xffffffffu : n == 1 ? 0x0000ffffu : 0u;
+}
+__device__ __forceinline__ void keep_first(uint4& v, int n) {
+    if (n < 4) v.w = 0u;
+    if (n < 3) v.z = 0u;
+    if (n < 2) v.y = 0u;
+    if (n < 1) v.x = 0u;
+}
+
+template <typename T> struct VRaw;                   // a lane's V: 4 slots of a dim
+template <> struct VRaw<bf16> { typedef uint2 t; };
+template <> struct VRaw<float> { typedef uint4 t; };
+
+// One value of an operand that stands for `yes`, for counting products.
+template <typename T> __device__ __forceinline__ T one_if(bool yes) { return from_f32<T>(yes ? 1.f : 0.f); }
+
+template <typename T> __device__ __forceinline__ T elem(const typename VRaw<T>::t& v, int e) {
+    T x[4];
+    __builtin_memcpy(x, &v, sizeof x);
+    return x[e];
+}
+
+// acc += V P over the 16 slots of a block: v0, v1 the lane's slots 4h.. and 8 + 4h.. of
+// its dim, p its eight weights in that order.
+template <typename T>
+__device__ __forceinline__ void mma_block(f32x16& acc, const typename VRaw<T>::t& v0, const typename VRaw<T>::t& v1, const T (&p)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        bf16x8 pv;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pv[i] = p[i];
+        const bf16x8 v = __builtin_bit_cast(bf16x8, uint4{v0.x, v0.y, v1.x, v1.y});
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pv, acc, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(elem<T>(v0, i), p[i], acc, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(elem<T>(v1, i), p[4 + i], acc, 0, 0, 0);
+    }
+}
+
+// The same where some slots are hidden from some rows and values may be infinite or
+// NaN: the product of the finite values, and for the others what their weights make of
+// them, counted by products of ones (seen: bits 0 .. 3 and 8 .. 11, for the weights in turn).
+template <typename T>
+__device__ __forceinline__ void mma_block_careful(f32x16& acc, const typename VRaw<T>::t& v0, const typename VRaw<T>::t& v1,
+                                                  const T (&p)[8], unsigned seen) {
+    T x[8], w[8], part[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[i] = i < 4 ? elem<T>(v0, i & 3) : elem<T>(v1, i & 3);
+        part[i] = __builtin_isfinite(to_f32(x[i])) ? x[i] : from_f32<T>(0.f);
+    }
+    auto raw = [](const T* e) {
+        typename VRaw<T>::t r;
+        __builtin_memcpy(&r, e, sizeof r);
+        return r;
+    };
+    mma_block<T>(acc, raw(part), raw(part + 4), p);
+    settle<T>();
+    // infinite values under a weight, in either sign; NaN, and infinite ones under none
+#pragma unroll 1
+    for (int kind = 0; kind < 4; ++kind) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float f = to_f32(x[i]);
+            const bool inf = __builtin_isinf(f), sees = (seen >> (i < 4 ? i : 4 + i) & 1) != 0, some = to_f32(p[i]) > 0.f;
+            part[i] = one_if<T>(kind == 0 ? f == INFINITY : kind == 1 ? f == -INFINITY : kind == 2 ? f != f : inf);
+            w[i] = one_if<T>(sees && (kind < 2 ? some : kind == 2 || !some));
+        }
+        f32x16 c;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[i] = 0.f;
+        mma_block<T>(c, raw(part), raw(part + 4), w);
+        settle<T>();
+        const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __builtin_nanf("");
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (c[i] > 0.f) acc[i] += what;
+    }
+}
+
+// One head row's four dims from d on, normalised.
+template <typename T, int HD>
+__device__ __forceinline__ void put_out(const RowsAttnArgs& a, size_t head_row, int d, const float (&x)[4]) {
+    typedef T __attribute__((ext_vector_type(4))) t4;
+    *(t4*)((T*)a.out + head_row * HD + d) = t4{from_f32<T>(x[0]), from_f32<T>(x[1]), from_f32<T>(x[2]), from_f32<T>(x[3])};
+}
+
+// log sum of a row from its maximum and sum (log2 units); none: a row that sees no slot.
+__device__ __forceinline__ float log_sum(float M, float L, bool none) {
+    return none ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.69314718055994530942f;
+}
+
+// ---------------------------------------------------------------------------
+// RW tiles of 32 head rows, KW waves to a tile, each with its own slots of a stage.
+// A weight of 0 hides no infinite or NaN value from the value product.  Slots past the
+// sequence are cleared; values that a row of the tile does not see while others do are
+// rare enough to be looked for in the result: a work-group whose output holds a NaN
+// goes over its slots again, 32 dims at a time, with products that leave them out.
+// ---------------------------------------------------------------------------
+template <typename T, int HD, int RW, int KW>
+__global__ __launch_bounds__((RW * KW + 1) * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 && RW * KW > 2 ? 3 : 2)))
+void k_rows_attn(RowsAttnArgs a) {
+    constexpr int NB = Stage<T>::BLOCKS, KEYS = NB * 16, NS = NB / 2 / KW;       // 32-slot parts of a stage that a wave has
+    constexpr int NW = RW * KW, ROWS = RW * 32;
+    constexpr int BLK = 16 * HD * (int)sizeof(T), SB = NB * 2 * BLK;             // bytes of a block's K, of a stage
+    constexpr int KS = HD * (int)sizeof(T) / 32, NT = HD / 32;
+    constexpr int RING = ROWS_RING;
+    typedef typename VRaw<T>::t vraw;
+    static_assert(NS >= 1 && KW <= 2, "a stage has a step for every wave");
+    extern __shared__ __align__(16) unsigned char smem[];                        // [RING][NB][K, V]
+    __shared__ int s_bad, s_odd;
+    const int kvh = blockIdx.x % a.n_kv, group = (int)(gridDim.x / a.n_kv) - 1 - (int)(blockIdx.x / a.n_kv), split = blockIdx.y;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (blockIdx.x == 0 && split == 0) report_bad(a);
+    const Place at = find_group<ROWS>(a, group);
+    if (!at.ok) return;
+    const int G = a.n_q / a.n_kv, base = at.len - at.n;
+    const int hr0 = at.tile * ROWS, hr_end = min(hr0 + ROWS, at.n * G);          // the group's head rows
+    const int limit = a.mask ? at.len : base + (hr_end - 1) / G + 1;             // slots that any of them sees
+    const int beg = split * a.kps, end = min(limit, beg + a.kps);
+    if (beg >= end) return;
+    const int n_st = (end - beg + KEYS - 1) / KEYS;
+    const int* table = a.pg.table + (size_t)at.b * a.pg.table_width;
+    const int bsh = a.pg.page_shift;
+    if (threadIdx.x == 0) s_bad = s_odd = 0;
+    lds_sync();
+
+    if (wave == NW) {
+        // the loader: lane i has the address of block blk0 + i of 64
+        typedef __attribute__((address_space(3))) void* lds;
+        constexpr int LOADS = SB / 1024;
+        static_assert(LOADS * (RING - 2) < 64, "the loads in flight fit the wait counter");
+        const int last = (end - 1) >> 4, blk0 = beg >> 4;
+        for (int pass = 0; pass <= NT; ++pass) {
+            auto look = [&](int blk) { return table[min(blk, last) >> bsh]; };
+            int next = look(blk0 + lane), off_lo = 0, off_hi = 0;
+            auto issue = [&](int st) {
+                const int i0 = st * NB;
+                if ((i0 & 63) == 0) {
+                    const int id = next >= 0 && next < a.pg.n_pages ? next : 0;  // (a bad page ends without output)
+                    const int blk = min(blk0 + i0 + lane, last);
+                    const long long off = ((long long)id * a.pg.page_stride + (long long)kvh * a.pg.head_stride +
+                                           (long long)(blk & ((1 << bsh) - 1)) * (16 * HD)) * (long long)sizeof(T);
+                    off_lo = (int)(off & 0xffffffffll);
+                    off_hi = (int)(off >> 32);
+                    next = look(blk0 + i0 + 64 + lane);
+                }
+                unsigned char* dst = smem + (size_t)(st % RING) * SB;
+#pragma unroll
+                for (int c = 0; c < NB; ++c) {
+                    const size_t o = (size_t)(unsigned)__builtin_amdgcn_readlane(off_lo, (i0 & 63) + c) |
+                                     (size_t)(unsigned)__builtin_amdgcn_readlane(off_hi, (i0 & 63) + c) << 32;
+                    const char *k = a.pg.k + o + lane * 16, *v = a.pg.v + o + lane * 16;
+#pragma unroll
+                    for (int i = 0; i < BLK / 1024; ++i)
+                        __builtin_amdgcn_global_load_lds((const void*)(k + i * 1024), (lds)(dst + c * 2 * BLK + i * 1024), 16, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < BLK / 1024; ++i)
+                        __builtin_amdgcn_global_load_lds((const void*)(v + i * 1024), (lds)(dst + c * 2 * BLK + BLK + i * 1024), 16, 0, 0);
+                }
+            };
+#pragma unroll
+            for (int s = 0; s < RING - 1; ++s)
+                if (s < n_st) issue(s);
+            for (int it = 0; it < n_st; ++it) {
+                // loads of the stages after this one may stay in flight
+                const int left = min(n_st - 1 - it, RING - 2);
+                if (left >= 2) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(RING >= 4 ? 2 * LOADS : 0) : "memory");
+                else if (left == 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(RING >= 3 ? LOADS : 0) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+                if (it + RING - 1 < n_st) issue(it + RING - 1);
+            }
+            lds_sync();                              // every wave past the last stage
+            if (pass == 0) {
+                if (KW > 1) {
+                    lds_sync();
+                    lds_sync();
+                }
+                if (!s_odd) return;
+            }
+        }
+        return;
+    }
+
+    const int rw = wave / KW, kw = wave % KW, col = lane & 31, h = lane >> 5;
+    // this lane's head row (past the last: the last) and what it sees
+    const int mine = min(hr0 + rw * 32 + col, hr_end - 1), tok = mine / G, row = at.row0 + tok;
+    const bool live = hr0 + rw * 32 + col < hr_end;
+    const size_t head_row = (size_t)row * a.n_q + kvh * G + mine % G;
+    const char* q = (const char*)a.q + ((size_t)row * a.q_stride + (size_t)(kvh * G + mine % G) * HD) * sizeof(T) + h * 16;
+    uint4 qf[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = *(const uint4*)(q + s * 32);
+    unsigned long long bits = 0;
+    if (a.mask) bits = a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull);
+    // pages that the sequence's slots use, all of them in every work-group: the same answer
+    {
+        const int pages = (at.len + (16 << bsh) - 1) >> (bsh + 4);
+        bool bad = false;
+        for (int p = wave * 64 + lane; p < pages; p += NW * 64) {
+            const int id = table[p];
+            bad |= id < 0 || id >= a.pg.n_pages;
+        }
+        if (__any(bad) && lane == 0) s_bad = 1;
+    }
+    // slots that all of the wave's rows see, and those that any does
+    const int r_first = min(hr0 + rw * 32, hr_end - 1), r_last = min(hr0 + rw * 32 + 31, hr_end - 1);
+    const int sees_all = a.mask ? base : base + r_first / G + 1;
+    const int sees_any = a.mask ? at.len : base + r_last / G + 1;
+    const int lim = base + tok + 1;
+    // what the lane's row sees of the 32 slots from k0 on: bit j slot k0 + j
+    auto seen_of = [&](int k0) -> unsigned {
+        const int d = a.mask ? k0 - base : k0 - lim;
+        if (d <= -32) return ~0u;
+        if (d < 0) return ((1u << -d) - 1) | (unsigned)(bits << -d);
+        return d < 64 ? (unsigned)(bits >> d) : 0u;
+    };
+    auto k_frag = [&](const unsigned char* st, int s) {
+        return *(const uint4*)(st + (col >> 4) * 2 * BLK + ((2 * s + h) * 16 + (col & 15)) * 16);
+    };
+    // scores of hidden slots are -inf (element i of a lane: slot 8 (i / 4) + 4 h + i % 4)
+    auto hide = [&](f32x16& sc, unsigned seen) {
+        seen >>= 4 * h;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (!(seen & (1u << (8 * (i / 4) + i % 4)))) sc[i] = -INFINITY;
+    };
+    // V of block u, tile t: the lane's slots 4 h .. and 8 + 4 h .. of its dim; cut: slots of the step in use
+    auto v_frag = [&](const unsigned char* st, int u, int t, int cut, vraw& v0, vraw& v1) {
+        const unsigned char* v = st + u * 2 * BLK + BLK + (((t * 2 + (col >> 4)) * 4 + h) * 16 + (col & 15)) * sizeof(vraw);
+        v0 = *(const vraw*)v;
+        v1 = *(const vraw*)(v + 32 * sizeof(vraw));
+        if (cut < 32) {
+            keep_first(v0, cut - 16 * u - 4 * h);
+            keep_first(v1, cut - 16 * u - 8 - 4 * h);
+        }
+    };
+
+    f32x16 o[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    float m = -INFINITY, ref = 0.f, l = 0.f;         // running maximum, the same as a finite number, sum of the lane's weights
+    for (int it = 0; it < n_st; ++it) {
+        lds_sync();
+#pragma unroll
+        for (int c = 0; c < NS; ++c) {
+            const unsigned char* st = smem + (size_t)(it % RING) * SB + (kw * NS + c) * 4 * BLK;
+            const int k0 = beg + it * KEYS + (kw * NS + c) * 32;
+            if (k0 >= sees_any) break;
+            f32x16 sc;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) mma32<T>(sc, k_frag(st, s), qf[s]);
+            settle<T>();
+            if (k0 + 32 > sees_all) hide(sc, seen_of(k0));
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[i]);
+            top *= a.scale_log2;
+            if (__any(top > m + SLACK)) {
+                top = fmaxf(m, half_max(top));
+                const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+                l *= f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[t][i] *= f;
+                m = top;
+                ref = top == -INFINITY ? 0.f : top;
+            }
+            T p[2][8];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -ref));
+                l += w;
+                // rounded to the cache's type for the product, as the passes of the step do
+                p[i / 8][i % 8] = from_f32<T>(w);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    vraw v0, v1;
+                    v_frag(st, u, t, at.len - k0, v0, v1);
+                    mma_block<T>(o[t], v0, v1, p[u]);
+                }
+            settle<T>();
+        }
+    }
+    l = half_sum(l);
+    {
+        f32x16 all = o[0];
+#pragma unroll
+        for (int t = 1; t < NT; ++t) all += o[t];
+        float one = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) one += all[i];
+        if (__any(live && one != one) && lane == 0) s_odd = 1;
+    }
+    lds_sync();                                      // every wave past the last stage; s_bad and s_odd are final
+    const bool redo = s_odd != 0, bad = s_bad != 0;
+    if constexpr (KW > 1) {
+        float* part = (float*)smem + (size_t)rw * 64 * (NT * 16 + 2);
+        if (kw > 0) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) part[(t * 16 + i) * 64 + lane] = o[t][i];
+            part[NT * 16 * 64 + lane] = m;
+            part[(NT * 16 + 1) * 64 + lane] = l;
+        }
+        lds_sync();
+        if (kw == 0) {
+            const float mw = part[NT * 16 * 64 + lane], lw = part[(NT * 16 + 1) * 64 + lane], M = fmaxf(m, mw);
+            // (a wave that saw nothing but -inf has a sum of 0 or NaN of its own)
+            const float f0 = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);
+            const float f1 = mw == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw - M);
+            l = l * f0 + lw * f1;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][i] = o[t][i] * f0 + part[(t * 16 + i) * 64 + lane] * f1;
+            m = M;
+            ref = m == -INFINITY ? 0.f : m;
+        }
+        lds_sync();                                  // the ring may be filled again
+    }
+    if (bad && threadIdx.x == 0) raise(a.pg.status, PBD_STATUS_PAGE);
+    const bool none = a.mask && base == 0 && bits == 0;          // a row that sees no slot
+    const float inv = none ? 0.f : 1.f / l;
+    const size_t part_row = head_row * a.splits + split;
+    // 32 dims of the lane's head row from 32 t on: the output's, or the split's sums
+    auto put = [&](int t, const f32x16& v) {
+        if (kw > 0 || !live || (a.direct && bad)) return;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int d = 32 * t + 8 * j + 4 * h;
+            if (a.direct) {
+                const float x[4] = {v[4 * j] * inv, v[4 * j + 1] * inv, v[4 * j + 2] * inv, v[4 * j + 3] * inv};
+                put_out<T, HD>(a, head_row, d, x);
+            } else {
+                *(f32x4*)(a.part_o + part_row * HD + d) = f32x4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+            }
+        }
+    };
+    if (kw == 0 && live && h == 0) {
+        if (!a.direct) {
+            a.part_ml[part_row * 2] = bad ? __builtin_nanf("") : m;
+            a.part_ml[part_row * 2 + 1] = l;
+        } else if (a.lse && !bad) {
+            a.lse[head_row] = log_sum(m, l, none);
+        }
+    }
+    if (__builtin_expect(!redo, true)) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) put(t, o[t]);
+        return;
+    }
+#pragma unroll 1
+    for (int t = 0; t < NT; ++t) {
+        f32x16 v;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = 0.f;
+        for (int it = 0; it < n_st; ++it) {
+            lds_sync();
+#pragma unroll 1
+            for (int c = 0; c < NB / 2; ++c) {
+                const unsigned char* st = smem + (size_t)(it % RING) * SB + c * 4 * BLK;
+                const int k0 = beg + it * KEYS + c * 32;
+                if (kw > 0 || k0 >= sees_any) break;
+                f32x16 sc;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+                for (int s = 0; s < KS; ++s) mma32<T>(sc, k_frag(st, s), *(const uint4*)(q + s * 32));
+                settle<T>();
+                const unsigned seen = seen_of(k0);
+                hide(sc, seen);
+#pragma unroll 1
+                for (int u = 0; u < 2; ++u) {
+                    T p[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        p[i] = from_f32<T>(__builtin_amdgcn_exp2f(__builtin_fmaf(u ? sc[8 + i] : sc[i], a.scale_log2, -ref)));
+                    vraw v0, v1;
+                    v_frag(st, u, t, at.len - k0, v0, v1);
+                    mma_block_careful<T>(v, v0, v1, p, seen >> (16 * u + 4 * h));
+                }
+            }
+        }
+        lds_sync();
+        put(t, v);
+    }
+}
+
+// Joins the splits of head rows, in split order; HD / 4 lanes to a head row.
+template <typename T, int HD, int ROWS>
+__global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
+    constexpr int LANES = HD / 4, N = 256 / LANES;
+    const int kvh = blockIdx.x % a.n_kv, group = blockIdx.x / a.n_kv;
+    const Place at = find_group<ROWS>(a, group);
+    if (!at.ok) return;
+    const int G = a.n_q / a.n_kv, hr = at.tile * ROWS + blockIdx.y * N + (int)threadIdx.x / LANES, d = (int)threadIdx.x % LANES * 4;
+    if (hr >= min((at.tile + 1) * ROWS, at.n * G)) return;
+    const int tok = hr / G, row = at.row0 + tok, base = at.len - at.n;
+    const size_t head_row = (size_t)row * a.n_q + kvh * G + hr % G;
+    const int n = ((a.mask ? at.len : base + tok + 1) + a.kps - 1) / a.kps;
+    typedef float __attribute__((ext_vector_type(2))) ml2;
+    const ml2* ml = (const ml2*)a.part_ml + head_row * a.splits;
+    const float* part = a.part_o + head_row * a.splits * HD + d;
+    float M = -INFINITY, L = 0.f;
+    bool bad = false;
+    for (int s = 0; s < n; ++s) {
+        bad |= ml[s][0] != ml[s][0];
+        M = fmaxf(M, ml[s][0]);
+    }
+    if (bad) return;
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < n; ++s) {
+        const float f = ml[s][0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[s][0] - M);
+        L += ml[s][1] * f;
+        acc += *(const f32x4*)(part + (size_t)s * HD) * f;
+    }
+    const bool none = a.mask && base == 0 && (a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull)) == 0;
+    const float inv = none ? 0.f : 1.f / L;
+    const float x[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+    put_out<T, HD>(a, head_row, d, x);
+    if (a.lse && d == 0) a.lse[head_row] = log_sum(M, L, none);
+}
+
+}  // namespace
+
+// Work-groups wanted where a call has fewer: two a CU.
+constexpr int GROUPS_WANTED = 512;
+constexpr int KPS_MIN = 256;
+
+RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int rows, int max_len) {
+    RowsAttnPlan p{};
+    const long long G = n_q / n_kv, each = (long long)rows * G / batch;
+    p.tiles = each > 64 ? 4 : each > 32 ? 2 : 1;
+    const int R = p.tiles * 32, keys = dtype == PBD_DTYPE_BF16 ? 64 : 32;
+    p.groups = (long long)rows * G / R + batch;
+    const long long live = ((long long)rows * G + R - 1) / R * n_kv;             // (as many as that have rows, about)
+    long long splits = std::max<long long>(1, std::min<long long>(GROUPS_WANTED / std::max(1ll, live), max_len / KPS_MIN));
+    long long kps = (max_len + splits - 1) / splits;
+    kps = std::max<long long>(keys, (kps + keys - 1) / keys * keys);
+    p.kps = (int)kps;
+    p.splits = (int)((max_len + kps - 1) / kps);
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    const size_t n = p.splits == 1 ? 0 : (size_t)rows * n_q * p.splits;
+    p.off_ml = up(n * head_dim * 4);
+    p.bytes = std::max<size_t>(256, p.off_ml + up(n * 2 * 4));
+    return p;
+}
+
+namespace {
+template <typename T, int HD, int RW, int KW>
+hipError_t launch(const RowsAttnArgs& a, const RowsAttnPlan& p, hipStream_t st) {
+    constexpr size_t lds = (size_t)ROWS_RING * Stage<T>::BLOCKS * 2 * 16 * HD * sizeof(T);
+    static_assert(KW == 1 || (size_t)RW * (KW - 1) * 64 * (HD / 2 + 2) * 4 <= lds, "the other waves' sums lie over the ring");
+    PBD_LAUNCH((k_rows_attn<T, HD, RW, KW>), dim3((unsigned)(p.groups * a.n_kv), p.splits), dim3((RW * KW + 1) * 64), lds, st, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.direct) return e;
+    PBD_LAUNCH((k_rows_join<T, HD, RW * 32>), dim3((unsigned)(p.groups * a.n_kv), RW * 32 * HD / 1024), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+template <typename T, int HD>
+hipError_t launch_tiles(const RowsAttnArgs& a, const RowsAttnPlan& p, hipStream_t st) {
+    constexpr int KW = sizeof(T) == 2 ? 2 : 1;
+    if (p.tiles == 4) return launch<T, HD, 4, 1>(a, p, st);
+    if (p.tiles == 2) return launch<T, HD, 2, KW>(a, p, st);
+    return launch<T, HD, 1, KW>(a, p, st);
+}
+}  // namespace
+
+hipError_t launch_rows_attn(int dtype, int head_dim, const RowsAttnArgs& a, const RowsAttnPlan& p, hipStream_t st) {
+    if (dtype == PBD_DTYPE_BF16) return head_dim == 128 ? launch_tiles<bf16, 128>(a, p, st) : launch_tiles<bf16, 64>(a, p, st);
+    return head_dim == 128 ? launch_tiles<float, 128>(a, p, st) : launch_tiles<float, 64>(a, p, st);
+}
+
+}  // namespace pbd
