@@ -209,7 +209,7 @@ __device__ __forceinline__ float log_sum(float M, float L, bool none) {
 // goes over its slots again, 32 dims at a time, with products that leave them out.
 // ---------------------------------------------------------------------------
 template <typename T, int HD, int RW, int KW>
-__global__ __launch_bounds__((RW * KW + 1) * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 && RW * KW > 2 ? 3 : 2)))
+__global__ __launch_bounds__(RW * KW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void k_rows_attn(RowsAttnArgs a) {
     constexpr int NB = Stage<T>::BLOCKS, KEYS = NB * 16, NS = NB / 2 / KW;       // 32-slot parts of a stage that a wave has
     constexpr int NW = RW * KW, ROWS = RW * 32;
@@ -236,62 +236,55 @@ void k_rows_attn(RowsAttnArgs a) {
     if (threadIdx.x == 0) s_bad = s_odd = 0;
     lds_sync();
 
-    if (wave == NW) {
-        // the loader: lane i has the address of block blk0 + i of 64
-        typedef __attribute__((address_space(3))) void* lds;
-        constexpr int LOADS = SB / 1024;
-        static_assert(LOADS * (RING - 2) < 64, "the loads in flight fit the wait counter");
-        const int last = (end - 1) >> 4, blk0 = beg >> 4;
-        for (int pass = 0; pass <= NT; ++pass) {
-            auto look = [&](int blk) { return table[min(blk, last) >> bsh]; };
-            int next = look(blk0 + lane), off_lo = 0, off_hi = 0;
-            auto issue = [&](int st) {
-                const int i0 = st * NB;
-                if ((i0 & 63) == 0) {
-                    const int id = next >= 0 && next < a.pg.n_pages ? next : 0;  // (a bad page ends without output)
-                    const int blk = min(blk0 + i0 + lane, last);
-                    const long long off = ((long long)id * a.pg.page_stride + (long long)kvh * a.pg.head_stride +
-                                           (long long)(blk & ((1 << bsh) - 1)) * (16 * HD)) * (long long)sizeof(T);
-                    off_lo = (int)(off & 0xffffffffll);
-                    off_hi = (int)(off >> 32);
-                    next = look(blk0 + i0 + 64 + lane);
-                }
-                unsigned char* dst = smem + (size_t)(st % RING) * SB;
-#pragma unroll
-                for (int c = 0; c < NB; ++c) {
-                    const size_t o = (size_t)(unsigned)__builtin_amdgcn_readlane(off_lo, (i0 & 63) + c) |
-                                     (size_t)(unsigned)__builtin_amdgcn_readlane(off_hi, (i0 & 63) + c) << 32;
-                    const char *k = a.pg.k + o + lane * 16, *v = a.pg.v + o + lane * 16;
-#pragma unroll
-                    for (int i = 0; i < BLK / 1024; ++i)
-                        __builtin_amdgcn_global_load_lds((const void*)(k + i * 1024), (lds)(dst + c * 2 * BLK + i * 1024), 16, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < BLK / 1024; ++i)
-                        __builtin_amdgcn_global_load_lds((const void*)(v + i * 1024), (lds)(dst + c * 2 * BLK + BLK + i * 1024), 16, 0, 0);
-                }
-            };
-#pragma unroll
-            for (int s = 0; s < RING - 1; ++s)
-                if (s < n_st) issue(s);
-            for (int it = 0; it < n_st; ++it) {
-                // loads of the stages after this one may stay in flight
-                const int left = min(n_st - 1 - it, RING - 2);
-                if (left >= 2) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(RING >= 4 ? 2 * LOADS : 0) : "memory");
-                else if (left == 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(RING >= 3 ? LOADS : 0) : "memory");
-                else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-                if (it + RING - 1 < n_st) issue(it + RING - 1);
-            }
-            lds_sync();                              // every wave past the last stage
-            if (pass == 0) {
-                if (KW > 1) {
-                    lds_sync();
-                    lds_sync();
-                }
-                if (!s_odd) return;
-            }
+    // A wave's part of the stages: K or V of NBW blocks, or both, whose addresses are
+    // looked up for many stages at once, one to a lane.  The loads go to LDS by asm: of
+    // those that it knows the compiler would wait for all before any read of LDS.
+    constexpr int PW = 2 * NB / NW, NBW = NB > NW ? NB / NW : 1, AHEAD = 64 / NBW;
+    static_assert(PW >= 1 && PW % NBW == 0, "the waves share a stage evenly");
+    const int last = (end - 1) >> 4, blk0 = (beg >> 4) + wave % NB;
+    const unsigned ring = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    int next = 0, off_lo = 0, off_hi = 0;
+    auto my_block = [&](int st) { return min(blk0 + (st + lane / NBW) * NB + lane % NBW * NW, last); };
+    auto look = [&](int st) { next = table[my_block(st) >> bsh]; };
+    auto issue = [&](int st) {
+        if (st % AHEAD == 0) {
+            const int id = next >= 0 && next < a.pg.n_pages ? next : 0;          // (a bad page ends without output)
+            const long long off = ((long long)id * a.pg.page_stride + (long long)kvh * a.pg.head_stride +
+                                   (long long)(my_block(st) & ((1 << bsh) - 1)) * (16 * HD)) * (long long)sizeof(T);
+            off_lo = (int)(off & 0xffffffffll);
+            off_hi = (int)(off >> 32);
+            look(st + AHEAD);
         }
-        return;
-    }
+#pragma unroll
+        for (int j = 0; j < PW; ++j) {
+            const int pair = wave + NW * j, blk = pair % NB, kv = pair / NB, i = st % AHEAD * NBW + j % NBW;
+            const char* src = (kv ? a.pg.v : a.pg.k) + lane * 16 +
+                              ((size_t)(unsigned)__builtin_amdgcn_readlane(off_lo, i) |
+                               (size_t)(unsigned)__builtin_amdgcn_readlane(off_hi, i) << 32);
+            const unsigned dst = __builtin_amdgcn_readfirstlane(ring + (unsigned)(st % RING) * SB + (unsigned)(blk * 2 + kv) * BLK);
+#pragma unroll
+            for (int c = 0; c < BLK / 1024; ++c)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                             :: "s"(dst + c * 1024), "v"(src + c * 1024) : "memory", "m0");
+        }
+    };
+    constexpr int LOADS = PW * BLK / 1024;           // a wave's of a stage
+    static_assert(LOADS * (RING - 2) < 64, "the loads in flight fit the wait counter");
+    auto start = [&] {
+        look(0);
+#pragma unroll
+        for (int st = 0; st < RING - 1; ++st)
+            if (st < n_st) issue(st);
+    };
+    // opens stage `it`: every wave's loads of it are there, every wave is past the one whose place is filled next
+    auto open = [&](int it) {
+        const int left = min(n_st - 1 - it, RING - 2);
+        if (RING >= 4 && left >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(RING >= 4 ? 2 * LOADS : 0) : "memory");
+        else if (RING >= 3 && left >= 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(RING >= 3 ? LOADS : 0) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (it + RING - 1 < n_st) issue(it + RING - 1);
+    };
+    start();
 
     const int rw = wave / KW, kw = wave % KW, col = lane & 31, h = lane >> 5;
     // this lane's head row (past the last: the last) and what it sees
@@ -336,15 +329,16 @@ void k_rows_attn(RowsAttnArgs a) {
         for (int i = 0; i < 16; ++i)
             if (!(seen & (1u << (8 * (i / 4) + i % 4)))) sc[i] = -INFINITY;
     };
-    // V of block u, tile t: the lane's slots 4 h .. and 8 + 4 h .. of its dim; cut: slots of the step in use
-    auto v_frag = [&](const unsigned char* st, int u, int t, int cut, vraw& v0, vraw& v1) {
-        const unsigned char* v = st + u * 2 * BLK + BLK + (((t * 2 + (col >> 4)) * 4 + h) * 16 + (col & 15)) * sizeof(vraw);
-        v0 = *(const vraw*)v;
-        v1 = *(const vraw*)(v + 32 * sizeof(vraw));
-        if (cut < 32) {
-            keep_first(v0, cut - 16 * u - 4 * h);
-            keep_first(v1, cut - 16 * u - 8 - 4 * h);
-        }
+    // V of block u, tile t: the lane's slots 4 h .. and 8 + 4 h .. of its dim
+    auto v_frag = [&](const unsigned char* st, int u, int t, vraw (&v)[2]) {
+        const unsigned char* at = st + u * 2 * BLK + BLK + (((t * 2 + (col >> 4)) * 4 + h) * 16 + (col & 15)) * sizeof(vraw);
+        v[0] = *(const vraw*)at;
+        v[1] = *(const vraw*)(at + 32 * sizeof(vraw));
+    };
+    // ... without the slots from `cut` of the step on, which hold nothing
+    auto v_cut = [&](int u, int cut, vraw (&v)[2]) {
+        keep_first(v[0], cut - 16 * u - 4 * h);
+        keep_first(v[1], cut - 16 * u - 8 - 4 * h);
     };
 
     f32x16 o[NT];
@@ -354,17 +348,28 @@ void k_rows_attn(RowsAttnArgs a) {
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
     float m = -INFINITY, ref = 0.f, l = 0.f;         // running maximum, the same as a finite number, sum of the lane's weights
     for (int it = 0; it < n_st; ++it) {
-        lds_sync();
+        open(it);
+        const unsigned char* stage = smem + (size_t)(it % RING) * SB + kw * NS * 4 * BLK;
+        const int first = beg + it * KEYS + kw * NS * 32;
+        if (first >= sees_any) continue;
+        uint4 kf[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) kf[s] = k_frag(stage, s);
 #pragma unroll
         for (int c = 0; c < NS; ++c) {
-            const unsigned char* st = smem + (size_t)(it % RING) * SB + (kw * NS + c) * 4 * BLK;
-            const int k0 = beg + it * KEYS + (kw * NS + c) * 32;
-            if (k0 >= sees_any) break;
+            const unsigned char* st = stage + c * 4 * BLK;
+            const int k0 = first + c * 32;
             f32x16 sc;
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) mma32<T>(sc, k_frag(st, s), qf[s]);
+            for (int s = 0; s < KS; ++s) mma32<T>(sc, kf[s], qf[s]);
+            // V on its way while the weights are made
+            vraw v[2][NT][2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) v_frag(st, u, t, v[u][t]);
             settle<T>();
             if (k0 + 32 > sees_all) hide(sc, seen_of(k0));
             float top = -INFINITY;
@@ -383,21 +388,29 @@ void k_rows_attn(RowsAttnArgs a) {
                 ref = top == -INFINITY ? 0.f : top;
             }
             T p[2][8];
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -ref));
-                l += w;
+                sum[i % 4] += w;
                 // rounded to the cache's type for the product, as the passes of the step do
                 p[i / 8][i % 8] = from_f32<T>(w);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            if (k0 + 32 > at.len) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) v_cut(u, at.len - k0, v[u][t]);
+            }
+            if (c + 1 < NS) {
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kf[s] = k_frag(st + 4 * BLK, s);
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    vraw v0, v1;
-                    v_frag(st, u, t, at.len - k0, v0, v1);
-                    mma_block<T>(o[t], v0, v1, p[u]);
-                }
+                for (int t = 0; t < NT; ++t) mma_block<T>(o[t], v[u][t][0], v[u][t][1], p[u]);
             settle<T>();
         }
     }
@@ -475,8 +488,9 @@ void k_rows_attn(RowsAttnArgs a) {
         f32x16 v;
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = 0.f;
+        start();
         for (int it = 0; it < n_st; ++it) {
-            lds_sync();
+            open(it);
 #pragma unroll 1
             for (int c = 0; c < NB / 2; ++c) {
                 const unsigned char* st = smem + (size_t)(it % RING) * SB + c * 4 * BLK;
@@ -496,9 +510,10 @@ void k_rows_attn(RowsAttnArgs a) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         p[i] = from_f32<T>(__builtin_amdgcn_exp2f(__builtin_fmaf(u ? sc[8 + i] : sc[i], a.scale_log2, -ref)));
-                    vraw v0, v1;
-                    v_frag(st, u, t, at.len - k0, v0, v1);
-                    mma_block_careful<T>(v, v0, v1, p, seen >> (16 * u + 4 * h));
+                    vraw x[2];
+                    v_frag(st, u, t, x);
+                    v_cut(u, at.len - k0, x);
+                    mma_block_careful<T>(v, x[0], x[1], p, seen >> (16 * u + 4 * h));
                 }
             }
         }
@@ -573,7 +588,7 @@ template <typename T, int HD, int RW, int KW>
 hipError_t launch(const RowsAttnArgs& a, const RowsAttnPlan& p, hipStream_t st) {
     constexpr size_t lds = (size_t)ROWS_RING * Stage<T>::BLOCKS * 2 * 16 * HD * sizeof(T);
     static_assert(KW == 1 || (size_t)RW * (KW - 1) * 64 * (HD / 2 + 2) * 4 <= lds, "the other waves' sums lie over the ring");
-    PBD_LAUNCH((k_rows_attn<T, HD, RW, KW>), dim3((unsigned)(p.groups * a.n_kv), p.splits), dim3((RW * KW + 1) * 64), lds, st, a);
+    PBD_LAUNCH((k_rows_attn<T, HD, RW, KW>), dim3((unsigned)(p.groups * a.n_kv), p.splits), dim3(RW * KW * 64), lds, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.direct) return e;
     PBD_LAUNCH((k_rows_join<T, HD, RW * 32>), dim3((unsigned)(p.groups * a.n_kv), RW * 32 * HD / 1024), dim3(256), 0, st, a);
