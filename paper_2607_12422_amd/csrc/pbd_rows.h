@@ -8,7 +8,6 @@
 namespace pbd {
 
 constexpr int TREE_MAX = 64;    // nodes of a tree: bits of a mask
-constexpr int ROWS_RING = 2;    // stages of the attention's ring
 
 struct PagePlanArgs {
     int batch, page_bits, n_pages, table_width, max_rows;
@@ -88,6 +87,7 @@ hipError_t launch_tree_commit(int dtype, int head_dim, const TreeCommitArgs& a, 
 struct RowsAttnPlan {
     int tiles;                  // tiles of 32 head rows a work-group takes
     long long groups;           // groups of that many head rows that the packed rows may need
+    bool once;                  // most sequences' K and V go to one work-group a KV head
     int kps, splits;            // slots per split
     size_t off_ml, bytes;
 };
@@ -104,6 +104,7 @@ struct RowsAttnArgs {
     float scale_log2;
     int kps, splits;
     bool direct;                // one split: it writes the output
+    bool once;                  // K and V past the caches
     float* part_o;              // [rows][n_q][splits][head_dim]
     float* part_ml;             // [rows][n_q][splits][2]: maximum (NaN: bad page), sum
     void* out;                  // [rows][n_q][head_dim]

@@ -25,13 +25,14 @@ __device__ __forceinline__ void raise(int* status, int bit) {
     if (status) atomicOr(status, bit);
 }
 
-// How far a score may exceed the running maximum before it is raised (log2 units):
-// weights up to 2^8 in place of a rescaling of the output at most steps.
-constexpr float SLACK = 8.f;
+// A lane's sum of four weights up to which the reference that they are taken against may
+// stay below the scores: looking for the maximum of every step, and raising the
+// reference with it, is a tenth of the vector work of a step.  (bf16 and fp32 weights
+// have the same relative precision at any size.)
+constexpr float HIGH = 65536.f;
 
-template <typename T> struct Stage;
-template <> struct Stage<bf16> { static constexpr int BLOCKS = 4; };     // 16-slot blocks of a stage
-template <> struct Stage<float> { static constexpr int BLOCKS = 2; };
+constexpr int NB = 4, KEYS = NB * 16;                // 16-slot blocks of a stage, its slots
+constexpr int RING = 2;                              // stages in LDS
 
 // acc += A B over the 16 bytes of a lane's row (column): halves of the wave hold the
 // two halves of the step's k values.
@@ -209,256 +210,156 @@ __device__ __forceinline__ float log_sum(float M, float L, bool none) {
 // goes over its slots again, 32 dims at a time, with products that leave them out.
 // ---------------------------------------------------------------------------
 template <typename T, int HD, int RW, int KW>
-__global__ __launch_bounds__(RW * KW * 64) __attribute__((amdgpu_waves_per_eu(2)))
-void k_rows_attn(RowsAttnArgs a) {
-    constexpr int NB = Stage<T>::BLOCKS, KEYS = NB * 16, NS = NB / 2 / KW;       // 32-slot parts of a stage that a wave has
-    constexpr int NW = RW * KW, ROWS = RW * 32;
-    constexpr int BLK = 16 * HD * (int)sizeof(T), SB = NB * 2 * BLK;             // bytes of a block's K, of a stage
-    constexpr int KS = HD * (int)sizeof(T) / 32, NT = HD / 32;
-    constexpr int RING = ROWS_RING;
+struct RowsWork {
+    static constexpr int NS = NB / 2 / KW;                                       // 32-slot parts of a stage that a wave has
+    static constexpr int NW = RW * KW, ROWS = RW * 32;
+    static constexpr int BLK = 16 * HD * (int)sizeof(T), SB = NB * 2 * BLK;      // bytes of a block's K, of a stage
+    static constexpr int KS = HD * (int)sizeof(T) / 32, NT = HD / 32;
+    static constexpr int PW = 2 * NB / NW, NBW = NB / NW > 1 ? NB / NW : 1, AHEAD = 64 / NBW;
+    static constexpr int LOADS = PW * BLK / 1024;                                // a wave's of a stage
+    static_assert(NS >= 1 && PW >= 1 && PW % NBW == 0, "the waves share a stage evenly");
+    static_assert(RING == 2, "a stage is waited for whole");
     typedef typename VRaw<T>::t vraw;
-    static_assert(NS >= 1 && KW <= 2, "a stage has a step for every wave");
-    extern __shared__ __align__(16) unsigned char smem[];                        // [RING][NB][K, V]
-    __shared__ int s_bad, s_odd;
-    const int kvh = blockIdx.x % a.n_kv, group = (int)(gridDim.x / a.n_kv) - 1 - (int)(blockIdx.x / a.n_kv), split = blockIdx.y;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (blockIdx.x == 0 && split == 0) report_bad(a);
-    const Place at = find_group<ROWS>(a, group);
-    if (!at.ok) return;
-    const int G = a.n_q / a.n_kv, base = at.len - at.n;
-    const int hr0 = at.tile * ROWS, hr_end = min(hr0 + ROWS, at.n * G);          // the group's head rows
-    const int limit = a.mask ? at.len : base + (hr_end - 1) / G + 1;             // slots that any of them sees
-    const int beg = split * a.kps, end = min(limit, beg + a.kps);
-    if (beg >= end) return;
-    const int n_st = (end - beg + KEYS - 1) / KEYS;
-    const int* table = a.pg.table + (size_t)at.b * a.pg.table_width;
-    const int bsh = a.pg.page_shift;
-    if (threadIdx.x == 0) s_bad = s_odd = 0;
-    lds_sync();
+
+    const RowsAttnArgs& a;
+    unsigned char* smem;                                                         // [RING][NB][K, V]
+    int kvh, split, wave, lane, rw, kw, col, h;
+    int k_lane, v_lane;                              // the lane's place in a step's K, in a tile's V
+    Place at;
+    int base, beg, end, n_st;
+    const int* table;
+    // this lane's head row (past the last: the last) and what it sees
+    bool live;
+    size_t head_row;
+    const char* q;
+    unsigned long long bits;
+    int sees_all, sees_any, lim;                     // slots that all of the wave's rows see, that any does; the lane's row
+    int next, off_lo, off_hi;
+
+    __device__ __forceinline__ RowsWork(const RowsAttnArgs& args, unsigned char* ring) : a(args), smem(ring) {}
+
+    // block: blockIdx.x.  false: nothing to do
+    __device__ __forceinline__ bool place(int block) {
+        kvh = block % a.n_kv;
+        split = blockIdx.y;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        lane = threadIdx.x & 63;
+        at = find_group<ROWS>(a, (int)(gridDim.x / a.n_kv) - 1 - block / a.n_kv);        // a sequence's last rows first
+        if (!at.ok) return false;
+        const int G = a.n_q / a.n_kv;
+        base = at.len - at.n;
+        const int hr0 = at.tile * ROWS, hr_end = min(hr0 + ROWS, at.n * G);              // the group's head rows
+        const int limit = a.mask ? at.len : base + (hr_end - 1) / G + 1;                 // slots that any of them sees
+        beg = split * a.kps;
+        end = min(limit, beg + a.kps);
+        if (beg >= end) return false;
+        n_st = (end - beg + KEYS - 1) / KEYS;
+        table = a.pg.table + (size_t)at.b * a.pg.table_width;
+        rw = wave / KW;
+        kw = wave % KW;
+        col = lane & 31;
+        h = lane >> 5;
+        k_lane = (col >> 4) * 2 * BLK + (h * 16 + (col & 15)) * 16;
+        v_lane = (((col >> 4) * 4 + h) * 16 + (col & 15)) * (int)sizeof(vraw);
+        const int mine = min(hr0 + rw * 32 + col, hr_end - 1), tok = mine / G, row = at.row0 + tok;
+        live = hr0 + rw * 32 + col < hr_end;
+        head_row = (size_t)row * a.n_q + kvh * G + mine % G;
+        q = (const char*)a.q + ((size_t)row * a.q_stride + (size_t)(kvh * G + mine % G) * HD) * sizeof(T) + h * 16;
+        bits = 0;
+        if (a.mask) bits = a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull);
+        const int r_first = min(hr0 + rw * 32, hr_end - 1), r_last = min(hr0 + rw * 32 + 31, hr_end - 1);
+        sees_all = a.mask ? base : base + r_first / G + 1;
+        sees_any = hr0 + rw * 32 >= hr_end ? 0 : a.mask ? at.len : base + r_last / G + 1;
+        lim = base + tok + 1;
+        return true;
+    }
 
     // A wave's part of the stages: K or V of NBW blocks, or both, whose addresses are
     // looked up for many stages at once, one to a lane.  The loads go to LDS by asm: of
     // those that it knows the compiler would wait for all before any read of LDS.
-    constexpr int PW = 2 * NB / NW, NBW = NB > NW ? NB / NW : 1, AHEAD = 64 / NBW;
-    static_assert(PW >= 1 && PW % NBW == 0, "the waves share a stage evenly");
-    const int last = (end - 1) >> 4, blk0 = (beg >> 4) + wave % NB;
-    const unsigned ring = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    int next = 0, off_lo = 0, off_hi = 0;
-    auto my_block = [&](int st) { return min(blk0 + (st + lane / NBW) * NB + lane % NBW * NW, last); };
-    auto look = [&](int st) { next = table[my_block(st) >> bsh]; };
-    auto issue = [&](int st) {
+    __device__ __forceinline__ int my_block(int st) const {
+        return min((beg >> 4) + wave % NB + (st + lane / NBW) * NB + lane % NBW * NW, (end - 1) >> 4);
+    }
+    __device__ __forceinline__ void look(int st) { next = table[my_block(st) >> a.pg.page_shift]; }
+    __device__ __forceinline__ void issue(int st) {
         if (st % AHEAD == 0) {
             const int id = next >= 0 && next < a.pg.n_pages ? next : 0;          // (a bad page ends without output)
             const long long off = ((long long)id * a.pg.page_stride + (long long)kvh * a.pg.head_stride +
-                                   (long long)(my_block(st) & ((1 << bsh) - 1)) * (16 * HD)) * (long long)sizeof(T);
+                                   (long long)(my_block(st) & ((1 << a.pg.page_shift) - 1)) * (16 * HD)) * (long long)sizeof(T);
             off_lo = (int)(off & 0xffffffffll);
             off_hi = (int)(off >> 32);
             look(st + AHEAD);
         }
+        const unsigned ring = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
 #pragma unroll
         for (int j = 0; j < PW; ++j) {
             const int pair = wave + NW * j, blk = pair % NB, kv = pair / NB, i = st % AHEAD * NBW + j % NBW;
-            const char* src = (kv ? a.pg.v : a.pg.k) + lane * 16 +
+            // (the address in scalars: a vector addition of 64 bits a KiB was a fifth of the loop's)
+            const char* src = (kv ? a.pg.v : a.pg.k) +
                               ((size_t)(unsigned)__builtin_amdgcn_readlane(off_lo, i) |
                                (size_t)(unsigned)__builtin_amdgcn_readlane(off_hi, i) << 32);
             const unsigned dst = __builtin_amdgcn_readfirstlane(ring + (unsigned)(st % RING) * SB + (unsigned)(blk * 2 + kv) * BLK);
+            if (a.once) {
 #pragma unroll
-            for (int c = 0; c < BLK / 1024; ++c)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                             :: "s"(dst + c * 1024), "v"(src + c * 1024) : "memory", "m0");
+                for (int c = 0; c < BLK / 1024; ++c)
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+                                 :: "s"(dst + c * 1024), "v"(lane * 16), "s"(src + c * 1024) : "memory", "m0");
+            } else {
+#pragma unroll
+                for (int c = 0; c < BLK / 1024; ++c)
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                                 :: "s"(dst + c * 1024), "v"(lane * 16), "s"(src + c * 1024) : "memory", "m0");
+            }
         }
-    };
-    constexpr int LOADS = PW * BLK / 1024;           // a wave's of a stage
-    static_assert(LOADS * (RING - 2) < 64, "the loads in flight fit the wait counter");
-    auto start = [&] {
-        look(0);
-#pragma unroll
-        for (int st = 0; st < RING - 1; ++st)
-            if (st < n_st) issue(st);
-    };
-    // opens stage `it`: every wave's loads of it are there, every wave is past the one whose place is filled next
-    auto open = [&](int it) {
-        const int left = min(n_st - 1 - it, RING - 2);
-        if (RING >= 4 && left >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(RING >= 4 ? 2 * LOADS : 0) : "memory");
-        else if (RING >= 3 && left >= 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(RING >= 3 ? LOADS : 0) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (it + RING - 1 < n_st) issue(it + RING - 1);
-    };
-    start();
-
-    const int rw = wave / KW, kw = wave % KW, col = lane & 31, h = lane >> 5;
-    // this lane's head row (past the last: the last) and what it sees
-    const int mine = min(hr0 + rw * 32 + col, hr_end - 1), tok = mine / G, row = at.row0 + tok;
-    const bool live = hr0 + rw * 32 + col < hr_end;
-    const size_t head_row = (size_t)row * a.n_q + kvh * G + mine % G;
-    const char* q = (const char*)a.q + ((size_t)row * a.q_stride + (size_t)(kvh * G + mine % G) * HD) * sizeof(T) + h * 16;
-    uint4 qf[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = *(const uint4*)(q + s * 32);
-    unsigned long long bits = 0;
-    if (a.mask) bits = a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull);
-    // pages that the sequence's slots use, all of them in every work-group: the same answer
-    {
-        const int pages = (at.len + (16 << bsh) - 1) >> (bsh + 4);
-        bool bad = false;
-        for (int p = wave * 64 + lane; p < pages; p += NW * 64) {
-            const int id = table[p];
-            bad |= id < 0 || id >= a.pg.n_pages;
-        }
-        if (__any(bad) && lane == 0) s_bad = 1;
     }
-    // slots that all of the wave's rows see, and those that any does
-    const int r_first = min(hr0 + rw * 32, hr_end - 1), r_last = min(hr0 + rw * 32 + 31, hr_end - 1);
-    const int sees_all = a.mask ? base : base + r_first / G + 1;
-    const int sees_any = a.mask ? at.len : base + r_last / G + 1;
-    const int lim = base + tok + 1;
-    // what the lane's row sees of the 32 slots from k0 on: bit j slot k0 + j
-    auto seen_of = [&](int k0) -> unsigned {
+    __device__ __forceinline__ void start() {
+        look(0);
+        issue(0);
+    }
+    // Opens stage `it`: every wave's loads of it are there, and every wave is past the one
+    // whose place the next is loaded to.
+    __device__ __forceinline__ const unsigned char* open(int it) const {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        return smem + (size_t)(it % RING) * SB;
+    }
+    __device__ __forceinline__ void ahead(int it) {
+        if (it + 1 < n_st) issue(it + 1);
+    }
+
+    // What the lane's row sees of the 32 slots from k0 on: bit j slot k0 + j.
+    __device__ __forceinline__ unsigned seen_of(int k0) const {
         const int d = a.mask ? k0 - base : k0 - lim;
         if (d <= -32) return ~0u;
         if (d < 0) return ((1u << -d) - 1) | (unsigned)(bits << -d);
         return d < 64 ? (unsigned)(bits >> d) : 0u;
-    };
-    auto k_frag = [&](const unsigned char* st, int s) {
-        return *(const uint4*)(st + (col >> 4) * 2 * BLK + ((2 * s + h) * 16 + (col & 15)) * 16);
-    };
+    }
+    // K of the 32 slots at st, step s of the dims
+    __device__ __forceinline__ uint4 k_frag(const unsigned char* st, int s) const {
+        return *(const uint4*)(st + k_lane + s * 512);
+    }
     // scores of hidden slots are -inf (element i of a lane: slot 8 (i / 4) + 4 h + i % 4)
-    auto hide = [&](f32x16& sc, unsigned seen) {
+    __device__ __forceinline__ void hide(f32x16& sc, unsigned seen) const {
         seen >>= 4 * h;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (!(seen & (1u << (8 * (i / 4) + i % 4)))) sc[i] = -INFINITY;
-    };
+    }
     // V of block u, tile t: the lane's slots 4 h .. and 8 + 4 h .. of its dim
-    auto v_frag = [&](const unsigned char* st, int u, int t, vraw (&v)[2]) {
-        const unsigned char* at = st + u * 2 * BLK + BLK + (((t * 2 + (col >> 4)) * 4 + h) * 16 + (col & 15)) * sizeof(vraw);
-        v[0] = *(const vraw*)at;
-        v[1] = *(const vraw*)(at + 32 * sizeof(vraw));
-    };
+    __device__ __forceinline__ void v_frag(const unsigned char* st, int u, int t, vraw (&v)[2]) const {
+        const unsigned char* p = st + v_lane + (u * 2 * BLK + BLK + t * 128 * (int)sizeof(vraw));
+        v[0] = *(const vraw*)p;
+        v[1] = *(const vraw*)(p + 32 * sizeof(vraw));
+    }
     // ... without the slots from `cut` of the step on, which hold nothing
-    auto v_cut = [&](int u, int cut, vraw (&v)[2]) {
+    __device__ __forceinline__ void v_cut(int u, int cut, vraw (&v)[2]) const {
         keep_first(v[0], cut - 16 * u - 4 * h);
         keep_first(v[1], cut - 16 * u - 8 - 4 * h);
-    };
+    }
 
-    f32x16 o[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-    float m = -INFINITY, ref = 0.f, l = 0.f;         // running maximum, the same as a finite number, sum of the lane's weights
-    for (int it = 0; it < n_st; ++it) {
-        open(it);
-        const unsigned char* stage = smem + (size_t)(it % RING) * SB + kw * NS * 4 * BLK;
-        const int first = beg + it * KEYS + kw * NS * 32;
-        if (first >= sees_any) continue;
-        uint4 kf[KS];
-#pragma unroll
-        for (int s = 0; s < KS; ++s) kf[s] = k_frag(stage, s);
-#pragma unroll
-        for (int c = 0; c < NS; ++c) {
-            const unsigned char* st = stage + c * 4 * BLK;
-            const int k0 = first + c * 32;
-            f32x16 sc;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = 0.f;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) mma32<T>(sc, kf[s], qf[s]);
-            // V on its way while the weights are made
-            vraw v[2][NT][2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) v_frag(st, u, t, v[u][t]);
-            settle<T>();
-            if (k0 + 32 > sees_all) hide(sc, seen_of(k0));
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[i]);
-            top *= a.scale_log2;
-            if (__any(top > m + SLACK)) {
-                top = fmaxf(m, half_max(top));
-                const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-                l *= f;
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[t][i] *= f;
-                m = top;
-                ref = top == -INFINITY ? 0.f : top;
-            }
-            T p[2][8];
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -ref));
-                sum[i % 4] += w;
-                // rounded to the cache's type for the product, as the passes of the step do
-                p[i / 8][i % 8] = from_f32<T>(w);
-            }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            if (k0 + 32 > at.len) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) v_cut(u, at.len - k0, v[u][t]);
-            }
-            if (c + 1 < NS) {
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kf[s] = k_frag(st + 4 * BLK, s);
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) mma_block<T>(o[t], v[u][t][0], v[u][t][1], p[u]);
-            settle<T>();
-        }
-    }
-    l = half_sum(l);
-    {
-        f32x16 all = o[0];
-#pragma unroll
-        for (int t = 1; t < NT; ++t) all += o[t];
-        float one = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) one += all[i];
-        if (__any(live && one != one) && lane == 0) s_odd = 1;
-    }
-    lds_sync();                                      // every wave past the last stage; s_bad and s_odd are final
-    const bool redo = s_odd != 0, bad = s_bad != 0;
-    if constexpr (KW > 1) {
-        float* part = (float*)smem + (size_t)rw * 64 * (NT * 16 + 2);
-        if (kw > 0) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) part[(t * 16 + i) * 64 + lane] = o[t][i];
-            part[NT * 16 * 64 + lane] = m;
-            part[(NT * 16 + 1) * 64 + lane] = l;
-        }
-        lds_sync();
-        if (kw == 0) {
-            const float mw = part[NT * 16 * 64 + lane], lw = part[(NT * 16 + 1) * 64 + lane], M = fmaxf(m, mw);
-            // (a wave that saw nothing but -inf has a sum of 0 or NaN of its own)
-            const float f0 = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);
-            const float f1 = mw == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw - M);
-            l = l * f0 + lw * f1;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[t][i] = o[t][i] * f0 + part[(t * 16 + i) * 64 + lane] * f1;
-            m = M;
-            ref = m == -INFINITY ? 0.f : m;
-        }
-        lds_sync();                                  // the ring may be filled again
-    }
-    if (bad && threadIdx.x == 0) raise(a.pg.status, PBD_STATUS_PAGE);
-    const bool none = a.mask && base == 0 && bits == 0;          // a row that sees no slot
-    const float inv = none ? 0.f : 1.f / l;
-    const size_t part_row = head_row * a.splits + split;
-    // 32 dims of the lane's head row from 32 t on: the output's, or the split's sums
-    auto put = [&](int t, const f32x16& v) {
+    // 32 dims of the lane's head row from 32 t on: the output's, or the split's sums.
+    __device__ __forceinline__ void put(int t, const f32x16& v, float inv, bool bad) const {
         if (kw > 0 || !live || (a.direct && bad)) return;
+        const size_t part_row = head_row * a.splits + split;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int d = 32 * t + 8 * j + 4 * h;
@@ -469,88 +370,288 @@ void k_rows_attn(RowsAttnArgs a) {
                 *(f32x4*)(a.part_o + part_row * HD + d) = f32x4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
             }
         }
-    };
-    if (kw == 0 && live && h == 0) {
-        if (!a.direct) {
-            a.part_ml[part_row * 2] = bad ? __builtin_nanf("") : m;
-            a.part_ml[part_row * 2 + 1] = l;
-        } else if (a.lse && !bad) {
-            a.lse[head_row] = log_sum(m, l, none);
+    }
+    __device__ __forceinline__ bool none() const { return a.mask && base == 0 && bits == 0; }    // the row sees no slot
+
+    // The pass over the slots: outputs, or true where a NaN asks for the careful one.  m, l:
+    // the row's maximum and sum (waves of kw 0).
+    __device__ __forceinline__ bool run(int* s_bad, int* s_odd, float& m, float& l) {
+        uint4 qf[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[s] = *(const uint4*)(q + s * 32);
+        // pages that the sequence's slots use, all of them in every work-group: the same answer
+        {
+            const int sh = a.pg.page_shift + 4, pages = (at.len + (1 << sh) - 1) >> sh;
+            bool bad = false;
+            for (int p = wave * 64 + lane; p < pages; p += NW * 64) {
+                const int id = table[p];
+                bad |= id < 0 || id >= a.pg.n_pages;
+            }
+            if (__any(bad) && lane == 0) *s_bad = 1;
         }
-    }
-    if (__builtin_expect(!redo, true)) {
+        // the queries are there before the first stage is requested: the compiler, which does not
+        // count the stages' loads, would wait for all of them in their place in every turn
 #pragma unroll
-        for (int t = 0; t < NT; ++t) put(t, o[t]);
-        return;
-    }
-#pragma unroll 1
-    for (int t = 0; t < NT; ++t) {
-        f32x16 v;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = 0.f;
+        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s].x), "+v"(qf[s].y), "+v"(qf[s].z), "+v"(qf[s].w));
         start();
+        f32x16 o[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+        float ref = 0.f;                             // the running maximum as a finite number
+        m = -INFINITY;
+        float part[4] = {0.f, 0.f, 0.f, 0.f};        // sums of the lane's weights
+        bool first_step = true;                      // some row has no reference
+        float scale = a.scale_log2;
+        asm volatile("" : "+v"(scale));              // (kept: as a scalar it was spilled to a lane, and fetched every step)
         for (int it = 0; it < n_st; ++it) {
-            open(it);
-#pragma unroll 1
-            for (int c = 0; c < NB / 2; ++c) {
-                const unsigned char* st = smem + (size_t)(it % RING) * SB + c * 4 * BLK;
-                const int k0 = beg + it * KEYS + c * 32;
-                if (kw > 0 || k0 >= sees_any) break;
+            const unsigned char* stage = open(it) + kw * NS * 4 * BLK;
+            ahead(it);
+            const int first = beg + it * KEYS + kw * NS * 32;
+            if (first >= sees_any) continue;
+            uint4 kf[KS];
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[s] = k_frag(stage, s);
+            __builtin_amdgcn_sched_barrier(0);       // (all of them requested first)
+#pragma unroll
+            for (int c = 0; c < NS; ++c) {
+                const unsigned char* st = stage + c * 4 * BLK;
+                const int k0 = first + c * 32;
                 f32x16 sc;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
-                for (int s = 0; s < KS; ++s) mma32<T>(sc, k_frag(st, s), *(const uint4*)(q + s * 32));
-                settle<T>();
-                const unsigned seen = seen_of(k0);
-                hide(sc, seen);
-#pragma unroll 1
-                for (int u = 0; u < 2; ++u) {
-                    T p[8];
+                for (int s = 0; s < KS; ++s) mma32<T>(sc, kf[s], qf[s]);
+                // V on its way while the weights are made
+                vraw v[2][NT][2];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        p[i] = from_f32<T>(__builtin_amdgcn_exp2f(__builtin_fmaf(u ? sc[8 + i] : sc[i], a.scale_log2, -ref)));
-                    vraw x[2];
-                    v_frag(st, u, t, x);
-                    v_cut(u, at.len - k0, x);
-                    mma_block_careful<T>(v, x[0], x[1], p, seen >> (16 * u + 4 * h));
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) v_frag(st, u, t, v[u][t]);
+                settle<T>();
+                if (k0 + 32 > sees_all) hide(sc, seen_of(k0));
+                float w[16], sum[4];
+                auto weights = [&] {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], scale, -ref));
+                        sum[i % 4] = i < 4 ? w[i] : sum[i % 4] + w[i];
+                    }
+                };
+                weights();
+                // the sums tell of a score far above the reference; the first ones have none
+                if (__any(fmaxf(fmaxf(sum[0], sum[1]), fmaxf(sum[2], sum[3])) > HIGH) || first_step) {
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[i]);
+                    top = fmaxf(m, half_max(top * scale));
+                    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) part[i] *= f;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[t][i] *= f;
+                    m = top;
+                    ref = top == -INFINITY ? 0.f : top;
+                    first_step = __any(m == -INFINITY);
+                    weights();
                 }
+                T p[2][8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) part[i] += sum[i];
+                // rounded to the cache's type for the product, as the passes of the step do
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p[i / 8][i % 8] = from_f32<T>(w[i]);
+                if (k0 + 32 > at.len) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) v_cut(u, at.len - k0, v[u][t]);
+                }
+                if (c + 1 < NS) {
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) kf[s] = k_frag(st + 4 * BLK, s);
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) mma_block<T>(o[t], v[u][t][0], v[u][t][1], p[u]);
+                settle<T>();
             }
         }
-        lds_sync();
-        put(t, v);
+        l = half_sum((part[0] + part[1]) + (part[2] + part[3]));
+        {
+            f32x16 all = o[0];
+#pragma unroll
+            for (int t = 1; t < NT; ++t) all += o[t];
+            float one = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) one += all[i];
+            if (__any(live && one != one) && lane == 0) *s_odd = 1;
+        }
+        lds_sync();                                  // every wave past the last stage; s_bad and s_odd are final
+        const bool redo = *s_odd != 0, bad = *s_bad != 0;
+        if constexpr (KW > 1) {
+            float* part = (float*)smem + (size_t)rw * 64 * (NT * 16 + 2);
+            if (kw > 0) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) part[(t * 16 + i) * 64 + lane] = o[t][i];
+                part[NT * 16 * 64 + lane] = m;
+                part[(NT * 16 + 1) * 64 + lane] = l;
+            }
+            lds_sync();
+            if (kw == 0) {
+                const float mw = part[NT * 16 * 64 + lane], lw = part[(NT * 16 + 1) * 64 + lane], M = fmaxf(m, mw);
+                // (a wave that saw nothing but -inf has a sum of 0 or NaN of its own)
+                const float f0 = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);
+                const float f1 = mw == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw - M);
+                l = l * f0 + lw * f1;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[t][i] = o[t][i] * f0 + part[(t * 16 + i) * 64 + lane] * f1;
+                m = M;
+            }
+            lds_sync();                              // the ring may be filled again
+        }
+        if (bad && threadIdx.x == 0) raise(a.pg.status, PBD_STATUS_PAGE);
+        if (kw == 0 && live && h == 0) {
+            const size_t part_row = head_row * a.splits + split;
+            if (!a.direct) {
+                a.part_ml[part_row * 2] = bad ? __builtin_nanf("") : m;
+                a.part_ml[part_row * 2 + 1] = l;
+            } else if (a.lse && !bad) {
+                a.lse[head_row] = log_sum(m, l, none());
+            }
+        }
+        if (__builtin_expect(redo, false)) return true;
+        const float inv = none() ? 0.f : 1.f / l;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) put(t, o[t], inv, bad);
+        return false;
     }
+
+    // The careful pass, under the maximum and the sum that the first one found.
+    __device__ __forceinline__ void again(float m, float l, bool bad) {
+        const float ref = m == -INFINITY ? 0.f : m, inv = none() ? 0.f : 1.f / l;
+#pragma unroll 1
+        for (int t = 0; t < NT; ++t) {
+            f32x16 v;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = 0.f;
+            start();
+            for (int it = 0; it < n_st; ++it) {
+                const unsigned char* stage = open(it);
+                ahead(it);
+#pragma unroll 1
+                for (int c = 0; c < NB / 2; ++c) {
+                    const unsigned char* st = stage + c * 4 * BLK;
+                    const int k0 = beg + it * KEYS + c * 32;
+                    if (kw > 0 || k0 >= sees_any) break;
+                    f32x16 sc;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) mma32<T>(sc, k_frag(st, s), *(const uint4*)(q + s * 32));
+                    settle<T>();
+                    const unsigned seen = seen_of(k0);
+                    hide(sc, seen);
+#pragma unroll 1
+                    for (int u = 0; u < 2; ++u) {
+                        T p[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            p[i] = from_f32<T>(__builtin_amdgcn_exp2f(__builtin_fmaf(u ? sc[8 + i] : sc[i], a.scale_log2, -ref)));
+                        vraw x[2];
+                        v_frag(st, u, t, x);
+                        v_cut(u, at.len - k0, x);
+                        mma_block_careful<T>(v, x[0], x[1], p, seen >> (16 * u + 4 * h));
+                    }
+                }
+            }
+            lds_sync();                              // every wave past the last stage
+            put(t, v, inv, bad);
+        }
+    }
+};
+
+template <typename T, int HD, int RW, int KW>
+__global__ __launch_bounds__(RW * KW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && HD == 128 ? 1 : 2)))
+void k_rows_attn(RowsAttnArgs a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ int s_bad, s_odd;
+    if (blockIdx.x == 0 && blockIdx.y == 0) report_bad(a);
+    float m, l;
+    {
+        RowsWork<T, HD, RW, KW> w(a, smem);
+        if (!w.place(blockIdx.x)) return;
+        if (threadIdx.x == 0) s_bad = s_odd = 0;
+        lds_sync();
+        if (!w.run(&s_bad, &s_odd, m, l)) return;
+    }
+    // everything is found anew, so that the first pass keeps no registers for this one
+    int block = blockIdx.x;
+    asm volatile("" : "+s"(block));
+    RowsWork<T, HD, RW, KW> w(a, smem);
+    if (w.place(block)) w.again(m, l, s_bad != 0);
 }
 
-// Joins the splits of head rows, in split order; HD / 4 lanes to a head row.
+// Joins the splits of head rows, one wave to a row: a lane has one split's maximum and
+// sum (and those 64 on), HD / 4 lanes the row's dims of every SETS-th split; the same
+// order whatever ran first.
 template <typename T, int HD, int ROWS>
 __global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
-    constexpr int LANES = HD / 4, N = 256 / LANES;
-    const int kvh = blockIdx.x % a.n_kv, group = blockIdx.x / a.n_kv;
+    constexpr int LANES = HD / 4, SETS = 64 / LANES, UNROLL = 8;
+    const int kvh = blockIdx.x % a.n_kv, group = blockIdx.x / a.n_kv, lane = threadIdx.x & 63;
     const Place at = find_group<ROWS>(a, group);
     if (!at.ok) return;
-    const int G = a.n_q / a.n_kv, hr = at.tile * ROWS + blockIdx.y * N + (int)threadIdx.x / LANES, d = (int)threadIdx.x % LANES * 4;
+    const int G = a.n_q / a.n_kv, hr = at.tile * ROWS + blockIdx.y * 4 + (int)(threadIdx.x >> 6);
     if (hr >= min((at.tile + 1) * ROWS, at.n * G)) return;
     const int tok = hr / G, row = at.row0 + tok, base = at.len - at.n;
     const size_t head_row = (size_t)row * a.n_q + kvh * G + hr % G;
     const int n = ((a.mask ? at.len : base + tok + 1) + a.kps - 1) / a.kps;
     typedef float __attribute__((ext_vector_type(2))) ml2;
     const ml2* ml = (const ml2*)a.part_ml + head_row * a.splits;
+    const int d = lane % LANES * 4, set = lane / LANES;
     const float* part = a.part_o + head_row * a.splits * HD + d;
-    float M = -INFINITY, L = 0.f;
-    bool bad = false;
-    for (int s = 0; s < n; ++s) {
-        bad |= ml[s][0] != ml[s][0];
-        M = fmaxf(M, ml[s][0]);
+    f32x4 first[UNROLL];                             // the first splits' sums, requested with their scales
+#pragma unroll
+    for (int i = 0; i < UNROLL; ++i) first[i] = *(const f32x4*)(part + (size_t)min(set + i * SETS, n - 1) * HD);
+    const ml2 mine = ml[min(lane, n - 1)];
+    float M = lane < n ? mine[0] : -INFINITY;
+    bool bad = lane < n && mine[0] != mine[0];
+    for (int s = lane + 64; s < n; s += 64) {
+        const ml2 x = ml[s];
+        bad |= x[0] != x[0];
+        M = fmaxf(M, x[0]);
     }
-    if (bad) return;
+    if (__any(bad)) return;
+    M = wave_max_dpp(M);
+    auto scale = [&](ml2 x) { return x[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x[0] - M); };
+    float L = lane < n ? mine[1] * scale(mine) : 0.f;
+    for (int s = lane + 64; s < n; s += 64) {
+        const ml2 x = ml[s];
+        L += x[1] * scale(x);
+    }
+    L = wave_sum_dpp(L);
     f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < n; ++s) {
-        const float f = ml[s][0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[s][0] - M);
-        L += ml[s][1] * f;
-        acc += *(const f32x4*)(part + (size_t)s * HD) * f;
+    const float f0 = scale(mine);
+#pragma unroll
+    for (int i = 0; i < UNROLL; ++i) {
+        const int s = set + i * SETS;
+        const float f = __shfl(f0, min(s, 63), 64);
+        if (s < n) acc += first[i] * f;
     }
+    for (int s = set + UNROLL * SETS; s < n; s += SETS) acc += *(const f32x4*)(part + (size_t)s * HD) * scale(ml[s]);
+#pragma unroll
+    for (int w = LANES; w < 64; w *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], w, 64);
+    if (set != 0) return;
     const bool none = a.mask && base == 0 && (a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull)) == 0;
     const float inv = none ? 0.f : 1.f / L;
     const float x[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
@@ -560,22 +661,47 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
 
 }  // namespace
 
-// Work-groups wanted where a call has fewer: two a CU.
-constexpr int GROUPS_WANTED = 512;
-constexpr int KPS_MIN = 256;
-
+// The work-group that takes a call's rows and the parts that the slots are split into.
+//
+// Two tiles by two waves (64 rows) fill the chip with half the rows; four tiles by one
+// wave read K and V half as often.  One prompt of 2048 tokens (16 / 8 heads of 128,
+// bf16) takes 37 us on the first and 50 on the second, of 4096 94 and 100, two of 8192
+// 630 and 545, six mixed ones with four heads a KV head 277 and 255.  Where a sequence
+// has at most 64 rows in bf16, four tiles leave two waves that only load: 64 trees of 17
+// nodes over 1000 slots take 48 us so and 63 on two tiles, 48 of 32 over 2000 70 and
+// 101; few trees take the same on both.
+//
+// A part costs its work-groups' start, its partial sums (written and read) and a join,
+// and saves stages: the estimate below, in us, is within 15 % of what these took (times
+// for the parts it takes, and for twice as many): a prompt of 1024 tokens 21 and 29 us,
+// 64 rows over 16384 slots 31 (32 parts; 16: 34), 512 over 8192 59 (4; 2: 84), 16 trees
+// of 64 nodes over 2000 slots 46 and 60, one tree of 17 over 4096 13 (32; 16: 14.2).
 RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int rows, int max_len) {
     RowsAttnPlan p{};
-    const long long G = n_q / n_kv, each = (long long)rows * G / batch;
-    p.tiles = each > 64 ? 4 : each > 32 ? 2 : 1;
-    const int R = p.tiles * 32, keys = dtype == PBD_DTYPE_BF16 ? 64 : 32;
-    p.groups = (long long)rows * G / R + batch;
-    const long long live = ((long long)rows * G + R - 1) / R * n_kv;             // (as many as that have rows, about)
-    long long splits = std::max<long long>(1, std::min<long long>(GROUPS_WANTED / std::max(1ll, live), max_len / KPS_MIN));
-    long long kps = (max_len + splits - 1) / splits;
-    kps = std::max<long long>(keys, (kps + keys - 1) / keys * keys);
-    p.kps = (int)kps;
-    p.splits = (int)((max_len + kps - 1) / kps);
+    const bool half = dtype == PBD_DTYPE_BF16;
+    const long long G = n_q / n_kv, head_rows = (long long)rows * G, each = head_rows / batch;
+    p.tiles = (half && each <= 64) || (head_rows + 127) / 128 * n_kv >= 1024 ? 4 : 2;
+    const int R = p.tiles * 32;
+    p.groups = head_rows / R + batch;
+    p.once = each <= R;
+    const long long live = std::max<long long>((head_rows + R - 1) / R, batch) * n_kv;   // work-groups with rows, about
+    const double stage = (half ? 1.0 : 4.0) * (p.tiles == 4 ? 1.5 : 1.0) * head_dim / 128;
+    const double bytes = 2.0 * batch * max_len * n_kv * head_dim * (half ? 2 : 4);
+    const double partial = 2.0 * rows * n_q * head_dim * 4;
+    const int most = std::min(64, (max_len + KEYS - 1) / KEYS);
+    double best = 0;
+    for (int s = 1; s <= most; ++s) {
+        const bool alone = live * s <= 256;                                       // one work-group a CU
+        if (s > 1 && live * s > 512) break;
+        const int kps = ((max_len + s - 1) / s + KEYS - 1) / KEYS * KEYS;
+        if ((max_len + kps - 1) / kps != s) continue;                             // (fewer parts do the same)
+        const double memory = bytes / (p.tiles == 2 ? (alone ? 5.6e6 : 4.2e6) : (alone ? 4.8e6 : 5.6e6));
+        const double est = std::max((kps / KEYS) * stage * (alone ? 1.0 : 1.1), memory) + (s > 1 ? 4 + s * partial / 4e6 : 0);
+        if (s > 1 && est >= best) continue;
+        best = est;
+        p.kps = kps;
+        p.splits = s;
+    }
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     const size_t n = p.splits == 1 ? 0 : (size_t)rows * n_q * p.splits;
     p.off_ml = up(n * head_dim * 4);
@@ -586,21 +712,18 @@ RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batc
 namespace {
 template <typename T, int HD, int RW, int KW>
 hipError_t launch(const RowsAttnArgs& a, const RowsAttnPlan& p, hipStream_t st) {
-    constexpr size_t lds = (size_t)ROWS_RING * Stage<T>::BLOCKS * 2 * 16 * HD * sizeof(T);
-    static_assert(KW == 1 || (size_t)RW * (KW - 1) * 64 * (HD / 2 + 2) * 4 <= lds, "the other waves' sums lie over the ring");
-    PBD_LAUNCH((k_rows_attn<T, HD, RW, KW>), dim3((unsigned)(p.groups * a.n_kv), p.splits), dim3(RW * KW * 64), lds, st, a);
+    constexpr size_t ring = (size_t)RING * NB * 2 * 16 * HD * sizeof(T);
+    static_assert(KW == 1 || (size_t)RW * (KW - 1) * 64 * (HD / 2 + 2) * 4 <= ring, "the other waves' sums lie over the ring");
+    PBD_LAUNCH((k_rows_attn<T, HD, RW, KW>), dim3((unsigned)(p.groups * a.n_kv), p.splits), dim3(RW * KW * 64), ring, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.direct) return e;
-    PBD_LAUNCH((k_rows_join<T, HD, RW * 32>), dim3((unsigned)(p.groups * a.n_kv), RW * 32 * HD / 1024), dim3(256), 0, st, a);
+    PBD_LAUNCH((k_rows_join<T, HD, RW * 32>), dim3((unsigned)(p.groups * a.n_kv), RW * 8), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
 template <typename T, int HD>
 hipError_t launch_tiles(const RowsAttnArgs& a, const RowsAttnPlan& p, hipStream_t st) {
-    constexpr int KW = sizeof(T) == 2 ? 2 : 1;
-    if (p.tiles == 4) return launch<T, HD, 4, 1>(a, p, st);
-    if (p.tiles == 2) return launch<T, HD, 2, KW>(a, p, st);
-    return launch<T, HD, 1, KW>(a, p, st);
+    return p.tiles == 4 ? launch<T, HD, 4, 1>(a, p, st) : launch<T, HD, 2, 2>(a, p, st);
 }
 }  // namespace
 

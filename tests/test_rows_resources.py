@@ -1,5 +1,5 @@
-"""Compile-time checks of the packed-row kernels (CPU, needs hipcc): no scratch memory, registers for two waves a SIMD at
-least, no vector instruction that reads an MFMA result too early, no product that takes another's result as an operand."""
+"""Compile-time checks of the packed-row kernels (CPU, needs hipcc): no scratch memory, registers for two waves a SIMD (one
+in fp32, whose stages fill the LDS), no vector instruction that reads an MFMA result too early, no product that takes another's result as an operand."""
 import os
 import re
 import shutil
@@ -27,7 +27,10 @@ def test_kernels_use_no_scratch_and_wait_for_mfma(src, mfma, tmp_path):
     vgprs = [int(x) for x in re.findall(r" VGPRs: (\d+)", r.stdout)]
     agprs = [int(x) for x in re.findall(r" AGPRs: (\d+)", r.stdout)]
     assert scratch and max(scratch) == 0, scratch
-    assert max(v + a for v, a in zip(vgprs, agprs)) <= 256
+    names = re.findall(r"Function Name: (\S+)", r.stdout)
+    assert len(names) == len(vgprs)
+    for name, v, a in zip(names, vgprs, agprs):
+        assert v + a <= (512 if "k_rows_attnIf" in name else 256), (name, v, a)
     asm = out.read_text()
     assert asm.count("v_mfma") >= mfma
     assert not early_reads(asm)[:10]
