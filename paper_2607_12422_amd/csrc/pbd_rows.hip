@@ -661,47 +661,52 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
 
 }  // namespace
 
-// The work-group that takes a call's rows and the parts that the slots are split into.
+// The tiles of a work-group, and the parts that the slots are split into: the pair of
+// least estimated time (us; 16-bit products of 128 dims, others by their length).
 //
-// Two tiles by two waves (64 rows) fill the chip with half the rows; four tiles by one
-// wave read K and V half as often.  One prompt of 2048 tokens (16 / 8 heads of 128,
-// bf16) takes 37 us on the first and 50 on the second, of 4096 94 and 100, two of 8192
-// 630 and 545, six mixed ones with four heads a KV head 277 and 255.  Where a sequence
-// has at most 64 rows in bf16, four tiles leave two waves that only load: 64 trees of 17
-// nodes over 1000 slots take 48 us so and 63 on two tiles, 48 of 32 over 2000 70 and
-// 101; few trees take the same on both.
+// A stage takes 1 us of two tiles by two waves (64 rows) and 1.5 of four by one, which
+// read K and V half as often, 10 % more with two work-groups a CU; K and V come at 4.2
+// to 5.6 TB/s; a part costs its partial sums, written and read, and a join.  Times (16 /
+// 8 heads of 128, bf16; two and four tiles): one prompt of 2048 tokens 37 and 50 us, of
+// 4096 94 and 100, two of 8192 630 and 545, six mixed ones of four heads a KV head 277 and
+// 255; (parts taken, and others) a prompt of 1024 21 (1) and 29 (2), 64 rows over 16384
+// slots 31 (32) and 34 (16), 512 over 8192 59 (4) and 84 (2), 16 trees of 64 nodes over
+// 2000 46 (1) and 60 (2), one tree of 17 over 4096 13 (32) and 14.2 (16).
 //
-// A part costs its work-groups' start, its partial sums (written and read) and a join,
-// and saves stages: the estimate below, in us, is within 15 % of what these took (times
-// for the parts it takes, and for twice as many): a prompt of 1024 tokens 21 and 29 us,
-// 64 rows over 16384 slots 31 (32 parts; 16: 34), 512 over 8192 59 (4; 2: 84), 16 trees
-// of 64 nodes over 2000 slots 46 and 60, one tree of 17 over 4096 13 (32; 16: 14.2).
+// Where a bf16 sequence has at most 64 rows, four tiles leave two waves that only load:
+// 64 trees of 17 nodes over 1000 slots take 48 us so and 63 on two tiles, 48 of 32 over
+// 2000 70 and 101; few trees the same on both.
 RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int rows, int max_len) {
     RowsAttnPlan p{};
     const bool half = dtype == PBD_DTYPE_BF16;
-    const long long G = n_q / n_kv, head_rows = (long long)rows * G, each = head_rows / batch;
-    p.tiles = (half && each <= 64) || (head_rows + 127) / 128 * n_kv >= 1024 ? 4 : 2;
+    const long long G = n_q / n_kv, head_rows = (long long)rows * G, each = (head_rows + batch - 1) / batch;
+    const double bytes = 2.0 * batch * max_len * n_kv * head_dim * (half ? 2 : 4);
+    const double partial = 2.0 * rows * n_q * head_dim * 4;
+    // of the slots, the share that an average row sees
+    const double seen = 1.0 - 0.5 * std::min(1.0, (double)rows / batch / max_len);
+    const int most = std::min(64, (max_len + KEYS - 1) / KEYS);
+    double best = 0;
+    for (int tiles = half && each <= 64 ? 4 : 2; tiles <= 4; tiles += 2) {
+        const long long live = batch * ((each + tiles * 32 - 1) / (tiles * 32)) * n_kv;  // work-groups with rows, about
+        const double stage = (half ? 1.0 : 4.0) * (tiles == 4 ? 1.5 : 1.0) * head_dim / 128;
+        for (int s = 1; s <= most; ++s) {
+            if (s > 1 && live * s > 512) break;
+            const bool alone = live * s <= 256;                                   // one work-group a CU
+            const int kps = ((max_len + s - 1) / s + KEYS - 1) / KEYS * KEYS;
+            if ((max_len + kps - 1) / kps != s) continue;                         // (fewer parts do the same)
+            const double rate = each <= 64 ? (alone ? 4.8e6 : 5.6e6) : tiles == 4 ? 4.2e6 : 5.0e6;
+            const double one = (kps / KEYS) * stage * (alone ? 1.0 : 1.1);
+            const double est = std::max({one, one * seen * live * s / 512.0, bytes / rate}) + (s > 1 ? 4 + s * partial / 4e6 : 0);
+            if (best > 0 && est >= best) continue;
+            best = est;
+            p.tiles = tiles;
+            p.kps = kps;
+            p.splits = s;
+        }
+    }
     const int R = p.tiles * 32;
     p.groups = head_rows / R + batch;
     p.once = each <= R;
-    const long long live = std::max<long long>((head_rows + R - 1) / R, batch) * n_kv;   // work-groups with rows, about
-    const double stage = (half ? 1.0 : 4.0) * (p.tiles == 4 ? 1.5 : 1.0) * head_dim / 128;
-    const double bytes = 2.0 * batch * max_len * n_kv * head_dim * (half ? 2 : 4);
-    const double partial = 2.0 * rows * n_q * head_dim * 4;
-    const int most = std::min(64, (max_len + KEYS - 1) / KEYS);
-    double best = 0;
-    for (int s = 1; s <= most; ++s) {
-        const bool alone = live * s <= 256;                                       // one work-group a CU
-        if (s > 1 && live * s > 512) break;
-        const int kps = ((max_len + s - 1) / s + KEYS - 1) / KEYS * KEYS;
-        if ((max_len + kps - 1) / kps != s) continue;                             // (fewer parts do the same)
-        const double memory = bytes / (p.tiles == 2 ? (alone ? 5.6e6 : 4.2e6) : (alone ? 4.8e6 : 5.6e6));
-        const double est = std::max((kps / KEYS) * stage * (alone ? 1.0 : 1.1), memory) + (s > 1 ? 4 + s * partial / 4e6 : 0);
-        if (s > 1 && est >= best) continue;
-        best = est;
-        p.kps = kps;
-        p.splits = s;
-    }
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     const size_t n = p.splits == 1 ? 0 : (size_t)rows * n_q * p.splits;
     p.off_ml = up(n * head_dim * 4);
