@@ -91,7 +91,7 @@ __device__ __forceinline__ Place find_group(const RowsAttnArgs& a, int group) {
     p.row0 = r0;
     p.n = r1 - r0;
     const bool valid = r0 >= 0 && r1 >= r0 && r1 <= a.rows && p.len >= p.n && p.len <= a.max_len && (!a.mask || p.n <= TREE_MAX);
-    const long long t = valid ? group - first(p.b) : -1;
+    const long long t = valid ? group - ((long long)r0 * G / ROWS + p.b) : -1;
     p.tile = (int)t;
     p.ok = valid && t >= 0 && t * ROWS < (long long)p.n * G;
     return p;
@@ -249,7 +249,9 @@ struct RowsWork {
         const int G = a.n_q / a.n_kv;
         base = at.len - at.n;
         const int hr0 = at.tile * ROWS, hr_end = min(hr0 + ROWS, at.n * G);              // the group's head rows
-        const int limit = a.mask ? at.len : base + (hr_end - 1) / G + 1;                 // slots that any of them sees
+        // (a quotient is made in vector registers: back to a scalar, or the loop's tests are the lanes')
+        auto token = [&](int hr) { return __builtin_amdgcn_readfirstlane(hr / G); };
+        const int limit = a.mask ? at.len : base + token(hr_end - 1) + 1;                // slots that any of them sees
         beg = split * a.kps;
         end = min(limit, beg + a.kps);
         if (beg >= end) return false;
@@ -268,8 +270,8 @@ struct RowsWork {
         bits = 0;
         if (a.mask) bits = a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull);
         const int r_first = min(hr0 + rw * 32, hr_end - 1), r_last = min(hr0 + rw * 32 + 31, hr_end - 1);
-        sees_all = a.mask ? base : base + r_first / G + 1;
-        sees_any = hr0 + rw * 32 >= hr_end ? 0 : a.mask ? at.len : base + r_last / G + 1;
+        sees_all = a.mask ? base : base + token(r_first) + 1;
+        sees_any = hr0 + rw * 32 >= hr_end ? 0 : a.mask ? at.len : base + token(r_last) + 1;
         lim = base + tok + 1;
         return true;
     }
