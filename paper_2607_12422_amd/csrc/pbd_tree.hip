@@ -54,6 +54,10 @@ __global__ __launch_bounds__(256) void k_tree_layout(TreeLayoutArgs a) {
 // it by itself, a few steps of one vote each, and the first writes what it found.  The
 // path ascends, so that its i-th node lies at or past slot i: 16 slots at a time leave
 // for registers and come down, and none is overwritten before it was read.
+// What bounds it: a slot of a head lies in 16 lines of K (16 bytes of each) and 8 of V
+// (bf16, head_dim 128), all of them read and written.  32 trees of 33 to 64 nodes over
+// 28 layers of 8 heads, two slots moved on average, take 20 us: 88 MB of lines for 7 MB
+// of slots.  Four layers a work-group, their loads together, took 24.
 // ---------------------------------------------------------------------------
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_tree_commit(TreeCommitArgs a) {

@@ -157,6 +157,17 @@ def test_pages_layers_and_strides(page, major):
     c.check()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_many_layers_of_many_trees(dtype):
+    """More layers of sequences' heads than run at once, in a number that four does not divide."""
+    g = torch.Generator().manual_seed(7)
+    sizes = [3 + b % 30 for b in range(60)]
+    c = Commit([n + b % 7 for b, n in enumerate(sizes)], [rr.random_tree(n, g, back=2) for n in sizes], 5, 64, dtype, layers=7,
+               seed=4, right=1.0)
+    c.run()
+    c.check()
+
+
 def test_a_line_of_64_and_a_path_of_the_last_ones():
     line = list(range(-1, 63))
     late = [-1] * 32 + [0] + list(range(32, 63))     # node 32 hangs on node 0, then a line
