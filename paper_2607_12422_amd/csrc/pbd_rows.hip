@@ -3,14 +3,32 @@
 //
 // The rows of a sequence are packed behind those of the sequence before; for one KV
 // head they are the products row x query head of its G heads (head row r: row r / G).
-// A work-group takes RW tiles of 32 head rows, one to a wave, over one range of slots,
-// whose blocks a wave of its own streams from their pages into a ring in LDS.  Both
-// products run as 32 x 32 tiles (S^T = K Q^T, O^T = V^T P^T): K and V come from the
-// cache's blocks as A operands, 16 bytes a lane of K, 4 slots of one dim of V, and the
-// weights leave the score accumulators in the lanes that the value product wants them
-// in, so that nothing crosses lanes but a rare new maximum.  A tile of 32 columns
-// reads a block from LDS once for 32 rows, which is as fast as the matrix cores take
-// it; with 16 it was twice that.
+// A work-group takes RW tiles of 32 head rows, KW waves to a tile, over one range of
+// slots, in stages of 64: each wave requests its share of the next stage from the pages
+// straight into LDS and computes this one.  Both products run as 32 x 32 tiles
+// (S^T = K Q^T, O^T = V^T P^T): K and V come from the cache's blocks as A operands, 16
+// bytes a lane of K, 4 slots of one dim of V, and the weights leave the score
+// accumulators in the lanes that the value product wants them in, so that nothing
+// crosses lanes but a rare new reference.  A tile of 32 columns reads a block from LDS
+// once for 32 rows, which is as fast as the matrix cores take it; with 16 it was twice
+// that.
+//
+// Bounds.  Many rows: the matrix cores and the vector units, which the two waves of a
+// SIMD hardly use at the same time.  A step of 32 rows and 32 slots of 128 dims is 512
+// cycles of products, 256 of exponentials (16 a wave, 16 cycles each) and about 250 of
+// other vector work, and takes 1000; the matrix cores are 46 % busy.  Two prompts of
+// 8192 tokens, 16 / 8 heads of 128 in bf16: 530 to 560 us, 0.97 to 1.03 PFLOP/s (an 8192^3
+// product of the library 1.1 to 1.3); 70 us less where no stage is loaded, 75 less again
+// without exponentials, no change without barriers.  Few rows: the cache's bytes.  32
+// trees of 33 nodes over 8192 slots (1.08 GB) take 205 us, 5.2 TB/s, of 17 nodes 185, 5.8.
+// One tree of 17 over 4096 takes 13 to 15 us: two launches, the waits of a part and the
+// join.
+//
+// Tried and not kept: a wave of its own for the loads (972 us where the computing waves
+// took 575 then); rings of three and four stages, or of half stages (570 to 775 against
+// 545; trees 219 to 494 against 190 to 253); eight waves a work-group, as eight tiles or
+// as four by two (537, 601; trees 300 against 240); a stage's products a step behind
+// its scores, with and without a higher priority of the wave (552, 559 against 544).
 #include "pbd_launch.h"
 #include "pbd_rows.h"
 
@@ -26,9 +44,9 @@ __device__ __forceinline__ void raise(int* status, int bit) {
 }
 
 // A lane's sum of four weights up to which the reference that they are taken against may
-// stay below the scores: looking for the maximum of every step, and raising the
-// reference with it, is a tenth of the vector work of a step.  (bf16 and fp32 weights
-// have the same relative precision at any size.)
+// stay below the scores: looking for the maximum of every step is a tenth of its vector
+// work (two prompts of 8192 tokens 561 us with it, 548 without).  bf16 and fp32 weights
+// have the same relative precision at any size.
 constexpr float HIGH = 65536.f;
 
 constexpr int NB = 4, KEYS = NB * 16;                // 16-slot blocks of a stage, its slots
@@ -602,63 +620,66 @@ void k_rows_attn(RowsAttnArgs a) {
     if (w.place(block)) w.again(m, l, s_bad != 0);
 }
 
-// Joins the splits of head rows, one wave to a row: a lane has one split's maximum and
-// sum (and those 64 on), HD / 4 lanes the row's dims of every SETS-th split; the same
-// order whatever ran first.
+// Joins the splits of head rows, a wave to one or several: a lane has one split's maximum
+// and sum (and those 64 on), HD / 4 lanes the row's dims of every SETS-th split; the same
+// order whatever ran first.  4 us for one sequence's 34 rows of 33 splits, most of it the
+// waits for the rows' place, their maxima and their sums.
 template <typename T, int HD, int ROWS>
 __global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
     constexpr int LANES = HD / 4, SETS = 64 / LANES, UNROLL = 8;
     const int kvh = blockIdx.x % a.n_kv, group = blockIdx.x / a.n_kv, lane = threadIdx.x & 63;
     const Place at = find_group<ROWS>(a, group);
     if (!at.ok) return;
-    const int G = a.n_q / a.n_kv, hr = at.tile * ROWS + blockIdx.y * 4 + (int)(threadIdx.x >> 6);
-    if (hr >= min((at.tile + 1) * ROWS, at.n * G)) return;
-    const int tok = hr / G, row = at.row0 + tok, base = at.len - at.n;
-    const size_t head_row = (size_t)row * a.n_q + kvh * G + hr % G;
-    const int n = ((a.mask ? at.len : base + tok + 1) + a.kps - 1) / a.kps;
-    typedef float __attribute__((ext_vector_type(2))) ml2;
-    const ml2* ml = (const ml2*)a.part_ml + head_row * a.splits;
+    const int G = a.n_q / a.n_kv, base = at.len - at.n, end = min((at.tile + 1) * ROWS, at.n * G);
     const int d = lane % LANES * 4, set = lane / LANES;
-    const float* part = a.part_o + head_row * a.splits * HD + d;
-    f32x4 first[UNROLL];                             // the first splits' sums, requested with their scales
+    for (int hr = at.tile * ROWS + blockIdx.y * 4 + (int)(threadIdx.x >> 6); hr < end; hr += gridDim.y * 4) {
+        const int tok = hr / G, row = at.row0 + tok;
+        const size_t head_row = (size_t)row * a.n_q + kvh * G + hr % G;
+        const int n = ((a.mask ? at.len : base + tok + 1) + a.kps - 1) / a.kps;
+        typedef float __attribute__((ext_vector_type(2))) ml2;
+        const ml2* ml = (const ml2*)a.part_ml + head_row * a.splits;
+        const float* part = a.part_o + head_row * a.splits * HD + d;
+        f32x4 first[UNROLL];                         // the first splits' sums, requested with their scales
 #pragma unroll
-    for (int i = 0; i < UNROLL; ++i) first[i] = *(const f32x4*)(part + (size_t)min(set + i * SETS, n - 1) * HD);
-    const ml2 mine = ml[min(lane, n - 1)];
-    float M = lane < n ? mine[0] : -INFINITY;
-    bool bad = lane < n && mine[0] != mine[0];
-    for (int s = lane + 64; s < n; s += 64) {
-        const ml2 x = ml[s];
-        bad |= x[0] != x[0];
-        M = fmaxf(M, x[0]);
+        for (int i = 0; i < UNROLL; ++i)
+            if (i * SETS < n) first[i] = *(const f32x4*)(part + (size_t)min(set + i * SETS, n - 1) * HD);
+        const ml2 mine = ml[min(lane, n - 1)];
+        float M = lane < n ? mine[0] : -INFINITY;
+        bool bad = lane < n && mine[0] != mine[0];
+        for (int s = lane + 64; s < n; s += 64) {
+            const ml2 x = ml[s];
+            bad |= x[0] != x[0];
+            M = fmaxf(M, x[0]);
+        }
+        if (__any(bad)) return;                      // (every row of the sequence says so)
+        M = wave_max_dpp(M);
+        auto scale = [&](ml2 x) { return x[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x[0] - M); };
+        float L = lane < n ? mine[1] * scale(mine) : 0.f;
+        for (int s = lane + 64; s < n; s += 64) {
+            const ml2 x = ml[s];
+            L += x[1] * scale(x);
+        }
+        L = wave_sum_dpp(L);
+        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        const float f0 = scale(mine);
+#pragma unroll
+        for (int i = 0; i < UNROLL; ++i) {
+            const int s = set + i * SETS;
+            const float f = __shfl(f0, min(s, 63), 64);
+            if (s < n) acc += first[i] * f;
+        }
+        for (int s = set + UNROLL * SETS; s < n; s += SETS) acc += *(const f32x4*)(part + (size_t)s * HD) * scale(ml[s]);
+#pragma unroll
+        for (int w = LANES; w < 64; w *= 2)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], w, 64);
+        if (set != 0) continue;
+        const bool none = a.mask && base == 0 && (a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull)) == 0;
+        const float inv = none ? 0.f : 1.f / L;
+        const float x[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+        put_out<T, HD>(a, head_row, d, x);
+        if (a.lse && d == 0) a.lse[head_row] = log_sum(M, L, none);
     }
-    if (__any(bad)) return;
-    M = wave_max_dpp(M);
-    auto scale = [&](ml2 x) { return x[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x[0] - M); };
-    float L = lane < n ? mine[1] * scale(mine) : 0.f;
-    for (int s = lane + 64; s < n; s += 64) {
-        const ml2 x = ml[s];
-        L += x[1] * scale(x);
-    }
-    L = wave_sum_dpp(L);
-    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-    const float f0 = scale(mine);
-#pragma unroll
-    for (int i = 0; i < UNROLL; ++i) {
-        const int s = set + i * SETS;
-        const float f = __shfl(f0, min(s, 63), 64);
-        if (s < n) acc += first[i] * f;
-    }
-    for (int s = set + UNROLL * SETS; s < n; s += SETS) acc += *(const f32x4*)(part + (size_t)s * HD) * scale(ml[s]);
-#pragma unroll
-    for (int w = LANES; w < 64; w *= 2)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], w, 64);
-    if (set != 0) return;
-    const bool none = a.mask && base == 0 && (a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull)) == 0;
-    const float inv = none ? 0.f : 1.f / L;
-    const float x[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
-    put_out<T, HD>(a, head_row, d, x);
-    if (a.lse && d == 0) a.lse[head_row] = log_sum(M, L, none);
 }
 
 }  // namespace
@@ -717,6 +738,8 @@ RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batc
 }
 
 namespace {
+constexpr int JOIN_ROWS = 4096;
+
 template <typename T, int HD, int RW, int KW>
 hipError_t launch(const RowsAttnArgs& a, const RowsAttnPlan& p, hipStream_t st) {
     constexpr size_t ring = (size_t)RING * NB * 2 * 16 * HD * sizeof(T);
@@ -724,7 +747,9 @@ hipError_t launch(const RowsAttnArgs& a, const RowsAttnPlan& p, hipStream_t st) 
     PBD_LAUNCH((k_rows_attn<T, HD, RW, KW>), dim3((unsigned)(p.groups * a.n_kv), p.splits), dim3(RW * KW * 64), ring, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.direct) return e;
-    PBD_LAUNCH((k_rows_join<T, HD, RW * 32>), dim3((unsigned)(p.groups * a.n_kv), RW * 8), dim3(256), 0, st, a);
+    // a row a wave while the waves run at once, else four
+    const int parts = (long long)a.rows * a.n_q > JOIN_ROWS ? RW * 2 : RW * 8;
+    PBD_LAUNCH((k_rows_join<T, HD, RW * 32>), dim3((unsigned)(p.groups * a.n_kv), parts), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
