@@ -71,12 +71,12 @@ int log2_of(int x) {
 }
 
 // Sizes of an attention of packed rows, and its layout.
-int rows_plan(const pbd_pages* pages, int batch, int rows, int max_len, RowsAttnPlan& plan) {
+int rows_plan(const pbd_pages* pages, int batch, int rows, int max_len, bool tree, RowsAttnPlan& plan) {
     const int rc = pages_ok(pages, batch, max_len);
     if (rc) return rc;
     if (max_len < 1) return op_fail(PBD_ERR_INVALID_ARG, "max_len must be >= 1");
     if (rows < 1 || rows > ROWS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "rows outside [1, 2^22]");
-    plan = rows_attn_plan(pages->dtype, pages->n_q_heads, pages->n_kv_heads, pages->head_dim, batch, rows, max_len);
+    plan = rows_attn_plan(pages->dtype, pages->n_q_heads, pages->n_kv_heads, pages->head_dim, batch, rows, max_len, tree);
     if (plan.groups * pages->n_kv_heads > GROUPS_MAX / 2) return op_fail(PBD_ERR_CAPACITY, "rows times heads is too much for one call");
     return PBD_OK;
 }
@@ -85,7 +85,7 @@ int rows_attention(const pbd_pages* pages, int batch, int rows, const void* q, i
                    const int32_t* lens, const uint64_t* mask, int max_len, float scale, void* out, float* lse, void* ws,
                    size_t ws_bytes, pbd_stream_t stream) {
     RowsAttnPlan plan;
-    const int rc = rows_plan(pages, batch, rows, max_len, plan);
+    const int rc = rows_plan(pages, batch, rows, max_len, mask != nullptr, plan);
     if (rc) return rc;
     if (!q || !row_start || !lens || !out || !ws) return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
     const int esz = pages->dtype == PBD_DTYPE_BF16 ? 2 : 4;
@@ -345,7 +345,7 @@ int pbd_paged_append_rows(const pbd_pages* pages, int32_t rows, const float* q, 
 
 size_t pbd_packed_attention_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t rows, int32_t max_len) {
     RowsAttnPlan plan;
-    return rows_plan(pages, batch, rows, max_len, plan) ? 0 : plan.bytes;
+    return rows_plan(pages, batch, rows, max_len, false, plan) ? 0 : plan.bytes;
 }
 
 int pbd_packed_attention(const pbd_pages* pages, int32_t batch, int32_t rows, const void* q, int64_t q_stride,
@@ -369,7 +369,8 @@ int pbd_tree_layout(int32_t batch, int32_t rows, const int32_t* row_start, const
 }
 
 size_t pbd_tree_attention_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t rows, int32_t max_len) {
-    return pbd_packed_attention_workspace_bytes(pages, batch, rows, max_len);
+    RowsAttnPlan plan;
+    return rows_plan(pages, batch, rows, max_len, true, plan) ? 0 : plan.bytes;
 }
 
 int pbd_tree_attention(const pbd_pages* pages, int32_t batch, int32_t rows, const void* q, int64_t q_stride,

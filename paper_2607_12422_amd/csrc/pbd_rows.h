@@ -91,7 +91,7 @@ struct RowsAttnPlan {
     int kps, splits;            // slots per split
     size_t off_ml, bytes;
 };
-RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int rows, int max_len);
+RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int rows, int max_len, bool tree);
 
 struct RowsAttnArgs {
     PageView pg;

@@ -699,7 +699,12 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
 // Where a bf16 sequence has at most 64 rows, four tiles leave two waves that only load:
 // 64 trees of 17 nodes over 1000 slots take 48 us so and 63 on two tiles, 48 of 32 over
 // 2000 70 and 101; few trees the same on both.
-RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int rows, int max_len) {
+//
+// The lengths are not known here.  Trees are taken to fill 0.7 of the slots where there
+// are several: 12 ragged ones with eight heads a KV head take 56 us with the parts
+// of that, 59 with those for full ones, 24 of 256 to 8000 slots 91 and 112, 20 of 300 to
+// 3000 40 and 45; but 16 of 64 nodes over 2000 slots each 59 and 46.
+RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int rows, int max_len, bool tree) {
     RowsAttnPlan p{};
     const bool half = dtype == PBD_DTYPE_BF16;
     const long long G = n_q / n_kv, head_rows = (long long)rows * G, each = (head_rows + batch - 1) / batch;
@@ -708,18 +713,19 @@ RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batc
     // of the slots, the share that an average row sees
     const double seen = 1.0 - 0.5 * std::min(1.0, (double)rows / batch / max_len);
     const int most = std::min(64, (max_len + KEYS - 1) / KEYS);
+    const double full = tree && batch > 1 ? 0.7 : 1.0;
     double best = 0;
     for (int tiles = half && each <= 64 ? 4 : 2; tiles <= 4; tiles += 2) {
         const long long live = batch * ((each + tiles * 32 - 1) / (tiles * 32)) * n_kv;  // work-groups with rows, about
         const double stage = (half ? 1.0 : 4.0) * (tiles == 4 ? 1.5 : 1.0) * head_dim / 128;
         for (int s = 1; s <= most; ++s) {
-            if (s > 1 && live * s > 512) break;
-            const bool alone = live * s <= 256;                                   // one work-group a CU
+            if (s > 1 && live * s * full > 512) break;
+            const bool alone = live * s * full <= 256;                            // one work-group a CU
             const int kps = ((max_len + s - 1) / s + KEYS - 1) / KEYS * KEYS;
             if ((max_len + kps - 1) / kps != s) continue;                         // (fewer parts do the same)
             const double rate = each <= 64 ? (alone ? 4.8e6 : 5.6e6) : tiles == 4 ? 4.2e6 : 5.0e6;
             const double one = (kps / KEYS) * stage * (alone ? 1.0 : 1.1);
-            const double est = std::max({one, one * seen * live * s / 512.0, bytes / rate}) + (s > 1 ? 4 + s * partial / 4e6 : 0);
+            const double est = std::max({one, one * seen * full * live * s / 512.0, full * bytes / rate}) + (s > 1 ? 4 + s * partial / 4e6 : 0);
             if (best > 0 && est >= best) continue;
             best = est;
             p.tiles = tiles;
