@@ -49,6 +49,12 @@ __device__ __forceinline__ void raise(int* status, int bit) {
 // have the same relative precision at any size.
 constexpr float HIGH = 65536.f;
 
+// Maxima (log2 units, either sign) past which a step of the scores' type is 64 or more:
+// nothing but equals of the maximum has a weight.  Up to there the fused product keeps
+// in the exponent what the rounding of the reference left out, 64 at most; past it, a
+// power of two for the scale makes the reference exact, and equal scores weigh 1.
+constexpr float FAR = 2147483648.f;
+
 constexpr int NB = 4, KEYS = NB * 16;                // 16-slot blocks of a stage, its slots
 constexpr int RING = 2;                              // stages in LDS
 
@@ -80,6 +86,12 @@ __device__ __forceinline__ float half_max(float v) {
 __device__ __forceinline__ float half_sum(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A product that no sum takes in.
+__device__ __forceinline__ float apart(float v) {
+    asm("" : "+v"(v));
+    return v;
 }
 
 // Where a group of head rows lies: its sequence, by a search of the wave over the
@@ -465,7 +477,8 @@ struct RowsWork {
                     float top = -INFINITY;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[i]);
-                    top = fmaxf(m, half_max(top * scale));
+                    const float raw = half_max(top), high = apart(raw * a.scale_log2), before = m;
+                    top = fmaxf(m, high);
                     const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) part[i] *= f;
@@ -474,7 +487,17 @@ struct RowsWork {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) o[t][i] *= f;
                     m = top;
-                    ref = top == -INFINITY ? 0.f : top;
+                    if (__builtin_expect(__any(fabsf(top) > FAR && top > -INFINITY), false)) {
+                        const float two = __uint_as_float(__float_as_uint(a.scale_log2) & 0x7f800000u);
+                        const bool far = fabsf(top) > FAR && top > -INFINITY;
+                        if (!far || high >= before) {
+                            scale = far ? two : a.scale_log2;
+                            ref = far ? raw * two : top == -INFINITY ? 0.f : top;
+                        }
+                    } else {
+                        ref = top == -INFINITY ? 0.f : top;
+                        scale = a.scale_log2;
+                    }
                     first_step = __any(m == -INFINITY);
                     weights();
                 }
@@ -580,12 +603,14 @@ struct RowsWork {
                     settle<T>();
                     const unsigned seen = seen_of(k0);
                     hide(sc, seen);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sc[i] = apart(sc[i] * a.scale_log2);     // (rounded as the maximum)
 #pragma unroll 1
                     for (int u = 0; u < 2; ++u) {
                         T p[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            p[i] = from_f32<T>(__builtin_amdgcn_exp2f(__builtin_fmaf(u ? sc[8 + i] : sc[i], a.scale_log2, -ref)));
+                            p[i] = from_f32<T>(__builtin_amdgcn_exp2f((u ? sc[8 + i] : sc[i]) - ref));
                         vraw x[2];
                         v_frag(st, u, t, x);
                         v_cut(u, at.len - k0, x);

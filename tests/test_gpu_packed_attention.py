@@ -266,6 +266,99 @@ def test_infinite_keys():
         assert torch.all(((out - o[:, 0]).abs() <= tol[:, 0])[~up])
 
 
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 128)])
+@pytest.mark.parametrize("step", [1.0, -1.0, 0.25, 3.0])
+def test_rising_and_falling_scores(dtype, D, step):
+    """Scores that grow or fall all along the slots: slowly, so that weights grow to many times the first ones' before the
+    reference follows, and fast."""
+    cache = ref.Cache([200, 180, 1500], 1, D, dtype, seed=2)
+    for b, m in enumerate(cache.lens):
+        cache.dk[b, 0, :m] = 0.0
+        cache.dk[b, 0, :m, 0] = (torch.arange(m) % 200).to(dtype)
+        cache.put(b, 0, cache.dk[b, :, :m], cache.dv[b, :, :m])
+    c = Call(cache, [200, 30, 3], 2)
+    c.q = torch.zeros_like(c.q)
+    c.q[..., 0] = step
+    c.dq.copy_(c.q.to(DEV))
+    for scale in (0.2, 0.7):
+        c.out.fill_(77.0)
+        c.lse.fill_(77.0)
+        c.run(scale=scale)
+        c.check(scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("odd", [False, True])
+def test_scores_of_any_size(dtype, odd):
+    """Scores of 1e30 in either sign, the largest ones last, first, or followed by scores of 0: the highest slots share all,
+    also where the last slot's NaN, hidden from the rows before, sends the tile through a second pass.
+
+    Weights of 1 and 0 are exact in either type: n roundings of the sum and two of the quotient, below U sum |v| / count each,
+    and the output's own."""
+    D, n = 64, 150
+    cache = ref.Cache([n] * 6, 1, D, dtype, seed=6)
+    ramp = torch.arange(n) % 128
+    for b, k in enumerate((1.0 + ramp, 1.0 - ramp, -400.0 + ramp, 400.0 - ramp, -1.0 * (ramp < 40), 1.0 * (ramp < 40))):
+        cache.dk[b, 0, :n] = 0.0
+        cache.dk[b, 0, :n, 0] = k.to(dtype)
+        if odd:
+            cache.dv[b, 0, n - 1] = math.nan
+        cache.put(b, 0, cache.dk[b, :, :n], cache.dv[b, :, :n])
+    c = Call(cache, [n] * 6, 1)
+    c.q = torch.zeros_like(c.q)
+    c.q[..., 0] = 2.0 ** 92
+    c.dq.copy_(c.q.to(DEV))
+    c.run()
+    out = c.out.double().cpu()
+    for b in range(6):
+        k, v = cache.dk[b, 0, :n, 0].double(), cache.dv[b, 0].double()
+        for i in range(n):
+            if odd and i == n - 1:
+                assert torch.isnan(out[b * n + i, 0]).all()
+                continue
+            top = (k[: i + 1] == k[: i + 1].max()).nonzero()[:, 0]
+            want = v[top].mean(0)
+            tol = want.abs() * torch.finfo(dtype).eps / 2 * 1.01 + (n + 2) * ref.U * v[top].abs().mean(0)
+            assert torch.all((out[b * n + i, 0] - want).abs() <= tol), (b, i)
+
+
+def test_queries_that_are_not_finite_stay_in_their_rows():
+    """The others keep the bound.  (Those of the same 32 may differ in their last bits: their weights are rounded against the
+    whole row's maximum where the tile is gone over again, and against an earlier one where not.)"""
+    for dtype in (BF, F32):
+        c = Call(ref.Cache([200, 40], 2, 64, dtype, seed=7), [60, 40], 2)
+        q = c.q.clone()
+        bad = [(3, 1), (59, 0), (70, 3)]
+        for r, h in bad:
+            q[r, h, 5] = math.nan
+        c.dq.copy_(q.to(DEV))
+        c.run()
+        out, lse = c.out.clone(), c.lse.clone()
+        c.dq.copy_(c.q.to(DEV))
+        c.run()
+        for r, h in bad:
+            assert torch.isnan(out[r, h]).all() and torch.isnan(lse[r, h])
+            out[r, h], lse[r, h] = c.out[r, h], c.lse[r, h]
+        c.check()
+        c.out.copy_(out)
+        c.lse.copy_(lse)
+        c.check()
+
+
+def test_two_streams_at_once():
+    g = torch.Generator().manual_seed(3)
+    a = Call(ref.Cache([3000, 40], 2, 128, BF, seed=1), [33, 40], 2)
+    b = Call(ref.Cache([900, 64], 2, 128, BF, seed=2), [17, 64], 2, trees=[rr.random_tree(17, g), rr.random_tree(64, g)])
+    torch.cuda.synchronize()
+    side = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        a.enqueue(stream=side[0])
+        b.enqueue(stream=side[1])
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+
+
 def test_scale_and_stream():
     c = Call(ref.Cache([100, 40], 2, 128, BF), [30, 40], 2)
     side = torch.cuda.Stream()
