@@ -545,6 +545,9 @@ int pbd_decode_paged(pbd_ctx* ctx, const pbd_pages* pages, int32_t batch, int32_
  * PBD_STATUS_PAGE and nobody who needs a page is served.
  * page_size: as in pbd_pages; n_pages * page_size below 2^31; max_rows in [0, 2^22].
  * row_start, new_lens and the other outputs overlap no input but the three in place.
+ * The append skips the rows of a sequence that was not served; an attention over its
+ * new_lens would take its last cached slots for them, so a program looks at status
+ * or new_lens before it uses their outputs.
  * A table, its stack and counts belong to one call at a time.
  */
 int pbd_page_plan(int32_t batch, int32_t page_size, int32_t n_pages, int32_t* table, int32_t table_width,
@@ -598,6 +601,7 @@ int pbd_paged_append_rows(const pbd_pages* pages, int32_t rows, const float* q, 
  * elements of slots that it sees count as in fp32 arithmetic.  Rows behind the last
  * sequence stay as they were.  Results are bitwise the same from run to run; they depend
  * on a sequence's own data and on batch, rows and max_len.
+ * out and lse overlap no input.
  * max_len: host bound on lens, in [1, table_width * page_size].  PBD_STATUS_CAPACITY:
  * lens[b] outside [0, max_len] or less than n, row_start out of [0, rows] or
  * descending (then others may be skipped with it).  PBD_STATUS_PAGE: a bad page among
@@ -643,8 +647,9 @@ int pbd_tree_attention(const pbd_pages* pages, int32_t batch, int32_t rows, cons
  * - n + k + 1; what lies behind is given up.  A sequence without rows is left as it is.
  * n above width or 64, or lens[b] < n: PBD_STATUS_CAPACITY; PBD_STATUS_TREE as
  * pbd_tree_layout; PBD_STATUS_PAGE for the nodes' pages: the sequence is skipped.
- * Outputs overlap no input (new_lens is not lens); the nodes' pages belong to one sequence.  A cache that keeps score or slot_pos
- * is refused (PBD_ERR_UNSUPPORTED).  n_layers >= 1, n_layers * n_kv_heads < 2^24; width in [1, 2^20].
+ * Outputs overlap no input (new_lens is not lens) and not each other; the nodes' pages
+ * belong to one sequence.  A cache that keeps score or slot_pos is refused
+ * (PBD_ERR_UNSUPPORTED).  n_layers >= 1, n_layers * n_kv_heads < 2^24; width in [1, 2^20].
  */
 int pbd_tree_commit(const pbd_pages* pages, int32_t n_layers, int32_t batch, int32_t rows, const int32_t* row_start,
                     const int32_t* lens, const int32_t* parent, const int32_t* tokens, const int32_t* verify,

@@ -93,6 +93,7 @@ int rows_attention(const pbd_pages* pages, int batch, int rows, const void* q, i
         return op_fail(PBD_ERR_INVALID_ARG, "q_stride must hold a row and be a multiple of 16 bytes");
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 16))
         return op_fail(PBD_ERR_INVALID_ARG, "q, out and ws must be 16-byte aligned");
+    if (out == q || (const void*)lse == q) return op_fail(PBD_ERR_INVALID_ARG, "out and lse must not be q");
     if (!(scale > 0.f) || isinf(scale)) return op_fail(PBD_ERR_INVALID_ARG, "scale must be positive and finite");
     if (ws_bytes < plan.bytes) return op_fail(PBD_ERR_CAPACITY, "workspace smaller than the call's workspace_bytes");
     RowsAttnArgs a{};

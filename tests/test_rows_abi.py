@@ -44,11 +44,11 @@ def append(lib, pg, rows=3, q=P, k=P, v=P, stride=512, slots=P, pos=P, qn=P, kn=
     return lib.pbd_paged_append_rows(ref(pg), rows, q, k, v, stride, slots, pos, qn, kn, eps, rope, rope_len, q_out, None)
 
 
-def packed(lib, pg, batch=2, rows=5, q=P, stride=256, start=P, lens=P, max_len=128, scale=0.1, out=P, lse=None, ws=P, n=1 << 40):
+def packed(lib, pg, batch=2, rows=5, q=P, stride=256, start=P, lens=P, max_len=128, scale=0.1, out=P + (1 << 20), lse=None, ws=P, n=1 << 40):
     return lib.pbd_packed_attention(ref(pg), batch, rows, q, stride, start, lens, max_len, scale, out, lse, ws, n, None)
 
 
-def tree(lib, pg, batch=2, rows=5, q=P, stride=256, start=P, lens=P, mask=P, max_len=128, scale=0.1, out=P, lse=None, ws=P,
+def tree(lib, pg, batch=2, rows=5, q=P, stride=256, start=P, lens=P, mask=P, max_len=128, scale=0.1, out=P + (1 << 20), lse=None, ws=P,
          n=1 << 40):
     return lib.pbd_tree_attention(ref(pg), batch, rows, q, stride, start, lens, mask, max_len, scale, out, lse, ws, n, None)
 
@@ -113,7 +113,7 @@ def test_attention(lib, call):
                      (dict(q=P + 4), INV), (dict(out=P + 8), INV), (dict(ws=P + 8), INV), (dict(stride=248), INV),
                      (dict(stride=260), INV), (dict(max_len=0), INV), (dict(max_len=129), CAP), (dict(scale=0.0), INV),
                      (dict(scale=float("nan")), INV), (dict(scale=float("inf")), INV), (dict(n=100), CAP), (dict(rows=0), INV),
-                     (dict(rows=(1 << 22) + 1), INV)]:
+                     (dict(rows=(1 << 22) + 1), INV), (dict(out=P), INV), (dict(lse=P), INV)]:
         assert call(lib, plain(), **kw) == code, kw
     assert call(lib, plain(n_q_heads=256, n_kv_heads=256), stride=1 << 14, rows=1 << 22) == CAP
     size = b.pbd_packed_attention_workspace_bytes if call is packed else b.pbd_tree_attention_workspace_bytes
