@@ -102,6 +102,7 @@ int rows_attention(const pbd_pages* pages, int batch, int rows, const void* q, i
     a.q = q; a.q_stride = q_stride; a.row_start = row_start; a.lens = lens; a.mask = (const unsigned long long*)mask;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.kps = plan.kps; a.splits = plan.splits; a.direct = plan.splits == 1; a.once = plan.once;
+    a.longest = plan.longest;
     a.part_o = (float*)ws;
     a.part_ml = (float*)((char*)ws + plan.off_ml);
     a.out = out; a.lse = lse;

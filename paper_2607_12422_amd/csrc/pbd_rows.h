@@ -88,6 +88,7 @@ struct RowsAttnPlan {
     int tiles;                  // tiles of 32 head rows a work-group takes
     long long groups;           // groups of that many head rows that the packed rows may need
     bool once;                  // most sequences' K and V go to one work-group a KV head
+    bool longest;               // the groups that see the most slots first
     int kps, splits;            // slots per split
     size_t off_ml, bytes;
 };
@@ -105,6 +106,7 @@ struct RowsAttnArgs {
     int kps, splits;
     bool direct;                // one split: it writes the output
     bool once;                  // K and V past the caches
+    bool longest;               // the groups that see the most slots first
     float* part_o;              // [rows][n_q][splits][head_dim]
     float* part_ml;             // [rows][n_q][splits][2]: maximum (NaN: bad page), sum
     void* out;                  // [rows][n_q][head_dim]

@@ -127,6 +127,48 @@ __device__ __forceinline__ Place find_group(const RowsAttnArgs& a, int group) {
     return p;
 }
 
+// The group of rank `rank` among all of them, those that see the most slots first: by
+// base G / ROWS + the group's number, a measure of its last row, and of equal ones the
+// lower sequence.  The measure with as many groups at or above it is searched for, each
+// lane counting for its sequence.
+template <int ROWS>
+__device__ __forceinline__ Place find_longest(const RowsAttnArgs& a, int rank) {
+    constexpr int MOST = 1 << 23;                    // (counts and measures are exact in fp32)
+    const int lane = threadIdx.x & 63, G = a.n_q / a.n_kv;
+    int from = 0, cnt = 0;
+    if (lane < a.batch) {
+        const int r0 = a.row_start[lane], r1 = a.row_start[lane + 1], len = a.lens[lane], n = r1 - r0;
+        if (r0 >= 0 && r1 >= r0 && r1 <= a.rows && len >= n && len <= a.max_len) {
+            from = (int)min((long long)(len - n) * G / ROWS, (long long)MOST);
+            cnt = (int)(((long long)n * G + ROWS - 1) / ROWS);
+        }
+    }
+    auto at_least = [&](int x) {
+        return __builtin_amdgcn_readfirstlane((int)wave_sum_dpp((float)max(0, cnt - max(0, x - from - 1))));
+    };
+    Place p{};
+    if (rank >= at_least(1)) return p;
+    int lo = 1, hi = __builtin_amdgcn_readfirstlane((int)wave_max_dpp((float)(from + cnt))) + 1, above = 0;
+    while (hi - lo > 1) {                            // at_least(lo) > rank >= at_least(hi) = above
+        const int mid = (lo + hi) >> 1, c = at_least(mid);
+        if (c > rank) lo = mid;
+        else {
+            hi = mid;
+            above = c;
+        }
+    }
+    const bool has = from < lo && lo <= from + cnt;
+    const unsigned long long all = __ballot(has), one = __ballot(has && __popcll(all & ((1ull << lane) - 1)) == rank - above);
+    if (!one) return p;
+    p.b = __builtin_ctzll(one);
+    p.tile = lo - 1 - __builtin_amdgcn_readlane(from, p.b);
+    p.row0 = __builtin_amdgcn_readfirstlane(a.row_start[p.b]);
+    p.n = __builtin_amdgcn_readfirstlane(a.row_start[p.b + 1]) - p.row0;
+    p.len = __builtin_amdgcn_readfirstlane(a.lens[p.b]);
+    p.ok = true;
+    return p;
+}
+
 // Reports sequences whose rows or length are out of range (the first work-group).
 __device__ __forceinline__ void report_bad(const RowsAttnArgs& a) {
     bool bad = false;
@@ -274,7 +316,8 @@ struct RowsWork {
         split = blockIdx.y;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         lane = threadIdx.x & 63;
-        at = find_group<ROWS>(a, (int)(gridDim.x / a.n_kv) - 1 - block / a.n_kv);        // a sequence's last rows first
+        at = a.longest ? find_longest<ROWS>(a, block / a.n_kv)
+                       : find_group<ROWS>(a, (int)(gridDim.x / a.n_kv) - 1 - block / a.n_kv);      // a sequence's last rows first
         if (!at.ok) return false;
         const int G = a.n_q / a.n_kv;
         base = at.len - at.n;
@@ -729,6 +772,14 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
 // are several: 12 ragged ones with eight heads a KV head take 56 us with the parts
 // of that, 59 with those for full ones, 24 of 256 to 8000 slots 91 and 112, 20 of 300 to
 // 3000 40 and 45; but 16 of 64 nodes over 2000 slots each 59 and 46.
+//
+// Which groups go first.  512 work-groups run at once; where there are a few times as
+// many, the last ones decide, and the longest go first.  Finding a work-group's place
+// among all sequences takes it about 1 us: 6 prompts and chunks of up to 6400 slots 222 us
+// so and 257 sequence by sequence, 8 prompts of 1000 to 2048 107 and 119, 64 chunks
+// of 64 to 512 behind up to 3000 316 and 336, two prompts of 8192 539 and 547; but 60
+// prompts of 10 to 300 44 and 40, and with more work-groups 40 of 100 to 2048 358 and
+// 350, 8 of 8192 2227 and 2176, whose K and V in turn leave the L2s.
 RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batch, int rows, int max_len, bool tree) {
     RowsAttnPlan p{};
     const bool half = dtype == PBD_DTYPE_BF16;
@@ -761,6 +812,8 @@ RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batc
     const int R = p.tiles * 32;
     p.groups = head_rows / R + batch;
     p.once = each <= R;
+    p.longest = !tree && p.splits == 1 && batch > 1 && batch <= 64 && p.groups * n_kv > 512 && p.groups * n_kv <= 4096 &&
+                max_len * seen >= 1024;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     const size_t n = p.splits == 1 ? 0 : (size_t)rows * n_q * p.splits;
     p.off_ml = up(n * head_dim * 4);

@@ -418,6 +418,36 @@ def test_offsets_past_32_bits(trees):
     c.check()
 
 
+@pytest.mark.parametrize("dtype,H,G,D", [(BF, 8, 2, 64), (BF, 4, 8, 128), (BF, 12, 3, 64), (F32, 12, 5, 64)])
+@pytest.mark.parametrize("B", [2, 17, 64])
+def test_many_groups_of_ragged_sequences(dtype, H, G, D, B):
+    """513 to 4096 work-groups over sequences of 1024 slots and more, which are taken by length: every row comes once,
+    whatever the others are, none at all or out of range among them."""
+    g = torch.Generator().manual_seed(B + H)
+    draw = lambda hi: int(torch.randint(0, hi + 1, (1,), generator=g))
+    R = 90000 // (G * H)
+    counts = [draw(2 * R // B) if b % 7 != 3 else 0 for b in range(B)] if B > 2 else [R // 2, R // 2 - 50]
+    lens = [n + (700 + draw(900) if b % 3 else 0) for b, n in enumerate(counts)]
+    c = Call(ref.Cache(lens, H, D, dtype, page=64, seed=B), counts, G)
+    assert (c.R * G // 128 + B) * H > 512 and (c.R * G // 64 + B) * H <= 4096
+    assert c.max_len - c.R / B / 2 >= 1024
+    c.run()
+    c.check()
+    assert int(c.status) == 0
+    bad = [b for b, n in enumerate(counts) if n and b % 5 == 1]
+    c.lens = torch.tensor([[-1, n - 1, 10 ** 6][b % 3] if b in bad else m for b, (m, n) in enumerate(zip(lens, counts))],
+                          dtype=torch.int32, device=DEV)
+    want = c.out.clone(), c.lse.clone()
+    c.out.fill_(77.0)
+    c.lse.fill_(77.0)
+    c.run()
+    assert int(c.status) == pbd.PBD_STATUS_CAPACITY
+    for b, n in enumerate(counts):
+        rows = slice(c.starts[b], c.starts[b] + n)
+        for got, was in zip((c.out, c.lse), want):
+            assert torch.all(got[rows] == 77.0) if b in bad else torch.equal(got[rows], was[rows])
+
+
 @pytest.mark.parametrize("long", [False, True])
 def test_lengths_and_rows_out_of_range_skip_the_sequence(long):
     m = 3000 if long else 100
