@@ -17,7 +17,7 @@
 // SIMD hardly use at the same time.  A step of 32 rows and 32 slots of 128 dims is 512
 // cycles of products, 256 of exponentials (16 a wave, 16 cycles each) and about 250 of
 // other vector work, and takes 1000; the matrix cores are 46 % busy.  Two prompts of
-// 8192 tokens, 16 / 8 heads of 128 in bf16: 530 to 560 us, 0.97 to 1.03 PFLOP/s (an 8192^3
+// 8192 tokens, 16 / 8 heads of 128 in bf16: 521 to 570 us, 0.95 to 1.04 PFLOP/s (an 8192^3
 // product of the library 1.1 to 1.3); 70 us less where no stage is loaded, 75 less again
 // without exponentials, no change without barriers.  Few rows: the cache's bytes.  32
 // trees of 33 nodes over 8192 slots (1.08 GB) take 205 us, 5.2 TB/s, of 17 nodes 185, 5.8.
