@@ -760,7 +760,7 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
 // to 5.6 TB/s; a part costs its partial sums, written and read, and a join.  Times (16 /
 // 8 heads of 128, bf16; two and four tiles): one prompt of 2048 tokens 37 and 50 us, of
 // 4096 94 and 100, two of 8192 630 and 545, six mixed ones of four heads a KV head 277 and
-// 255; (parts taken, and others) a prompt of 1024 21 (1) and 29 (2), 64 rows over 16384
+// 255, sequence by sequence; (parts taken, and others) a prompt of 1024 21 (1) and 29 (2), 64 rows over 16384
 // slots 31 (32) and 34 (16), 512 over 8192 59 (4) and 84 (2), 16 trees of 64 nodes over
 // 2000 46 (1) and 60 (2), one tree of 17 over 4096 13 (32) and 14.2 (16).
 //
