@@ -107,7 +107,7 @@ struct RowsAttnArgs {
     bool direct;                // one split: it writes the output
     bool once;                  // K and V past the caches
     bool longest;               // the groups that see the most slots first
-    float* part_o;              // [rows][n_q][splits][head_dim]
+    float* part_o;              // [rows][n_q][splits][head_dim]: weighted means of the splits' values
     float* part_ml;             // [rows][n_q][splits][2]: maximum (NaN: bad page), sum
     void* out;                  // [rows][n_q][head_dim]
     float* lse;

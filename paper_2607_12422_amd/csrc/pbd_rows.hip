@@ -431,22 +431,22 @@ struct RowsWork {
         keep_first(v[1], cut - 16 * u - 8 - 4 * h);
     }
 
-    // 32 dims of the lane's head row from 32 t on: the output's, or the split's sums.
+    // 32 dims of the lane's head row from 32 t on: the output's, or what the split's slots make of them.
     __device__ __forceinline__ void put(int t, const f32x16& v, float inv, bool bad) const {
         if (kw > 0 || !live || (a.direct && bad)) return;
         const size_t part_row = head_row * a.splits + split;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int d = 32 * t + 8 * j + 4 * h;
-            if (a.direct) {
-                const float x[4] = {v[4 * j] * inv, v[4 * j + 1] * inv, v[4 * j + 2] * inv, v[4 * j + 3] * inv};
-                put_out<T, HD>(a, head_row, d, x);
-            } else {
-                *(f32x4*)(a.part_o + part_row * HD + d) = f32x4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
-            }
+            const float x[4] = {v[4 * j] * inv, v[4 * j + 1] * inv, v[4 * j + 2] * inv, v[4 * j + 3] * inv};
+            if (a.direct) put_out<T, HD>(a, head_row, d, x);
+            else *(f32x4*)(a.part_o + part_row * HD + d) = f32x4{x[0], x[1], x[2], x[3]};
         }
     }
     __device__ __forceinline__ bool none() const { return a.mask && base == 0 && bits == 0; }    // the row sees no slot
+    // What the weighted sums are multiplied by.  A split whose every score is -inf counts for
+    // nothing; a row whose every score is, is NaN.
+    __device__ __forceinline__ float share(float l) const { return none() || (!a.direct && l == 0.f) ? 0.f : 1.f / l; }
 
     // The pass over the slots: outputs, or true where a NaN asks for the careful one.  m, l:
     // the row's maximum and sum (waves of kw 0).
@@ -615,53 +615,76 @@ struct RowsWork {
             }
         }
         if (__builtin_expect(redo, false)) return true;
-        const float inv = none() ? 0.f : 1.f / l;
+        const float inv = share(l);
 #pragma unroll
         for (int t = 0; t < NT; ++t) put(t, o[t], inv, bad);
         return false;
     }
 
-    // The careful pass, under the maximum and the sum that the first one found.
-    __device__ __forceinline__ void again(float m, float l, bool bad) {
-        const float ref = m == -INFINITY ? 0.f : m, inv = none() ? 0.f : 1.f / l;
+    // One pass over the slots for the careful one: of(stage, first slot, what the row sees, scores) for
+    // each 32 of them, in the waves of kw 0.
+    template <typename F> __device__ __forceinline__ void sweep(F&& of) {
+        start();
+        for (int it = 0; it < n_st; ++it) {
+            const unsigned char* stage = open(it);
+            ahead(it);
+#pragma unroll 1
+            for (int c = 0; c < NB / 2; ++c) {
+                const unsigned char* st = stage + c * 4 * BLK;
+                const int k0 = beg + it * KEYS + c * 32;
+                if (kw > 0 || k0 >= sees_any) break;
+                f32x16 sc;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+                for (int s = 0; s < KS; ++s) mma32<T>(sc, k_frag(st, s), *(const uint4*)(q + s * 32));
+                settle<T>();
+                const unsigned seen = seen_of(k0);
+                hide(sc, seen);
+                of(st, k0, seen, sc);
+            }
+        }
+        lds_sync();                                  // every wave past the last stage
+    }
+
+    // The careful pass: the row's highest score, the sum of its weights, then its outputs 32
+    // dims at a time.  Weights are taken against the score itself, at most 1, and have a sum of
+    // their own: the first pass' sum holds what the rounding of its reference left out, a
+    // factor of 2^0.25 at scores of 2^24 and of 2^16 at 2^30.  They meet the values by a power
+    // of two below 1 / sum, which rounds nothing.
+    __device__ __forceinline__ void again(bool bad) {
+        float top = -INFINITY, l = 0.f;
+        sweep([&](const unsigned char*, int, unsigned, const f32x16& sc) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[i]);
+        });
+        top = half_max(top);
+        if (top == -INFINITY) top = 0.f;
+        auto weight = [&](float x) { return __builtin_amdgcn_exp2f((x - top) * a.scale_log2); };
+        sweep([&](const unsigned char*, int, unsigned, const f32x16& sc) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) l += weight(sc[i]);
+        });
+        l = half_sum(l);
+        const float cut = l >= 1.f ? __uint_as_float(0x7e800000u - (__float_as_uint(l) & 0x7f800000u)) : 1.f;
+        const float inv = share(l * cut);
 #pragma unroll 1
         for (int t = 0; t < NT; ++t) {
             f32x16 v;
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] = 0.f;
-            start();
-            for (int it = 0; it < n_st; ++it) {
-                const unsigned char* stage = open(it);
-                ahead(it);
+            sweep([&](const unsigned char* st, int k0, unsigned seen, const f32x16& sc) {
 #pragma unroll 1
-                for (int c = 0; c < NB / 2; ++c) {
-                    const unsigned char* st = stage + c * 4 * BLK;
-                    const int k0 = beg + it * KEYS + c * 32;
-                    if (kw > 0 || k0 >= sees_any) break;
-                    f32x16 sc;
+                for (int u = 0; u < 2; ++u) {
+                    T p[8];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) mma32<T>(sc, k_frag(st, s), *(const uint4*)(q + s * 32));
-                    settle<T>();
-                    const unsigned seen = seen_of(k0);
-                    hide(sc, seen);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) sc[i] = apart(sc[i] * a.scale_log2);     // (rounded as the maximum)
-#pragma unroll 1
-                    for (int u = 0; u < 2; ++u) {
-                        T p[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            p[i] = from_f32<T>(__builtin_amdgcn_exp2f((u ? sc[8 + i] : sc[i]) - ref));
-                        vraw x[2];
-                        v_frag(st, u, t, x);
-                        v_cut(u, at.len - k0, x);
-                        mma_block_careful<T>(v, x[0], x[1], p, seen >> (16 * u + 4 * h));
-                    }
+                    for (int i = 0; i < 8; ++i) p[i] = from_f32<T>(weight(u ? sc[8 + i] : sc[i]) * cut);
+                    vraw x[2];
+                    v_frag(st, u, t, x);
+                    v_cut(u, at.len - k0, x);
+                    mma_block_careful<T>(v, x[0], x[1], p, seen >> (16 * u + 4 * h));
                 }
-            }
-            lds_sync();                              // every wave past the last stage
+            });
             put(t, v, inv, bad);
         }
     }
@@ -685,7 +708,7 @@ void k_rows_attn(RowsAttnArgs a) {
     int block = blockIdx.x;
     asm volatile("" : "+s"(block));
     RowsWork<T, HD, RW, KW> w(a, smem);
-    if (w.place(block)) w.again(m, l, s_bad != 0);
+    if (w.place(block)) w.again(s_bad != 0);
 }
 
 // Joins the splits of head rows, a wave to one or several: a lane has one split's maximum
@@ -728,23 +751,23 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
             L += x[1] * scale(x);
         }
         L = wave_sum_dpp(L);
+        const bool none = a.mask && base == 0 && (a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull)) == 0;
+        const float inv = none ? 0.f : 1.f / L;
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-        const float f0 = scale(mine);
+        const float f0 = mine[1] * scale(mine) * inv;            // the split's share of the row's weights
 #pragma unroll
         for (int i = 0; i < UNROLL; ++i) {
             const int s = set + i * SETS;
             const float f = __shfl(f0, min(s, 63), 64);
             if (s < n) acc += first[i] * f;
         }
-        for (int s = set + UNROLL * SETS; s < n; s += SETS) acc += *(const f32x4*)(part + (size_t)s * HD) * scale(ml[s]);
+        for (int s = set + UNROLL * SETS; s < n; s += SETS) acc += *(const f32x4*)(part + (size_t)s * HD) * (ml[s][1] * scale(ml[s]) * inv);
 #pragma unroll
         for (int w = LANES; w < 64; w *= 2)
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], w, 64);
         if (set != 0) continue;
-        const bool none = a.mask && base == 0 && (a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull)) == 0;
-        const float inv = none ? 0.f : 1.f / L;
-        const float x[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+        const float x[4] = {acc[0], acc[1], acc[2], acc[3]};
         put_out<T, HD>(a, head_row, d, x);
         if (a.lse && d == 0) a.lse[head_row] = log_sum(M, L, none);
     }

@@ -1,0 +1,125 @@
+"""pbd_packed_attention and pbd_tree_attention where scores or values are far from 1: what a row gets when its tile is gone
+over a second time, in one part and in several."""
+import math
+
+import pytest
+import torch
+
+import paged_ref as ref
+import rows_ref as rr
+from test_gpu_packed_attention import BF, DEV, F32, Call
+
+pytestmark = pytest.mark.gpu
+
+U = ref.U
+
+
+def spread(parts, D, dtype):
+    """(cache, rows of each sequence): one sequence of 150 rows over as many slots, or of 40 over 3000."""
+    return (ref.Cache([3000], 1, D, dtype, seed=6), [40]) if parts else (ref.Cache([150], 1, D, dtype, seed=6), [150])
+
+
+def put(cache, k0):
+    """Keys that are 0 but in dim 0."""
+    n = cache.lens[0]
+    cache.dk[0, 0, :n] = 0.0
+    cache.dk[0, 0, :n, 0] = k0.to(cache.dtype)
+    cache.put(0, 0, cache.dk[0, :, :n], cache.dv[0, :, :n])
+
+
+def call(cache, counts, e, masks=None):
+    c = Call(cache, counts, 1, masks=masks)
+    c.q = torch.zeros_like(c.q)
+    c.q[..., 0] = 2.0 ** e
+    c.dq.copy_(c.q.to(DEV))
+    return c
+
+
+@pytest.mark.parametrize("parts", [False, True])
+@pytest.mark.parametrize("odd", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_one_score_far_above_the_others(dtype, odd, parts):
+    """Scores up to some 2^14 .. 2^37, also where the last slot's NaN, hidden from the rows before, sends their tile through
+    the second pass: each row gets the mean of the highest slots that it sees.
+
+    Scores are products of one power of two, exact, and 2^14 / 8 at least apart, so that the others' weights are 0.  Equal
+    scores have equal weights, whatever the reference: n + 80 roundings of the sums, four of the quotients and factors, and in
+    bf16 one of the weight, half a step; the output's own."""
+    D = 64
+    half = torch.finfo(dtype).eps / 2
+    for e in (14, 17, 18, 20, 23, 24, 26, 28, 29, 30):
+        for down in (False, True):
+            cache, counts = spread(parts, D, dtype)
+            n, R = cache.lens[0], counts[0]
+            ramp = torch.arange(n) * 37 % 113 if parts else torch.arange(n) % 113
+            k0 = 5.0 + (112 - ramp if down else ramp)    # (up to 117: products with the scale are not exact)
+            if odd:
+                cache.dv[0, 0, n - 1] = math.nan
+            put(cache, k0)
+            c = call(cache, counts, e)
+            assert (c.ws.numel() > 256) == parts
+            c.run()
+            out, lse, v = c.out.double().cpu(), c.lse.double().cpu(), cache.dv[0, 0].double()
+            for i in range(R):
+                if odd and i == R - 1:
+                    assert torch.isnan(out[i, 0]).all()
+                    continue
+                seen = k0[: n - R + i + 1].double()
+                top = (seen == seen.max()).nonzero()[:, 0]
+                want, size = v[top].mean(0), v[top].abs().mean(0)
+                tol = want.abs() * half * 1.01 + size * ((n + 84) * U + (half * 1.01 if dtype == BF else 0.0))
+                off = (out[i, 0] - want).abs()
+                assert torch.all(off <= tol), (e, down, i, (off / size).max())
+                s = float(seen.max()) * 2.0 ** e / 8
+                assert abs(float(lse[i, 0]) - s - math.log(len(top))) <= 8 * U * s + (n + 84) * U
+
+
+@pytest.mark.parametrize("parts", [False, True])
+@pytest.mark.parametrize("odd", [False, True])
+@pytest.mark.parametrize("down", [False, True])
+def test_scores_one_step_apart(down, odd, parts):
+    """fp32 scores past 2^31, each a step of the type above (below) the one before: in units of log2 some of two such round to
+    one number.  A row gets the highest slot that it sees, or a mean of it and slots that are one step below."""
+    D = 64
+    for e in (33, 60, 92):
+        cache, counts = spread(parts, D, F32)
+        n, R = cache.lens[0], counts[0]
+        step = torch.arange(n).double()
+        k0 = 1.9 + (n - 1 - step if down else step) * 2.0 ** -23
+        k0 = k0.float()
+        assert torch.all((k0.double().diff().abs() * 2 ** 23).round() == 1)
+        if odd:
+            cache.dv[0, 0, n - 1] = math.nan
+        put(cache, k0)
+        c = call(cache, counts, e)
+        assert (c.ws.numel() > 256) == parts
+        c.run()
+        out, v = c.out.double().cpu(), cache.dv[0, 0].double()
+        for i in range(R - 1 if odd else R):
+            last = 0 if down else n - R + i
+            pair = v[[last, min(1, n - R + i) if down else max(0, last - 1)]]
+            tol = 4 * U * pair.abs().amax(0)
+            assert torch.all(out[i, 0] >= pair.amin(0) - tol) and torch.all(out[i, 0] <= pair.amax(0) + tol), (e, i)
+
+
+@pytest.mark.parametrize("trees", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_query_that_is_not_finite_beside_large_scores(dtype, D, trees):
+    """Rows of a tile in which another row's query is NaN, ordinary weights between scores of some thousands: the bound that
+    holds without it holds with it."""
+    g = torch.Generator().manual_seed(D)
+    for lens, counts in (([150, 40], [60, 40]), ([3000], [40])):
+        t = [rr.random_tree(n, g) for n in counts] if trees else None
+        c = Call(ref.Cache(lens, 2, D, dtype, seed=7), counts, 2, trees=t)
+        c.dq[3, 1, 5] = math.nan
+        c.run(scale=2000.0)
+        assert torch.isnan(c.out[3, 1]).all() and torch.isnan(c.lse[3, 1])
+        out, lse = c.out.clone(), c.lse.clone()
+        c.dq.copy_(c.q.to(DEV))
+        c.run(scale=2000.0)
+        c.check(scale=2000.0)
+        out[3, 1], lse[3, 1] = c.out[3, 1], c.lse[3, 1]
+        c.out.copy_(out)
+        c.lse.copy_(lse)
+        c.check(scale=2000.0)
