@@ -621,71 +621,73 @@ struct RowsWork {
         return false;
     }
 
-    // One pass over the slots for the careful one: of(stage, first slot, what the row sees, scores) for
-    // each 32 of them, in the waves of kw 0.
-    template <typename F> __device__ __forceinline__ void sweep(F&& of) {
-        start();
-        for (int it = 0; it < n_st; ++it) {
-            const unsigned char* stage = open(it);
-            ahead(it);
-#pragma unroll 1
-            for (int c = 0; c < NB / 2; ++c) {
-                const unsigned char* st = stage + c * 4 * BLK;
-                const int k0 = beg + it * KEYS + c * 32;
-                if (kw > 0 || k0 >= sees_any) break;
-                f32x16 sc;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sc[i] = 0.f;
-#pragma unroll
-                for (int s = 0; s < KS; ++s) mma32<T>(sc, k_frag(st, s), *(const uint4*)(q + s * 32));
-                settle<T>();
-                const unsigned seen = seen_of(k0);
-                hide(sc, seen);
-                of(st, k0, seen, sc);
-            }
-        }
-        lds_sync();                                  // every wave past the last stage
-    }
-
-    // The careful pass: the row's highest score, the sum of its weights, then its outputs 32
-    // dims at a time.  Weights are taken against the score itself, at most 1, and have a sum of
-    // their own: the first pass' sum holds what the rounding of its reference left out, a
-    // factor of 2^0.25 at scores of 2^24 and of 2^16 at 2^30.  They meet the values by a power
-    // of two below 1 / sum, which rounds nothing.
+    // The careful pass: the row's highest score and the sum of its weights, then its outputs 32
+    // dims at a time, each in a turn over the slots.  Weights are taken against the score
+    // itself, at most 1, and have a sum of their own: the first pass' sum holds what the
+    // rounding of its reference left out, a factor of 2^0.25 at scores of 2^24 and of 2^16 at
+    // 2^30.  They meet the values by a power of two below 1 / sum, which rounds nothing.
     __device__ __forceinline__ void again(bool bad) {
-        float top = -INFINITY, l = 0.f;
-        sweep([&](const unsigned char*, int, unsigned, const f32x16& sc) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[i]);
-        });
-        top = half_max(top);
-        if (top == -INFINITY) top = 0.f;
-        auto weight = [&](float x) { return __builtin_amdgcn_exp2f((x - top) * a.scale_log2); };
-        sweep([&](const unsigned char*, int, unsigned, const f32x16& sc) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) l += weight(sc[i]);
-        });
-        l = half_sum(l);
-        const float cut = l >= 1.f ? __uint_as_float(0x7e800000u - (__float_as_uint(l) & 0x7f800000u)) : 1.f;
-        const float inv = share(l * cut);
+        float top = -INFINITY, l = 0.f, cut = 1.f, inv = 0.f;
 #pragma unroll 1
-        for (int t = 0; t < NT; ++t) {
+        for (int t = -1; t < NT; ++t) {
             f32x16 v;
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] = 0.f;
-            sweep([&](const unsigned char* st, int k0, unsigned seen, const f32x16& sc) {
+            start();
+            for (int it = 0; it < n_st; ++it) {
+                const unsigned char* stage = open(it);
+                ahead(it);
 #pragma unroll 1
-                for (int u = 0; u < 2; ++u) {
-                    T p[8];
+                for (int c = 0; c < NB / 2; ++c) {
+                    const unsigned char* st = stage + c * 4 * BLK;
+                    const int k0 = beg + it * KEYS + c * 32;
+                    if (kw > 0 || k0 >= sees_any) break;
+                    f32x16 sc;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) p[i] = from_f32<T>(weight(u ? sc[8 + i] : sc[i]) * cut);
-                    vraw x[2];
-                    v_frag(st, u, t, x);
-                    v_cut(u, at.len - k0, x);
-                    mma_block_careful<T>(v, x[0], x[1], p, seen >> (16 * u + 4 * h));
+                    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) mma32<T>(sc, k_frag(st, s), *(const uint4*)(q + s * 32));
+                    settle<T>();
+                    const unsigned seen = seen_of(k0);
+                    hide(sc, seen);
+                    if (t < 0) {
+                        float high = top;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) high = fmaxf(high, sc[i]);
+                        high = half_max(high);
+                        l *= top == high ? 1.f : __builtin_amdgcn_exp2f((top - high) * a.scale_log2);
+                        top = high;
+                    }
+                    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll 1
+                    for (int u = 0; u < 2; ++u) {
+                        T p[8];
+                        float sum = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float w = __builtin_amdgcn_exp2f(((u ? sc[8 + i] : sc[i]) - ref) * a.scale_log2);
+                            sum += w;
+                            p[i] = from_f32<T>(w * cut);
+                        }
+                        if (t < 0) {
+                            l += sum;
+                            continue;
+                        }
+                        vraw x[2];
+                        v_frag(st, u, t, x);
+                        v_cut(u, at.len - k0, x);
+                        mma_block_careful<T>(v, x[0], x[1], p, seen >> (16 * u + 4 * h));
+                    }
                 }
-            });
-            put(t, v, inv, bad);
+            }
+            lds_sync();                              // every wave past the last stage
+            if (t < 0) {
+                l = half_sum(l);
+                if (l >= 1.f) cut = __uint_as_float(0x7e800000u - (__float_as_uint(l) & 0x7f800000u));
+                inv = share(l * cut);
+            } else {
+                put(t, v, inv, bad);
+            }
         }
     }
 };
