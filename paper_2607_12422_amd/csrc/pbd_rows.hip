@@ -46,7 +46,8 @@ __device__ __forceinline__ void raise(int* status, int bit) {
 // A lane's sum of four weights up to which the reference that they are taken against may
 // stay below the scores: looking for the maximum of every step is a tenth of its vector
 // work (two prompts of 8192 tokens 561 us with it, 548 without).  bf16 and fp32 weights
-// have the same relative precision at any size.
+// have the same relative precision at any size; values that overflow under them are taken
+// again in the second pass.
 constexpr float HIGH = 65536.f;
 
 // Maxima (log2 units, either sign) past which a step of the scores' type is 64 or more:
@@ -278,8 +279,11 @@ __device__ __forceinline__ float log_sum(float M, float L, bool none) {
 // RW tiles of 32 head rows, KW waves to a tile, each with its own slots of a stage.
 // A weight of 0 hides no infinite or NaN value from the value product.  Slots past the
 // sequence are cleared; values that a row of the tile does not see while others do are
-// rare enough to be looked for in the result: a work-group whose output holds a NaN
-// goes over its slots again, 32 dims at a time, with products that leave them out.
+// rare enough to be looked for in the result: a work-group whose sums hold a NaN
+// goes over its slots again, 32 dims at a time, with products that leave them out.  So
+// does one whose sums are infinite: weights up to HIGH, or many at once, take large finite
+// values there, and the second pass' weights, whose sum is at most 1, do not.
+// A split writes the weighted means of its slots' values, its maximum and its sum.
 // ---------------------------------------------------------------------------
 template <typename T, int HD, int RW, int KW>
 struct RowsWork {
@@ -568,18 +572,8 @@ struct RowsWork {
             }
         }
         l = half_sum((part[0] + part[1]) + (part[2] + part[3]));
-        {
-            f32x16 all = o[0];
-#pragma unroll
-            for (int t = 1; t < NT; ++t) all += o[t];
-            float one = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) one += all[i];
-            if (__any(live && one != one) && lane == 0) *s_odd = 1;
-        }
-        lds_sync();                                  // every wave past the last stage; s_bad and s_odd are final
-        const bool redo = *s_odd != 0, bad = *s_bad != 0;
         if constexpr (KW > 1) {
+            lds_sync();                              // every wave past the last stage
             float* part = (float*)smem + (size_t)rw * 64 * (NT * 16 + 2);
             if (kw > 0) {
 #pragma unroll
@@ -602,8 +596,19 @@ struct RowsWork {
                     for (int i = 0; i < 16; ++i) o[t][i] = o[t][i] * f0 + part[(t * 16 + i) * 64 + lane] * f1;
                 m = M;
             }
-            lds_sync();                              // the ring may be filled again
         }
+        // a NaN or an infinite sum (or finite ones whose sum is infinite)
+        if (kw == 0) {
+            f32x16 all = o[0];
+#pragma unroll
+            for (int t = 1; t < NT; ++t) all += o[t];
+            float one = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) one += all[i];
+            if (__any(live && !__builtin_isfinite(one)) && lane == 0) *s_odd = 1;
+        }
+        lds_sync();                                  // s_bad and s_odd are final, the ring may be filled again
+        const bool redo = *s_odd != 0, bad = *s_bad != 0;
         if (bad && threadIdx.x == 0) raise(a.pg.status, PBD_STATUS_PAGE);
         if (kw == 0 && live && h == 0) {
             const size_t part_row = head_row * a.splits + split;

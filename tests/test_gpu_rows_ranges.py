@@ -123,3 +123,75 @@ def test_a_query_that_is_not_finite_beside_large_scores(dtype, D, trees):
         c.out.copy_(out)
         c.lse.copy_(lse)
         c.check(scale=2000.0)
+
+
+@pytest.mark.parametrize("trees", [False, True])
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("kind", ["rising", "flat", "any"])
+def test_values_near_the_largest_finite_ones(kind, dtype, D, trees):
+    """Values up to 2^127, of either sign or of one: a weighted mean of them is finite, however many slots share the weight
+    and however far the scores rise.  The bound is the usual one, relative to the values."""
+    g = torch.Generator().manual_seed(D)
+    for lens, counts in (([200, 33, 1500], [64, 33, 64]), ([3000], [40]), ([9000, 700], [3, 64])):
+        for e in (110, 126):
+            cache = ref.Cache(lens, 1, D, dtype, seed=2)
+            cache.dv = (cache.dv.float().clamp(-1.9, 1.9) * 2.0 ** e).to(dtype)
+            if kind != "any":
+                cache.dv = cache.dv.abs()
+            for b, m in enumerate(lens):
+                if kind != "any":
+                    cache.dk[b, 0, :m] = 0.0
+                    cache.dk[b, 0, :m, 0] = (torch.arange(m) % 200).to(dtype)
+                cache.put(b, 0, cache.dk[b, :, :m], cache.dv[b, :, :m])
+            c = Call(cache, counts, 2, trees=[rr.random_tree(n, g) for n in counts] if trees else None)
+            if kind != "any":
+                c.q = torch.zeros_like(c.q)
+                c.q[..., 0] = 0.0 if kind == "flat" else 0.25
+                c.dq.copy_(c.q.to(DEV))
+            c.run(scale=0.5)
+            assert torch.isfinite(c.out[: c.starts[-1]]).all(), (lens, e)
+            c.check(scale=0.5)
+
+
+@pytest.mark.parametrize("parts", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_large_values_under_large_scores(dtype, parts):
+    """What a rounded reference leaves in the exponent, up to 2^64, reaches no value: the highest slot's values come out."""
+    D = 64
+    half = torch.finfo(dtype).eps / 2
+    for e in (17, 24, 28, 30):
+        cache, counts = spread(parts, D, dtype)
+        n, R = cache.lens[0], counts[0]
+        cache.dv = (cache.dv.float().clamp(-1.9, 1.9).abs() * 2.0 ** 126).to(dtype)
+        put(cache, 5.0 + torch.arange(n) * 37 % 113)
+        c = call(cache, counts, e)
+        c.run()
+        out, v = c.out.double().cpu(), cache.dv[0, 0].double()
+        k0 = cache.dk[0, 0, :n, 0].double()
+        for i in range(R):
+            seen = k0[: n - R + i + 1]
+            top = (seen == seen.max()).nonzero()[:, 0]
+            want, size = v[top].mean(0), v[top].abs().mean(0)
+            tol = want.abs() * half * 1.01 + size * ((n + 84) * U + (half * 1.01 if dtype == BF else 0.0))
+            assert torch.all((out[i, 0] - want).abs() <= tol), (e, i)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_infinite_values_that_all_rows_see(dtype):
+    """An infinite value under a weight is infinite in its dim, both signs together are NaN; other dims keep the bound."""
+    for lens, counts in (([150], [40]), ([3000], [40])):
+        cache = ref.Cache(lens, 1, 64, dtype, seed=3)
+        n = lens[0]
+        clean = cache.dv.clone()
+        cache.dv[0, 0, 50, 3] = math.inf
+        cache.dv[0, 0, n - 60, 4] = -math.inf
+        cache.dv[0, 0, 20, 9], cache.dv[0, 0, n - 50, 9] = math.inf, -math.inf
+        cache.put(0, 0, cache.dk[0, :, :n], cache.dv[0, :, :n])
+        c = Call(cache, counts, 2)
+        c.run()
+        out = c.out.double().cpu()[: counts[0]]
+        assert torch.all(out[..., 3] == math.inf) and torch.all(out[..., 4] == -math.inf) and torch.isnan(out[..., 9]).all()
+        cache.dv = clean
+        o, _, tol, _ = rr.attention(cache, 0, c.q[: counts[0]], c.see(0), 64 ** -0.5)
+        keep = [d for d in range(64) if d not in (3, 4, 9)]
+        assert torch.all((out - o).abs()[..., keep] <= tol[..., keep])
