@@ -542,7 +542,8 @@ int pbd_decode_paged(pbd_ctx* ctx, const pbd_pages* pages, int32_t batch, int32_
  * range, or whose rows do not end within max_rows, raises PBD_STATUS_CAPACITY: it keeps
  * its pages, its rows (there for n_new > 0, within max_rows) have slot -1 and
  * new_lens[b] is lens[b].  A page id outside [0, n_pages) among those to be taken raises
- * PBD_STATUS_PAGE and nobody who needs a page is served.
+ * PBD_STATUS_PAGE and nobody who needs a page is served.  So does one among the pages that
+ * a sequence has already, where new rows go to it: those rows have slot -1.
  * page_size: as in pbd_pages; n_pages * page_size below 2^31; max_rows in [0, 2^22].
  * row_start, new_lens and the other outputs overlap no input but the three in place.
  * The append skips the rows of a sequence that was not served; an attention over its

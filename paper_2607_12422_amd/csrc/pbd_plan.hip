@@ -64,7 +64,10 @@ __device__ __forceinline__ void put_row(const PagePlanArgs& a, int r, int b) {
         if (a.row_pos) at = a.pos[b] + i;
         if (a.new_lens[b] != len) {                  // (it has rows: equal only where it was skipped)
             const int s = len + i;
-            slot = a.table[(size_t)b * a.table_width + (s >> a.page_bits)] << a.page_bits | (s & ((1 << a.page_bits) - 1));
+            const int id = a.table[(size_t)b * a.table_width + (s >> a.page_bits)];
+            // (a page that the sequence had: shifted, an id past the pool may be another page's slot)
+            if (id >= 0 && id < a.n_pages) slot = id << a.page_bits | (s & ((1 << a.page_bits) - 1));
+            else raise(a.status, PBD_STATUS_PAGE);
         }
     }
     a.slot_map[r] = slot;
