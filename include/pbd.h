@@ -548,7 +548,8 @@ int pbd_decode_paged(pbd_ctx* ctx, const pbd_pages* pages, int32_t batch, int32_
  * row_start, new_lens and the other outputs overlap no input but the three in place.
  * The append skips the rows of a sequence that was not served; an attention over its
  * new_lens would take its last cached slots for them, so a program looks at status
- * or new_lens before it uses their outputs.
+ * or new_lens before it uses their outputs.  pbd_tree_commit would move those slots:
+ * where sequences may not be served, pbd_tree_commit_served is the one to call.
  * A table, its stack and counts belong to one call at a time.
  */
 int pbd_page_plan(int32_t batch, int32_t page_size, int32_t n_pages, int32_t* table, int32_t table_width,
@@ -649,7 +650,10 @@ int pbd_tree_attention(const pbd_pages* pages, int32_t batch, int32_t rows, cons
  * and V of the path's nodes move to the slots lens[b] - n + 0..k, and new_lens[b] = lens[b]
  * - n + k + 1; what lies behind is given up.  A sequence without rows is left as it is.
  * n above width or 64, or lens[b] < n: PBD_STATUS_CAPACITY; PBD_STATUS_TREE as
- * pbd_tree_layout; PBD_STATUS_PAGE for the nodes' pages: the sequence is skipped.
+ * pbd_tree_layout; PBD_STATUS_PAGE for the nodes' pages: the sequence is skipped, its
+ * outputs stay as they were.
+ * The last n of the lens[b] slots are taken for the nodes, whatever was appended there: for
+ * a sequence that a plan did not serve they are tokens committed earlier.
  * Outputs overlap no input (new_lens is not lens) and not each other; the nodes' pages
  * belong to one sequence.  A cache that keeps score or slot_pos is refused
  * (PBD_ERR_UNSUPPORTED).  n_layers >= 1, n_layers * n_kv_heads < 2^24; width in [1, 2^20].
@@ -658,6 +662,21 @@ int pbd_tree_commit(const pbd_pages* pages, int32_t n_layers, int32_t batch, int
                     const int32_t* lens, const int32_t* parent, const int32_t* tokens, const int32_t* verify,
                     int32_t width, int32_t* path, int32_t* n_accepted, int32_t* out_tokens, int32_t* new_lens,
                     int32_t* anchor, pbd_stream_t stream);
+
+/*
+ * pbd_tree_commit where some sequences may have no slots for their nodes: before (device
+ * int32 [batch]) are the lengths that the plan was given, lens its new_lens.  A sequence
+ * whose lens[b] is not before[b] + n was not served: it is skipped, with no status of its
+ * own.  A sequence that is skipped, for this or any other reason, or has no rows keeps
+ * its cache as it is and has new_lens[b] = lens[b], n_accepted[b] = -1 and -1 all along path
+ * and out_tokens; its anchor stays as it was.  So new_lens can go to the next plan
+ * and to pbd_page_release with no look at it by the host.  Everything else as
+ * pbd_tree_commit.
+ */
+int pbd_tree_commit_served(const pbd_pages* pages, int32_t n_layers, int32_t batch, int32_t rows, const int32_t* row_start,
+                           const int32_t* before, const int32_t* lens, const int32_t* parent, const int32_t* tokens,
+                           const int32_t* verify, int32_t width, int32_t* path, int32_t* n_accepted, int32_t* out_tokens,
+                           int32_t* new_lens, int32_t* anchor, pbd_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Implementation controls.  The calls below are not part of the step's

@@ -109,6 +109,32 @@ int rows_attention(const pbd_pages* pages, int batch, int rows, const void* q, i
     return hip_result(launch_rows_attn(pages->dtype, pages->head_dim, a, plan, (hipStream_t)stream), "attention of rows");
 }
 
+int tree_commit(const pbd_pages* pages, int32_t n_layers, int32_t batch, int32_t rows, const int32_t* row_start,
+                const int32_t* before, const int32_t* lens, const int32_t* parent, const int32_t* tokens,
+                const int32_t* verify, int32_t width, int32_t* path, int32_t* n_accepted, int32_t* out_tokens,
+                int32_t* new_lens, int32_t* anchor, pbd_stream_t stream) {
+    const int rc = pages_ok(pages, batch, 0);
+    if (rc) return rc;
+    if (pages->score || pages->slot_pos) return op_fail(PBD_ERR_UNSUPPORTED, "the cache keeps score or slot_pos");
+    if (n_layers < 1 || (long long)n_layers * pages->n_kv_heads > GROUPS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "n_layers out of range");
+    if (rows < 1 || rows > ROWS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "rows outside [1, 2^22]");
+    if (width < 1 || width > (1 << 20)) return op_fail(PBD_ERR_INVALID_ARG, "width outside [1, 2^20]");
+    if (!row_start || !lens || !parent || !tokens || !verify || !path || !n_accepted || !out_tokens || !new_lens)
+        return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
+    if (n_layers > 1 && (pages->layer_stride < 0 || pages->layer_stride % (16 * pages->head_dim)))
+        return op_fail(PBD_ERR_INVALID_ARG, "layer_stride must be a multiple of 16 head_dim");
+    if (new_lens == lens || new_lens == before || path == out_tokens || anchor == new_lens || anchor == n_accepted || n_accepted == new_lens)
+        return op_fail(PBD_ERR_INVALID_ARG, "new_lens must not be lens, and outputs not each other");
+    TreeCommitArgs a{};
+    a.pg = page_view(*pages);
+    a.n_kv = pages->n_kv_heads; a.n_layers = n_layers; a.batch = batch; a.rows = rows; a.width = width;
+    a.layer_stride = n_layers > 1 ? pages->layer_stride : 0;
+    a.row_start = row_start; a.lens = lens; a.parent = parent; a.tokens = tokens; a.verify = verify;
+    a.path = path; a.n_accepted = n_accepted; a.out_tokens = out_tokens; a.new_lens = new_lens; a.anchor = anchor;
+    a.before = before;
+    return hip_result(launch_tree_commit(pages->dtype, pages->head_dim, a, (hipStream_t)stream), "tree commit");
+}
+
 }  // namespace
 
 int check_pages(const pbd_pages* p, int batch, int max_len, char (&msg)[192]) {
@@ -387,25 +413,17 @@ int pbd_tree_commit(const pbd_pages* pages, int32_t n_layers, int32_t batch, int
                     const int32_t* lens, const int32_t* parent, const int32_t* tokens, const int32_t* verify,
                     int32_t width, int32_t* path, int32_t* n_accepted, int32_t* out_tokens, int32_t* new_lens,
                     int32_t* anchor, pbd_stream_t stream) {
-    const int rc = pages_ok(pages, batch, 0);
-    if (rc) return rc;
-    if (pages->score || pages->slot_pos) return op_fail(PBD_ERR_UNSUPPORTED, "the cache keeps score or slot_pos");
-    if (n_layers < 1 || (long long)n_layers * pages->n_kv_heads > GROUPS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "n_layers out of range");
-    if (rows < 1 || rows > ROWS_MAX) return op_fail(PBD_ERR_INVALID_ARG, "rows outside [1, 2^22]");
-    if (width < 1 || width > (1 << 20)) return op_fail(PBD_ERR_INVALID_ARG, "width outside [1, 2^20]");
-    if (!row_start || !lens || !parent || !tokens || !verify || !path || !n_accepted || !out_tokens || !new_lens)
-        return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
-    if (n_layers > 1 && (pages->layer_stride < 0 || pages->layer_stride % (16 * pages->head_dim)))
-        return op_fail(PBD_ERR_INVALID_ARG, "layer_stride must be a multiple of 16 head_dim");
-    if (new_lens == lens || path == out_tokens || anchor == new_lens || anchor == n_accepted || n_accepted == new_lens)
-        return op_fail(PBD_ERR_INVALID_ARG, "new_lens must not be lens, and outputs not each other");
-    TreeCommitArgs a{};
-    a.pg = page_view(*pages);
-    a.n_kv = pages->n_kv_heads; a.n_layers = n_layers; a.batch = batch; a.rows = rows; a.width = width;
-    a.layer_stride = n_layers > 1 ? pages->layer_stride : 0;
-    a.row_start = row_start; a.lens = lens; a.parent = parent; a.tokens = tokens; a.verify = verify;
-    a.path = path; a.n_accepted = n_accepted; a.out_tokens = out_tokens; a.new_lens = new_lens; a.anchor = anchor;
-    return hip_result(launch_tree_commit(pages->dtype, pages->head_dim, a, (hipStream_t)stream), "tree commit");
+    return tree_commit(pages, n_layers, batch, rows, row_start, nullptr, lens, parent, tokens, verify, width, path, n_accepted,
+                       out_tokens, new_lens, anchor, stream);
+}
+
+int pbd_tree_commit_served(const pbd_pages* pages, int32_t n_layers, int32_t batch, int32_t rows, const int32_t* row_start,
+                           const int32_t* before, const int32_t* lens, const int32_t* parent, const int32_t* tokens,
+                           const int32_t* verify, int32_t width, int32_t* path, int32_t* n_accepted, int32_t* out_tokens,
+                           int32_t* new_lens, int32_t* anchor, pbd_stream_t stream) {
+    if (!before) return op_fail(PBD_ERR_INVALID_ARG, "before is NULL");
+    return tree_commit(pages, n_layers, batch, rows, row_start, before, lens, parent, tokens, verify, width, path, n_accepted,
+                       out_tokens, new_lens, anchor, stream);
 }
 
 }  // extern "C"

@@ -81,6 +81,7 @@ struct TreeCommitArgs {
     int* out_tokens;            // [batch][width]
     int* new_lens;
     int* anchor;                // or null
+    const int* before;          // lengths before the rows: sequences whose rows have no slots keep all they have; or null
 };
 hipError_t launch_tree_commit(int dtype, int head_dim, const TreeCommitArgs& a, hipStream_t st);
 

@@ -58,6 +58,8 @@ __global__ __launch_bounds__(256) void k_tree_layout(TreeLayoutArgs a) {
 // (bf16, head_dim 128), all of them read and written.  32 trees of 33 to 64 nodes over
 // 28 layers of 8 heads, two slots moved on average, take 20 us: 88 MB of lines for 7 MB
 // of slots.  Four layers a work-group, their loads together, took 24.
+// Rows that a plan gave no slots are not behind the sequence: with the lengths before
+// the plan, such a sequence is told by its length, and no slot of it is touched.
 // ---------------------------------------------------------------------------
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_tree_commit(TreeCommitArgs a) {
@@ -68,11 +70,24 @@ __global__ __launch_bounds__(256) void k_tree_commit(TreeCommitArgs a) {
     int r0, n;
     const bool rows_ok = tree_rows(a.row_start, b, a.rows, min(a.width, TREE_MAX), r0, n);
     const int len = a.lens[b], base = len - n;
-    if (!rows_ok || len < n || len > a.pg.cap) {
+    auto keep = [&] {                                // what a skipped sequence has
+        if (!a.before || blockIdx.x != 0) return;
+        for (int i = threadIdx.x; i < a.width; i += 256) a.path[(size_t)b * a.width + i] = a.out_tokens[(size_t)b * a.width + i] = -1;
+        if (threadIdx.x == 0) {
+            a.n_accepted[b] = -1;
+            a.new_lens[b] = len;
+        }
+    };
+    const bool slots = rows_ok && !(a.before && base != a.before[b]);
+    if (!rows_ok || len < 0 || len > a.pg.cap || (slots && base < 0)) {
         if (first) raise(a.pg.status, PBD_STATUS_CAPACITY);
+        keep();
         return;
     }
-    if (n == 0) return;
+    if (n == 0 || !slots) {
+        keep();
+        return;
+    }
     const bool node = lane < n;
     const int up = node ? a.parent[r0 + lane] : -1, tok = node ? a.tokens[r0 + lane] : -1, says = node ? a.verify[r0 + lane] : -1;
     const int sh = a.pg.page_shift + 4, *table = a.pg.table + (size_t)b * a.pg.table_width;
@@ -87,10 +102,12 @@ __global__ __launch_bounds__(256) void k_tree_commit(TreeCommitArgs a) {
     }
     if (__any(up < -1 || up >= lane)) {
         if (first) raise(a.pg.status, PBD_STATUS_TREE);
+        keep();
         return;
     }
     if (__any(bad_page)) {
         if (first) raise(a.pg.status, PBD_STATUS_PAGE);
+        keep();
         return;
     }
     int at = 0, count = 1, mine = lane == 0 ? 0 : -1;        // mine: the path's node number `lane`
