@@ -610,7 +610,11 @@ int pbd_paged_append_rows(const pbd_pages* pages, int32_t rows, const float* q, 
  * lens[b] outside [0, max_len] or less than n, row_start out of [0, rows] or
  * descending (then others may be skipped with it).  PBD_STATUS_PAGE: a bad page among
  * those of the lens[b] slots.  Such a sequence's outputs stay as they were.
+ * ws: of at least the call's workspace_bytes for its batch, rows and max_len.  Fewer or
+ * shorter sequences may need more: they are split into more parts.  No call needs more
+ * than PBD_ROWS_WORKSPACE_MAX, so that a program whose batches come and go takes that.
  */
+#define PBD_ROWS_WORKSPACE_MAX ((size_t)48 << 20)
 size_t pbd_packed_attention_workspace_bytes(const pbd_pages* pages, int32_t batch, int32_t rows, int32_t max_len);
 int pbd_packed_attention(const pbd_pages* pages, int32_t batch, int32_t rows, const void* q, int64_t q_stride,
                          const int32_t* row_start, const int32_t* lens, int32_t max_len, float scale,

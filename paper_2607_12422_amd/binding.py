@@ -42,6 +42,7 @@ PBD_STATUS_FORCED_N = 4
 PBD_STATUS_TIMEOUT = 8
 PBD_STATUS_PAGE = 16
 PBD_STATUS_TREE = 32
+PBD_ROWS_WORKSPACE_MAX = 48 << 20       # no pbd_packed_attention or pbd_tree_attention needs a larger workspace
 
 EXPORTED = (
     "pbd_packed_weight_bytes", "pbd_kv_bytes", "pbd_workspace_bytes", "pbd_init_weights",
@@ -556,7 +557,8 @@ def pbd_packed_attention_workspace_bytes(pages: PbdPages, batch: int, rows: int,
 def pbd_packed_attention(pages: PbdPages, q, row_start, lens, max_len: int, out, ws, lse=None,
                          scale: Optional[float] = None, stream=None):
     """q [rows][n_q_heads][head_dim] of the cache's type (any stride from a row to the next), row_start int32 [batch + 1],
-    lens int32 [batch]; out like q, contiguous, lse float32 [rows][n_q_heads].  scale: 1 / sqrt(head_dim) if None."""
+    lens int32 [batch]; out like q, contiguous, lse float32 [rows][n_q_heads].  scale: 1 / sqrt(head_dim) if None.
+    ws: the call's workspace_bytes, or PBD_ROWS_WORKSPACE_MAX for calls of any sizes."""
     _rows_attention("pbd_packed_attention", pages, q, row_start, lens, None, max_len, out, ws, lse, scale, stream)
 
 

@@ -845,6 +845,7 @@ RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batc
     p.longest = !tree && p.splits == 1 && batch > 1 && batch <= 64 && p.groups * n_kv > 512 && p.groups * n_kv <= 4096 &&
                 max_len * seen >= 1024;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    // (parts of at most 512 / 0.7 = 731 work-groups with rows, of at most 128 head rows each)
     const size_t n = p.splits == 1 ? 0 : (size_t)rows * n_q * p.splits;
     p.off_ml = up(n * head_dim * 4);
     p.bytes = std::max<size_t>(256, p.off_ml + up(n * 2 * 4));
@@ -853,6 +854,7 @@ RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batc
 
 namespace {
 constexpr int JOIN_ROWS = 4096;
+static_assert(731 * 128 * (128 + 2) * 4 + 512 <= PBD_ROWS_WORKSPACE_MAX, "the partial sums of any call");
 
 template <typename T, int HD, int RW, int KW>
 hipError_t launch(const RowsAttnArgs& a, const RowsAttnPlan& p, hipStream_t st) {

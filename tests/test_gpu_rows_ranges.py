@@ -7,6 +7,7 @@ import torch
 
 import paged_ref as ref
 import rows_ref as rr
+from paper_2607_12422_amd import binding as pbd
 from test_gpu_packed_attention import BF, DEV, F32, Call
 
 pytestmark = pytest.mark.gpu
@@ -195,3 +196,20 @@ def test_infinite_values_that_all_rows_see(dtype):
         o, _, tol, _ = rr.attention(cache, 0, c.q[: counts[0]], c.see(0), 64 ** -0.5)
         keep = [d for d in range(64) if d not in (3, 4, 9)]
         assert torch.all((out - o).abs()[..., keep] <= tol[..., keep])
+
+
+@pytest.mark.parametrize("trees", [False, True])
+def test_one_workspace_for_batches_that_shrink(trees):
+    """The largest batch's workspace is too small for the ones after it; one of the documented bound does for all."""
+    ws = torch.full((pbd.PBD_ROWS_WORKSPACE_MAX,), 0xFF, dtype=torch.uint8, device=DEV)
+    g = torch.Generator().manual_seed(4)
+    need = []
+    for B in (64, 20, 5, 1):
+        lens = [2000 - 7 * i for i in range(B)]
+        c = Call(ref.Cache(lens, 4, 64, BF, page=64, seed=B), [33] * B, 2, max_len=2048,
+                 trees=[rr.random_tree(33, g) for _ in lens] if trees else None)
+        need.append(c.ws.numel())
+        c.ws = ws
+        c.run()
+        c.check()
+    assert max(need) > need[0] and max(need) <= ws.numel()
