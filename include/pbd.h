@@ -658,8 +658,8 @@ int pbd_tree_attention(const pbd_pages* pages, int32_t batch, int32_t rows, cons
  * outputs stay as they were.
  * The last n of the lens[b] slots are taken for the nodes, whatever was appended there: for
  * a sequence that a plan did not serve they are tokens committed earlier.
- * Outputs overlap no input (new_lens is not lens) and not each other; the nodes' pages
- * belong to one sequence.  A cache that keeps score or slot_pos is refused
+ * Outputs overlap no input (new_lens is not lens) and not each other (PBD_ERR_INVALID_ARG);
+ * the nodes' pages belong to one sequence.  A cache that keeps score or slot_pos is refused
  * (PBD_ERR_UNSUPPORTED).  n_layers >= 1, n_layers * n_kv_heads < 2^24; width in [1, 2^20].
  */
 int pbd_tree_commit(const pbd_pages* pages, int32_t n_layers, int32_t batch, int32_t rows, const int32_t* row_start,

@@ -590,31 +590,29 @@ def pbd_tree_commit(pages: PbdPages, row_start, lens, parent, tokens, verify, pa
     """int32: row_start [batch + 1]; parent, tokens, verify [rows]; path, out_tokens [batch][width]; lens, n_accepted,
     new_lens, anchor [batch].  All layers of the cache are moved.  For sequences that a plan may not have served:
     pbd_tree_commit_served."""
-    _tree_commit("pbd_tree_commit", pages, row_start, (), lens, parent, tokens, verify, path, n_accepted, out_tokens,
-                 new_lens, anchor, stream)
+    dev, B, R = pages.device, lens.numel(), parent.numel()
+    if B > pages.rows:
+        raise PbdError(PBD_ERR_INVALID_ARG, "the table has fewer rows than lens")
+    W = path.shape[-1]
+    _call(dev, stream, load_library().pbd_tree_commit, pages.ref, pages.layers or 1, B, R,
+          _i32(row_start, B + 1, "row_start", dev), _i32(lens, B, "lens", dev), _i32(parent, R, "parent", dev),
+          _i32(tokens, R, "tokens", dev), _i32(verify, R, "verify", dev), W, _i32(path, B * W, "path", dev),
+          _i32(n_accepted, B, "n_accepted", dev), _i32(out_tokens, B * W, "out_tokens", dev),
+          _i32(new_lens, B, "new_lens", dev), _i32(anchor, B, "anchor", dev))
 
 
 def pbd_tree_commit_served(pages: PbdPages, row_start, before, lens, parent, tokens, verify, path, n_accepted, out_tokens,
                            new_lens, anchor=None, stream=None):
     """As pbd_tree_commit; before int32 [batch]: the lengths that the plan was given (lens: its new_lens).  Sequences that
     it did not serve keep all they have, with new_lens = lens and n_accepted = -1."""
-    if before is None:
-        raise PbdError(PBD_ERR_INVALID_ARG, "before must be given")
-    _tree_commit("pbd_tree_commit_served", pages, row_start,
-                 (_i32(before, lens.numel(), "before", pages.device),), lens, parent, tokens, verify, path, n_accepted,
-                 out_tokens, new_lens, anchor, stream)
-
-
-def _tree_commit(name: str, pages, row_start, before, lens, parent, tokens, verify, path, n_accepted, out_tokens, new_lens,
-                 anchor, stream):
     dev, B, R = pages.device, lens.numel(), parent.numel()
     if B > pages.rows:
         raise PbdError(PBD_ERR_INVALID_ARG, "the table has fewer rows than lens")
     W = path.shape[-1]
-    _call(dev, stream, getattr(load_library(), name), pages.ref, pages.layers or 1, B, R,
-          _i32(row_start, B + 1, "row_start", dev), *before, _i32(lens, B, "lens", dev), _i32(parent, R, "parent", dev),
-          _i32(tokens, R, "tokens", dev), _i32(verify, R, "verify", dev), W, _i32(path, B * W, "path", dev),
-          _i32(n_accepted, B, "n_accepted", dev), _i32(out_tokens, B * W, "out_tokens", dev),
+    _call(dev, stream, load_library().pbd_tree_commit_served, pages.ref, pages.layers or 1, B, R,
+          _i32(row_start, B + 1, "row_start", dev), _i32(before, B, "before", dev), _i32(lens, B, "lens", dev),
+          _i32(parent, R, "parent", dev), _i32(tokens, R, "tokens", dev), _i32(verify, R, "verify", dev), W,
+          _i32(path, B * W, "path", dev), _i32(n_accepted, B, "n_accepted", dev), _i32(out_tokens, B * W, "out_tokens", dev),
           _i32(new_lens, B, "new_lens", dev), _i32(anchor, B, "anchor", dev))
 
 

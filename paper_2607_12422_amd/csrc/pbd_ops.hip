@@ -109,6 +109,17 @@ int rows_attention(const pbd_pages* pages, int batch, int rows, const void* q, i
     return hip_result(launch_rows_attn(pages->dtype, pages->head_dim, a, plan, (hipStream_t)stream), "attention of rows");
 }
 
+// int32 arrays of a call.
+struct Words {
+    const int32_t* p;           // null: not there
+    size_t n;
+};
+
+bool overlap(const Words& a, const Words& b) {
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return x && y && x < y + 4 * b.n && y < x + 4 * a.n;
+}
+
 int tree_commit(const pbd_pages* pages, int32_t n_layers, int32_t batch, int32_t rows, const int32_t* row_start,
                 const int32_t* before, const int32_t* lens, const int32_t* parent, const int32_t* tokens,
                 const int32_t* verify, int32_t width, int32_t* path, int32_t* n_accepted, int32_t* out_tokens,
@@ -123,8 +134,16 @@ int tree_commit(const pbd_pages* pages, int32_t n_layers, int32_t batch, int32_t
         return op_fail(PBD_ERR_INVALID_ARG, "NULL pointer argument");
     if (n_layers > 1 && (pages->layer_stride < 0 || pages->layer_stride % (16 * pages->head_dim)))
         return op_fail(PBD_ERR_INVALID_ARG, "layer_stride must be a multiple of 16 head_dim");
-    if (new_lens == lens || new_lens == before || path == out_tokens || anchor == new_lens || anchor == n_accepted || n_accepted == new_lens)
-        return op_fail(PBD_ERR_INVALID_ARG, "new_lens must not be lens, and outputs not each other");
+    const size_t B = batch, R = rows, W = width;
+    const Words out[] = {{path, B * W}, {out_tokens, B * W}, {n_accepted, B}, {new_lens, B}, {anchor, B}};
+    const Words in[] = {{row_start, B + 1}, {before, B}, {lens, B}, {parent, R}, {tokens, R}, {verify, R},
+                        {pages->table, B * pages->table_width}};
+    for (const Words& o : out) {
+        for (const Words& x : in)
+            if (overlap(o, x)) return op_fail(PBD_ERR_INVALID_ARG, "outputs overlap an input");
+        for (const Words* x = out; x != &o; ++x)
+            if (overlap(o, *x)) return op_fail(PBD_ERR_INVALID_ARG, "outputs overlap each other");
+    }
     TreeCommitArgs a{};
     a.pg = page_view(*pages);
     a.n_kv = pages->n_kv_heads; a.n_layers = n_layers; a.batch = batch; a.rows = rows; a.width = width;
