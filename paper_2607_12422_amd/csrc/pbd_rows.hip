@@ -58,6 +58,7 @@ constexpr float FAR = 2147483648.f;
 
 constexpr int NB = 4, KEYS = NB * 16;                // 16-slot blocks of a stage, its slots
 constexpr int RING = 2;                              // stages in LDS
+constexpr int PARTS_MAX = 64;                        // splits of a row's slots: the join's lanes have one each
 
 // acc += A B over the 16 bytes of a lane's row (column): halves of the wave hold the
 // two halves of the step's k values.
@@ -719,8 +720,8 @@ void k_rows_attn(RowsAttnArgs a) {
 }
 
 // Joins the splits of head rows, a wave to one or several: a lane has one split's maximum
-// and sum (and those 64 on), HD / 4 lanes the row's dims of every SETS-th split; the same
-// order whatever ran first.  4 us for one sequence's 34 rows of 33 splits, most of it the
+// and sum, HD / 4 lanes the row's dims of every SETS-th split; the same order whatever ran
+// first.  4 us for one sequence's 34 rows of 33 splits, most of it the
 // waits for the rows' place, their maxima and their sums.
 template <typename T, int HD, int ROWS>
 __global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
@@ -742,26 +743,17 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttnArgs a) {
         for (int i = 0; i < UNROLL; ++i)
             if (i * SETS < n) first[i] = *(const f32x4*)(part + (size_t)min(set + i * SETS, n - 1) * HD);
         const ml2 mine = ml[min(lane, n - 1)];
-        float M = lane < n ? mine[0] : -INFINITY;
-        bool bad = lane < n && mine[0] != mine[0];
-        for (int s = lane + 64; s < n; s += 64) {
-            const ml2 x = ml[s];
-            bad |= x[0] != x[0];
-            M = fmaxf(M, x[0]);
-        }
+        const float M0 = lane < n ? mine[0] : -INFINITY;
+        const bool bad = lane < n && mine[0] != mine[0];
         if (__any(bad)) return;                      // (every row of the sequence says so)
-        M = wave_max_dpp(M);
+        const float M = wave_max_dpp(M0);
         auto scale = [&](ml2 x) { return x[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x[0] - M); };
-        float L = lane < n ? mine[1] * scale(mine) : 0.f;
-        for (int s = lane + 64; s < n; s += 64) {
-            const ml2 x = ml[s];
-            L += x[1] * scale(x);
-        }
-        L = wave_sum_dpp(L);
+        const float own = mine[1] * scale(mine);
+        const float L = wave_sum_dpp(lane < n ? own : 0.f);
         const bool none = a.mask && base == 0 && (a.mask[row] & (at.n < 64 ? (1ull << at.n) - 1 : ~0ull)) == 0;
         const float inv = none ? 0.f : 1.f / L;
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-        const float f0 = mine[1] * scale(mine) * inv;            // the split's share of the row's weights
+        const float f0 = own * inv;                  // the split's share of the row's weights
 #pragma unroll
         for (int i = 0; i < UNROLL; ++i) {
             const int s = set + i * SETS;
@@ -818,7 +810,7 @@ RowsAttnPlan rows_attn_plan(int dtype, int n_q, int n_kv, int head_dim, int batc
     const double partial = 2.0 * rows * n_q * head_dim * 4;
     // of the slots, the share that an average row sees
     const double seen = 1.0 - 0.5 * std::min(1.0, (double)rows / batch / max_len);
-    const int most = std::min(64, (max_len + KEYS - 1) / KEYS);
+    const int most = std::min(PARTS_MAX, (max_len + KEYS - 1) / KEYS);
     const double full = tree && batch > 1 ? 0.7 : 1.0;
     double best = 0;
     for (int tiles = half && each <= 64 ? 4 : 2; tiles <= 4; tiles += 2) {
