@@ -712,10 +712,14 @@ void k_rows_attn(RowsAttnArgs a) {
         lds_sync();
         if (!w.run(&s_bad, &s_odd, m, l)) return;
     }
-    // everything is found anew, so that the first pass keeps no registers for this one
+    // everything is found anew, the arguments too, so that the first pass keeps no registers
+    // for this one (scalars, spilled to lanes, took a call of few stages 0.5 us)
     int block = blockIdx.x;
-    asm volatile("" : "+s"(block));
-    RowsWork<T, HD, RW, KW> w(a, smem);
+    auto* kernarg = (const __attribute__((address_space(4))) RowsAttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(block), "+s"(kernarg));
+    RowsAttnArgs b;
+    __builtin_memcpy(&b, (const RowsAttnArgs*)kernarg, sizeof b);
+    RowsWork<T, HD, RW, KW> w(b, smem);
     if (w.place(block)) w.again(s_bad != 0);
 }
 
