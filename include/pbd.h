@@ -672,9 +672,9 @@ int pbd_tree_commit(const pbd_pages* pages, int32_t n_layers, int32_t batch, int
  * int32 [batch]) are the lengths that the plan was given, lens its new_lens.  A sequence
  * whose lens[b] is not before[b] + n was not served: it is skipped, with no status of its
  * own.  A sequence that is skipped, for this or any other reason, or has no rows keeps
- * its cache as it is and has new_lens[b] = lens[b], n_accepted[b] = -1 and -1 all along path
- * and out_tokens; its anchor stays as it was.  So new_lens can go to the next plan
- * and to pbd_page_release with no look at it by the host.  Everything else as
+ * its cache as it is and has the length that it had, new_lens[b] = before[b], n_accepted[b]
+ * = -1 and -1 all along path and out_tokens; its anchor stays as it was.  So new_lens can go
+ * to the next plan and to pbd_page_release with no look at it by the host.  Everything else as
  * pbd_tree_commit.
  */
 int pbd_tree_commit_served(const pbd_pages* pages, int32_t n_layers, int32_t batch, int32_t rows, const int32_t* row_start,

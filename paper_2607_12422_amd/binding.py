@@ -604,7 +604,7 @@ def pbd_tree_commit(pages: PbdPages, row_start, lens, parent, tokens, verify, pa
 def pbd_tree_commit_served(pages: PbdPages, row_start, before, lens, parent, tokens, verify, path, n_accepted, out_tokens,
                            new_lens, anchor=None, stream=None):
     """As pbd_tree_commit; before int32 [batch]: the lengths that the plan was given (lens: its new_lens).  Sequences that
-    it did not serve keep all they have, with new_lens = lens and n_accepted = -1."""
+    it did not serve, or whose tree is bad, keep all they have, with new_lens = before and n_accepted = -1."""
     dev, B, R = pages.device, lens.numel(), parent.numel()
     if B > pages.rows:
         raise PbdError(PBD_ERR_INVALID_ARG, "the table has fewer rows than lens")

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void k_tree_commit(TreeCommitArgs a) {
         for (int i = threadIdx.x; i < a.width; i += 256) a.path[(size_t)b * a.width + i] = a.out_tokens[(size_t)b * a.width + i] = -1;
         if (threadIdx.x == 0) {
             a.n_accepted[b] = -1;
-            a.new_lens[b] = len;
+            a.new_lens[b] = a.before[b];
         }
     };
     const bool slots = rows_ok && !(a.before && base != a.before[b]);

@@ -213,3 +213,34 @@ def test_one_workspace_for_batches_that_shrink(trees):
         c.run()
         c.check()
     assert max(need) > need[0] and max(need) <= ws.numel()
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 64)])
+def test_parts_whose_every_score_is_infinite(dtype, D):
+    """Keys that make scores of -inf along whole parts, before, between and behind the others: those slots have weight 0.
+    Where a row sees nothing else it is NaN, as in fp32 arithmetic, and so is a row with a score of +inf."""
+    n, R = 3000, 40
+    for first, end in ((0, 1500), (700, 2000), (2500, 2960), (0, 2940)):
+        cache = ref.Cache([n], 1, D, dtype, seed=5)
+        cache.dk[0, 0, first:end, 0] = -math.inf
+        cache.put(0, 0, cache.dk[0, :, :n], cache.dv[0, :, :n])
+        c = Call(cache, [R], 2)
+        assert c.ws.numel() > 256
+        c.q[..., 0] = c.q[..., 0].abs() + 0.5
+        c.dq.copy_(c.q.to(DEV))
+        c.run()
+        out, lse = c.out.double().cpu()[:R], c.lse.double().cpu()[:R]
+        see = rr.causal(R, n)
+        see[:, first:end] = False
+        cache.dk[0, 0, first:end, 0] = 0.0
+        o, s, tol, s_tol = rr.attention(cache, 0, c.q[:R], see, D ** -0.5)
+        assert torch.all((out - o).abs() <= tol), (first, end)
+        assert torch.all((lse - s).abs() <= s_tol)
+    cache.dk[0, 0, :, 0] = -math.inf
+    cache.dk[0, 0, n - 10, 0] = math.inf
+    cache.put(0, 0, cache.dk[0, :, :n], cache.dv[0, :, :n])
+    c = Call(cache, [R], 2)
+    c.q[..., 0] = 1.0
+    c.dq.copy_(c.q.to(DEV))
+    c.run()
+    assert torch.isnan(c.out[:R]).all() and torch.all(c.lse[: R - 10] == -math.inf) and torch.isnan(c.lse[R - 10: R]).all()

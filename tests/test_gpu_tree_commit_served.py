@@ -21,11 +21,11 @@ def served(c, before, lens=None, parents=None, starts=None):
     torch.cuda.synchronize()
 
 
-def check(c, kept, lens=None):
-    """As c.check, with the outputs of the sequences `kept` those of skipped ones."""
+def check(c, kept, before):
+    """As c.check, with the outputs of the sequences `kept` those of skipped ones: the lengths they had."""
     for b in kept:
         assert torch.all(c.path[b] == -1) and torch.all(c.out[b] == -1)
-        assert int(c.n[b]) == -1 and int(c.new[b]) == (lens or c.lens)[b] and int(c.anchor[b]) == -77
+        assert int(c.n[b]) == -1 and int(c.new[b]) == before[b] and int(c.anchor[b]) == -77
         for o in (c.path, c.out, c.n, c.new):
             o[b] = -77
     c.check(skip=kept)
@@ -43,12 +43,13 @@ def test_sequences_that_were_not_served_keep_all_they_have(dtype, D):
     base = [m - n for m, n in zip(lens, sizes)]
     c = Commit(lens, trees(sizes), 2, D, dtype, right=1.0)
     served(c, base)
-    check(c, (4,))
+    check(c, (4,), base)
     assert int(c.status) == 0
     # 1, 2, 3 and 5: the length has not grown, their rows are there
     c = Commit(lens, trees(sizes), 2, D, dtype, right=1.0)
-    served(c, [base[0], 40, 50, 64, 20, 17])
-    check(c, (1, 2, 3, 4, 5))
+    before = [base[0], 40, 50, 64, 20, 17]
+    served(c, before)
+    check(c, (1, 2, 3, 4, 5), before)
     assert int(c.status) == 0
 
 
@@ -57,13 +58,13 @@ def test_fewer_slots_than_rows_and_lengths_out_of_range():
     # a sequence with fewer slots than rows, not served: nothing wrong with it
     c = Commit(lens, trees(sizes), 2, 64, BF, right=1.0)
     served(c, [21, 5, 43], lens=[30, 5, 50])
-    check(c, (1,), lens=[30, 5, 50])
+    check(c, (1,), [21, 5, 43])
     assert int(c.status) == 0
     # lengths that no cache has, and slots before the first
     for length, before in ((-5, -17), (-5, -5), (5, -7), (10 ** 6, 10 ** 6 - 12), (10 ** 6, 10 ** 6), (-2 ** 31, 2 ** 31 - 12)):
         c = Commit(lens, trees(sizes), 2, 64, BF, right=1.0)
         served(c, [21, before, 43], lens=[30, length, 50])
-        check(c, (1,), lens=[30, length, 50])
+        check(c, (1,), [21, before, 43])
         assert int(c.status) == pbd.PBD_STATUS_CAPACITY
 
 
@@ -75,20 +76,20 @@ def test_other_commits_that_are_skipped():
         t = list(c.trees[1])
         t[5] = bad
         served(c, base, parents=[c.trees[0], t, c.trees[2]])
-        check(c, (1,))
+        check(c, (1,), base)
         assert int(c.status) == pbd.PBD_STATUS_TREE
     c = Commit(lens, trees(sizes), 2, 64, BF)
     t = c.table.clone()
     t[1, 2] = -1
     c.pages = pbd.make_pages(c.k, c.v, t.to(DEV), n_q_heads=2, head_dim=64, status=c.status)
     served(c, base)
-    check(c, (1,))
+    check(c, (1,), base)
     assert int(c.status) == pbd.PBD_STATUS_PAGE
     c = Commit(lens, trees(sizes), 2, 64, BF)
     c.width = 9
     c.path, c.out = c.path[:, :9].contiguous(), c.out[:, :9].contiguous()
     served(c, base)
-    check(c, (1,))
+    check(c, (1,), base)
     assert int(c.status) == pbd.PBD_STATUS_CAPACITY
 
 
