@@ -602,7 +602,7 @@ int pbd_paged_append_rows(const pbd_pages* pages, int32_t rows, const float* q, 
  * Slots that a row does not see never reach it, whatever they hold; infinite and NaN
  * elements of slots that it sees count as in fp32 arithmetic.  Finite values up to 2^127
  * have finite outputs, whatever the finite scores: tiles whose sums would not be are gone
- * over a second time, as those that meet a NaN, at several times the cost.  Rows behind the last
+ * over a second time, as those that meet a NaN, at about ten times the cost.  Rows behind the last
  * sequence stay as they were.  Results are bitwise the same from run to run; they depend
  * on a sequence's own data and on batch, rows and max_len.
  * out and lse overlap no input.

@@ -205,6 +205,14 @@ template <typename T> __device__ __forceinline__ T elem(const typename VRaw<T>::
     return x[e];
 }
 
+// Whether a lane's four values are: no exponent of ones.
+template <typename T> __device__ __forceinline__ bool finite(const typename VRaw<T>::t& v) {
+    bool all = true;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) all &= __builtin_isfinite(to_f32(elem<T>(v, e)));
+    return all;
+}
+
 // acc += V P over the 16 slots of a block: v0, v1 the lane's slots 4h.. and 8 + 4h.. of
 // its dim, p its eight weights in that order.
 template <typename T>
@@ -224,17 +232,31 @@ __device__ __forceinline__ void mma_block(f32x16& acc, const typename VRaw<T>::t
 }
 
 // The same where some slots are hidden from some rows and values may be infinite or
-// NaN: the product of the finite values, and for the others what their weights make of
-// them, counted by products of ones (seen: bits 0 .. 3 and 8 .. 11, for the weights in turn).
+// NaN: the product of the finite values, and for the others, if there are any, what their
+// weights make of them, counted by products of ones (seen: bits 0 .. 3 and 8 .. 11, for the
+// weights in turn).  What the values are is kept as bits of a lane: as masks of lanes it
+// spilled scalars all over the kernel, 0.4 us of a call of few stages.
 template <typename T>
 __device__ __forceinline__ void mma_block_careful(f32x16& acc, const typename VRaw<T>::t& v0, const typename VRaw<T>::t& v1,
                                                   const T (&p)[8], unsigned seen) {
-    T x[8], w[8], part[8];
+    if (__all(finite<T>(v0) && finite<T>(v1))) {
+        mma_block<T>(acc, v0, v1, p);
+        settle<T>();
+        return;
+    }
+    T w[8], part[8];
+    unsigned plus = 0, minus = 0, nan = 0, some = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        x[i] = i < 4 ? elem<T>(v0, i & 3) : elem<T>(v1, i & 3);
-        part[i] = __builtin_isfinite(to_f32(x[i])) ? x[i] : from_f32<T>(0.f);
+        const T x = i < 4 ? elem<T>(v0, i & 3) : elem<T>(v1, i & 3);
+        const float f = to_f32(x);
+        plus |= (f == INFINITY) << i;
+        minus |= (f == -INFINITY) << i;
+        nan |= (f != f) << i;
+        some |= (to_f32(p[i]) > 0.f) << i;
+        part[i] = __builtin_isfinite(f) ? x : from_f32<T>(0.f);
     }
+    const unsigned sees = (seen & 15) | (seen >> 4 & 0xf0);
     auto raw = [](const T* e) {
         typename VRaw<T>::t r;
         __builtin_memcpy(&r, e, sizeof r);
@@ -245,12 +267,12 @@ __device__ __forceinline__ void mma_block_careful(f32x16& acc, const typename VR
     // infinite values under a weight, in either sign; NaN, and infinite ones under none
 #pragma unroll 1
     for (int kind = 0; kind < 4; ++kind) {
+        const unsigned hit = kind == 0 ? plus : kind == 1 ? minus : kind == 2 ? nan : plus | minus;
+        const unsigned use = kind < 2 ? sees & some : kind == 2 ? sees : sees & ~some;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float f = to_f32(x[i]);
-            const bool inf = __builtin_isinf(f), sees = (seen >> (i < 4 ? i : 4 + i) & 1) != 0, some = to_f32(p[i]) > 0.f;
-            part[i] = one_if<T>(kind == 0 ? f == INFINITY : kind == 1 ? f == -INFINITY : kind == 2 ? f != f : inf);
-            w[i] = one_if<T>(sees && (kind < 2 ? some : kind == 2 || !some));
+            part[i] = one_if<T>((hit >> i & 1) != 0);
+            w[i] = one_if<T>((use >> i & 1) != 0);
         }
         f32x16 c;
 #pragma unroll
@@ -283,7 +305,8 @@ __device__ __forceinline__ float log_sum(float M, float L, bool none) {
 // rare enough to be looked for in the result: a work-group whose sums hold a NaN
 // goes over its slots again, 32 dims at a time, with products that leave them out.  So
 // does one whose sums are infinite: weights up to HIGH, or many at once, take large finite
-// values there, and the second pass' weights, whose sum is at most 1, do not.
+// values there, and the second pass' weights, whose sum is at most 1, do not.  Where all
+// of them do, two prompts of 8192 tokens take 6.3 ms, one tree of 17 over 4096 slots 46 us.
 // A split writes the weighted means of its slots' values, its maximum and its sum.
 // ---------------------------------------------------------------------------
 template <typename T, int HD, int RW, int KW>
@@ -609,7 +632,8 @@ struct RowsWork {
             if (__any(live && !__builtin_isfinite(one)) && lane == 0) *s_odd = 1;
         }
         lds_sync();                                  // s_bad and s_odd are final, the ring may be filled again
-        const bool redo = *s_odd != 0, bad = *s_bad != 0;
+        // (scalars: a branch of the lanes' would keep these sums through the second pass)
+        const bool redo = __builtin_amdgcn_readfirstlane(*s_odd) != 0, bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
         if (bad && threadIdx.x == 0) raise(a.pg.status, PBD_STATUS_PAGE);
         if (kw == 0 && live && h == 0) {
             const size_t part_row = head_row * a.splits + split;
@@ -698,8 +722,10 @@ struct RowsWork {
     }
 };
 
+// (three waves a SIMD at 64 dims in bf16, which the second pass' registers would not leave by
+// themselves: two prompts of 4096 tokens 92 us so and 109 with two)
 template <typename T, int HD, int RW, int KW>
-__global__ __launch_bounds__(RW * KW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && HD == 128 ? 1 : 2)))
+__global__ __launch_bounds__(RW * KW * 64) __attribute__((amdgpu_waves_per_eu(HD == 64 ? sizeof(T) == 2 ? 3 : 2 : sizeof(T) == 2 ? 2 : 1)))
 void k_rows_attn(RowsAttnArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ int s_bad, s_odd;
@@ -712,14 +738,10 @@ void k_rows_attn(RowsAttnArgs a) {
         lds_sync();
         if (!w.run(&s_bad, &s_odd, m, l)) return;
     }
-    // everything is found anew, the arguments too, so that the first pass keeps no registers
-    // for this one (scalars, spilled to lanes, took a call of few stages 0.5 us)
+    // everything is found anew, so that the first pass keeps no registers for this one
     int block = blockIdx.x;
-    auto* kernarg = (const __attribute__((address_space(4))) RowsAttnArgs*)__builtin_amdgcn_kernarg_segment_ptr();
-    asm volatile("" : "+s"(block), "+s"(kernarg));
-    RowsAttnArgs b;
-    __builtin_memcpy(&b, (const RowsAttnArgs*)kernarg, sizeof b);
-    RowsWork<T, HD, RW, KW> w(b, smem);
+    asm volatile("" : "+s"(block));
+    RowsWork<T, HD, RW, KW> w(a, smem);
     if (w.place(block)) w.again(s_bad != 0);
 }
 
