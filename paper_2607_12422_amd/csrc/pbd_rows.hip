@@ -16,13 +16,14 @@
 // Bounds.  Many rows: the matrix cores and the vector units, which the two waves of a
 // SIMD hardly use at the same time.  A step of 32 rows and 32 slots of 128 dims is 512
 // cycles of products, 256 of exponentials (16 a wave, 16 cycles each) and about 250 of
-// other vector work, and takes 1000; the matrix cores are 46 % busy.  Two prompts of
+// other vector work, and takes 1000; the matrix cores are 47 to 48 % busy.  Two prompts of
 // 8192 tokens, 16 / 8 heads of 128 in bf16: 521 to 570 us, 0.95 to 1.04 PFLOP/s (an 8192^3
 // product of the library 1.1 to 1.3); 70 us less where no stage is loaded, 75 less again
 // without exponentials, no change without barriers.  Few rows: the cache's bytes.  32
 // trees of 33 nodes over 8192 slots (1.08 GB) take 205 us, 5.2 TB/s, of 17 nodes 185, 5.8.
 // One tree of 17 over 4096 takes 13 to 15 us: two launches, the waits of a part and the
-// join.
+// join.  In fp32 a product of 32 x 32 x 2 is 64 cycles: a prompt of 129 rows of 64 dims has 64
+// of them a stage and wave, three stages one after the other, 5 of its 12 us.
 //
 // Tried and not kept: a wave of its own for the loads (972 us where the computing waves
 // took 575 then); rings of three and four stages, or of half stages (570 to 775 against
